@@ -19,7 +19,7 @@
  * Conventions as in bitlinear.h: device pointers end in _dev, no entry point allocates, frees or
  * synchronizes, `stream` is a hipStream_t (NULL = default stream), errors are bl_status codes and
  * nothing is launched when one is returned.  All floating-point data here is fp32 except the
- * key/value cache (bf16 bit patterns).
+ * key/value cache (bf16 bit patterns, or int8 codes with fp32 scales: bl_kv8_cache).
  */
 #ifndef BITLINEAR_DECODER_H
 #define BITLINEAR_DECODER_H
@@ -262,6 +262,145 @@ typedef struct bl_attn_prefill_args {
 uint64_t bl_attn_prefill_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M);
 
 bl_status bl_attn_prefill(const bl_attn_prefill_args *args, void *stream);
+
+/*
+ * The 8-bit key/value cache.  A position's key and value are stored per key head as head_dim int8 codes and one fp32 scale, quantized as
+ * bl_quant_act quantizes a row: amax = max|x|, inv = 127 / amax, code = clip(round_half_even(x * inv)), scale = amax / 127; a head
+ * whose inv is not finite: codes 0, scale 0.  Half of the bf16 cache's bytes, several sequences per call, and key heads that several query
+ * heads share.
+ *   n_heads      key heads; head_dim a multiple of 4 (4 .. BL_ATTN_MAX_HEAD_DIM)
+ *   k_codes_dev, v_codes_dev   sequences * bl_kv8_code_bytes(n_heads, head_dim, max_pos) bytes each, 16-byte aligned
+ *   k_scale_dev, v_scale_dev   sequences * bl_kv8_scale_count(n_heads, max_pos) floats each, 16-byte aligned
+ * Layout (S = head_dim rounded up to 16, C = max_pos / BL_KV8_CHUNK rounded up): codes [sequence][key head][C][64 * S], scales
+ * [sequence][key head][64 * C].  In a chunk of 64 positions, position p and dim e: the key's code at 4096 * (e / 64) + (16 * (p % 4) + p % 64 / 4) *
+ * min(64, S - 64 * (e / 64)) + e % 64, the value's at 64 * e + p % 64.  The padding dims are written as zero with their row; rows that were
+ * never written may hold anything.
+ */
+#define BL_KV8_CHUNK 64
+#define BL_ATTN8_MAX_GROUP 64      /* query heads per key head */
+#define BL_ATTN8_MAX_BATCH 1024    /* sequences of one launch */
+
+typedef struct bl_kv8_cache {
+    int8_t *k_codes_dev;
+    int8_t *v_codes_dev;
+    float  *k_scale_dev;
+    float  *v_scale_dev;
+    int32_t n_heads;
+    int32_t head_dim;
+    int32_t max_pos;
+    int32_t sequences;
+} bl_kv8_cache;
+
+/* Bytes of k_codes_dev (and of v_codes_dev), floats of k_scale_dev (and of v_scale_dev) per sequence; 0 if a shape is out of range. */
+uint64_t bl_kv8_code_bytes(int32_t n_heads, int32_t head_dim, int32_t max_pos);
+uint64_t bl_kv8_scale_count(int32_t n_heads, int32_t max_pos);
+
+/*
+ * Rows pos0 .. pos0 + M - 1 of one sequence into the cache.  All other rows keep their bytes.
+ *   k_dev, v_dev     [M, ld] fp32 or bf16 (dt), ld >= n_heads * head_dim elements; aligned to the element
+ *   rope_table_dev   the table of bl_rope_table: the key of row r is rotated by the table's row r (fp32: two products and a sum, each
+ *                    rounded) before it is quantized.  NULL: keys are stored as they are (already rotated ones).  The rows of a cache
+ *                    that continues another one have later angles: pass the address of the row that belongs to position 0.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also a sequence or rows beyond the cache, ld too small), BL_ERR_DTYPE, BL_ERR_ALIGN, BL_ERR_HIP.
+ */
+typedef struct bl_kv8_write_args {
+    const bl_kv8_cache *cache;      /* host */
+    const void  *k_dev;
+    const void  *v_dev;
+    const float *rope_table_dev;
+    int64_t      ld;
+    int32_t      dt;                /* bl_dtype */
+    int32_t      sequence;
+    int32_t      pos0;
+    int32_t      M;
+} bl_kv8_write_args;
+
+bl_status bl_kv8_write(const bl_kv8_write_args *args, void *stream);
+
+/*
+ * The values that rows pos0 .. pos0 + M - 1 of one sequence stand for, code * scale, as [M, ld] fp32 or bf16 (one rounding); keys as they
+ * are stored, rotated.  k_out_dev or v_out_dev may be NULL, not both.  Columns behind n_heads * head_dim are not touched.
+ * Errors: as for bl_kv8_write.
+ */
+typedef struct bl_kv8_read_args {
+    const bl_kv8_cache *cache;      /* host */
+    void    *k_out_dev;
+    void    *v_out_dev;
+    int64_t  ld;
+    int32_t  dt;                    /* bl_dtype */
+    int32_t  sequence;
+    int32_t  pos0;
+    int32_t  M;
+} bl_kv8_read_args;
+
+bl_status bl_kv8_read(const bl_kv8_read_args *args, void *stream);
+
+/*
+ * bl_attn_decode over 8-bit caches, for one token of each of `cache.sequences` sequences, which may share a prefix.
+ * Sequence b's token has position pos = pos_dev[b] (read on the device).  Its key (rotated by the table's row pos) and value go into row
+ * pos - prefix_len of its own cache; then, per query head, softmax over rows 0 .. prefix_len - 1 of the prefix cache and rows
+ * 0 .. pos - prefix_len of its own, scores scaled by 1 / sqrt(head_dim).  Query head i reads key head i / (n_q_heads / cache.n_heads).
+ * The prefix is read once for all sequences.  A sequence whose position is outside prefix_len .. prefix_len + cache.max_pos - 1 takes no part:
+ * its cache and its row of out_dev stay as they are.
+ *   q_lin_dev [sequences, n_q_heads * head_dim] fp32; k_lin_dev, v_lin_dev [sequences, cache.n_heads * head_dim] fp32; rows contiguous
+ *   pos_dev        [sequences] int32
+ *   rope_table_dev rows 0 .. prefix_len + cache.max_pos - 1
+ *   prefix         NULL with prefix_len 0, or a cache of the same heads and head size whose first sequence holds rows 0 .. prefix_len - 1
+ *   scratch_dev    bl_attn8_scratch_bytes(...) bytes, 16-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
+ *                  the next.  Calls that may overlap in time must not share it.
+ * Arithmetic: the queries enter as 24-bit fixed-point numbers (relative to their row's largest value), the weights as fixed-point numbers of
+ * at least 22 bits (relative to their chunk's largest), the codes as they are; integer sums are exact, everything else is fp32.
+ * Nobody waits for anybody: the workgroups of a row leave their figures in scratch_dev, the last one adds them up, in a fixed order:
+ * a call repeated gives the same bits.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache.n_heads, a prefix of another shape), BL_ERR_ALIGN, BL_ERR_HIP.
+ */
+typedef struct bl_attn8_args {
+    const float        *q_lin_dev;
+    const float        *k_lin_dev;
+    const float        *v_lin_dev;
+    const int32_t      *pos_dev;
+    const float        *rope_table_dev;
+    float              *out_dev;
+    void               *scratch_dev;
+    bl_kv8_cache        cache;
+    bl_kv8_cache        prefix;      /* read if prefix_len > 0 */
+    int32_t             n_q_heads;
+    int32_t             prefix_len;
+} bl_attn8_args;
+
+/* Bytes of bl_attn8_args.scratch_dev; 0 if a shape is out of range. */
+uint64_t bl_attn8_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t max_pos, int32_t sequences,
+                                int32_t prefix_len);
+
+bl_status bl_attn8_decode(const bl_attn8_args *args, void *stream);
+
+/*
+ * bl_attn_prefill over an 8-bit cache: M consecutive tokens of one sequence at positions pos0 .. pos0 + M - 1 go into the cache
+ * (bl_kv8_write's bytes), then token m attends to rows 0 .. pos0 + m.  Two launches.
+ *   q_lin_dev [M, n_q_heads * head_dim], k_lin_dev, v_lin_dev [M, cache->n_heads * head_dim] fp32, rows contiguous
+ *   out_dev      [M, n_q_heads * head_dim] fp32
+ *   scratch_dev  bl_attn8_prefill_scratch_bytes(...) bytes, 16-byte aligned, contents free
+ * 0 <= pos0, pos0 + M <= max_pos, 1 <= M <= 65535.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE, BL_ERR_ALIGN, BL_ERR_HIP.
+ */
+typedef struct bl_attn8_prefill_args {
+    const float        *q_lin_dev;
+    const float        *k_lin_dev;
+    const float        *v_lin_dev;
+    const float        *rope_table_dev;
+    float              *out_dev;
+    void               *scratch_dev;
+    bl_kv8_cache        cache;
+    int32_t             n_q_heads;
+    int32_t             sequence;
+    int32_t             pos0;
+    int32_t             M;
+} bl_attn8_prefill_args;
+
+/* Bytes of bl_attn8_prefill_args.scratch_dev; 0 if a shape is out of range. */
+uint64_t bl_attn8_prefill_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M);
+
+bl_status bl_attn8_prefill(const bl_attn8_prefill_args *args, void *stream);
 
 /*
  * A model's last norm, y = rmsnorm(h + delta, gamma) without a quantizer (bl_norm_quant's arithmetic in mode

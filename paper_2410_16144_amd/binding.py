@@ -36,6 +36,8 @@ DECLARED_SYMBOLS = (
     "bl_quant_act", "bl_quant_act_batch", "bl_gemv", "bl_gemv_batch", "bl_gemv_batch_static", "bl_decode_batch", "bl_gemm", "bl_gemm_batch", "bl_set_tuning", "bl_get_stat", "bl_status_str", "bl_last_hip_error", "bl_last_kernel", "bl_version",
     "bl_tl2_padded_k", "bl_tl2_desc_init", "bl_tl2_pack", "bl_tl2_unpack", "bl_tl2_gemv", "bl_tl2_gemv_batch",
     "bl_norm_quant", "bl_final_norm", "bl_rope_table", "bl_attn_scratch_bytes", "bl_attn_decode", "bl_pos_advance", "bl_decode_norm_batch", "bl_pack_gate_up", "bl_attn_prefill", "bl_attn_prefill_scratch_bytes",
+    "bl_kv8_code_bytes", "bl_kv8_scale_count", "bl_kv8_write", "bl_kv8_read", "bl_attn8_scratch_bytes", "bl_attn8_decode",
+    "bl_attn8_prefill_scratch_bytes", "bl_attn8_prefill",
 )
 
 BL_NORM_MAX_K = 49152
@@ -43,6 +45,9 @@ BL_NORM_SCRATCH_BYTES = 256
 BL_ATTN_MAX_HEAD_DIM = 256
 BL_ATTN_CHUNK = 64
 BL_ATTN_BLOCK_MAX_HEAD_DIM = 128
+BL_KV8_CHUNK = 64
+BL_ATTN8_MAX_GROUP = 64
+BL_ATTN8_MAX_BATCH = 1024
 BL_NORM_PLAIN, BL_NORM_RESIDUAL, BL_NORM_GATED, BL_NORM_PREMULTIPLIED = 0, 1, 2, 3
 BL_DECODE_NORM_MAX_K = 16384
 
@@ -127,6 +132,42 @@ class AttnPrefillArgs(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("max_pos", ctypes.c_int32), ("pos0", ctypes.c_int32), ("M", ctypes.c_int32)]
 
 
+class Kv8Cache(ctypes.Structure):
+    """Mirror of bl_kv8_cache."""
+    _fields_ = [("k_codes_dev", ctypes.c_void_p), ("v_codes_dev", ctypes.c_void_p), ("k_scale_dev", ctypes.c_void_p),
+                ("v_scale_dev", ctypes.c_void_p), ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("max_pos", ctypes.c_int32), ("sequences", ctypes.c_int32)]
+
+
+class Kv8WriteArgs(ctypes.Structure):
+    """Mirror of bl_kv8_write_args."""
+    _fields_ = [("cache", ctypes.POINTER(Kv8Cache)), ("k_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
+                ("rope_table_dev", ctypes.c_void_p), ("ld", ctypes.c_int64), ("dt", ctypes.c_int32), ("sequence", ctypes.c_int32),
+                ("pos0", ctypes.c_int32), ("M", ctypes.c_int32)]
+
+
+class Kv8ReadArgs(ctypes.Structure):
+    """Mirror of bl_kv8_read_args."""
+    _fields_ = [("cache", ctypes.POINTER(Kv8Cache)), ("k_out_dev", ctypes.c_void_p), ("v_out_dev", ctypes.c_void_p),
+                ("ld", ctypes.c_int64), ("dt", ctypes.c_int32), ("sequence", ctypes.c_int32), ("pos0", ctypes.c_int32), ("M", ctypes.c_int32)]
+
+
+class Attn8Args(ctypes.Structure):
+    """Mirror of bl_attn8_args."""
+    _fields_ = [("q_lin_dev", ctypes.c_void_p), ("k_lin_dev", ctypes.c_void_p), ("v_lin_dev", ctypes.c_void_p),
+                ("pos_dev", ctypes.c_void_p), ("rope_table_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
+                ("scratch_dev", ctypes.c_void_p), ("cache", Kv8Cache), ("prefix", Kv8Cache), ("n_q_heads", ctypes.c_int32),
+                ("prefix_len", ctypes.c_int32)]
+
+
+class Attn8PrefillArgs(ctypes.Structure):
+    """Mirror of bl_attn8_prefill_args."""
+    _fields_ = [("q_lin_dev", ctypes.c_void_p), ("k_lin_dev", ctypes.c_void_p), ("v_lin_dev", ctypes.c_void_p),
+                ("rope_table_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p), ("scratch_dev", ctypes.c_void_p),
+                ("cache", Kv8Cache), ("n_q_heads", ctypes.c_int32), ("sequence", ctypes.c_int32), ("pos0", ctypes.c_int32),
+                ("M", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -179,6 +220,16 @@ def lib():
     l.bl_attn_prefill.argtypes = [ctypes.POINTER(AttnPrefillArgs), vp]
     l.bl_attn_prefill_scratch_bytes.argtypes = [i32, i32, i32, i32]
     l.bl_attn_prefill_scratch_bytes.restype = ctypes.c_uint64
+    l.bl_kv8_code_bytes.argtypes = [i32, i32, i32]
+    l.bl_kv8_scale_count.argtypes = [i32, i32]
+    l.bl_attn8_scratch_bytes.argtypes = [i32] * 6
+    l.bl_attn8_prefill_scratch_bytes.argtypes = [i32] * 5
+    for f in (l.bl_kv8_code_bytes, l.bl_kv8_scale_count, l.bl_attn8_scratch_bytes, l.bl_attn8_prefill_scratch_bytes):
+        f.restype = ctypes.c_uint64
+    l.bl_kv8_write.argtypes = [ctypes.POINTER(Kv8WriteArgs), vp]
+    l.bl_kv8_read.argtypes = [ctypes.POINTER(Kv8ReadArgs), vp]
+    l.bl_attn8_decode.argtypes = [ctypes.POINTER(Attn8Args), vp]
+    l.bl_attn8_prefill.argtypes = [ctypes.POINTER(Attn8PrefillArgs), vp]
     l.bl_set_tuning.argtypes = [ctypes.c_char_p, i32]
     l.bl_get_stat.argtypes = [ctypes.c_char_p]
     l.bl_get_stat.restype = i64
@@ -190,7 +241,8 @@ def lib():
     for name in ("bl_packed_desc_init", "bl_pack_ternary", "bl_unpack_ternary", "bl_quant_act", "bl_quant_act_batch", "bl_gemv",
                  "bl_gemv_batch", "bl_decode_batch", "bl_gemm", "bl_set_tuning", "bl_tl2_desc_init", "bl_tl2_pack",
                  "bl_tl2_unpack", "bl_tl2_gemv", "bl_tl2_gemv_batch", "bl_norm_quant", "bl_final_norm", "bl_rope_table", "bl_attn_decode",
-                 "bl_pos_advance", "bl_decode_norm_batch", "bl_attn_prefill", "bl_gemm_batch", "bl_gemv_batch_static", "bl_pack_gate_up"):
+                 "bl_pos_advance", "bl_decode_norm_batch", "bl_attn_prefill", "bl_gemm_batch", "bl_gemv_batch_static", "bl_pack_gate_up",
+                 "bl_kv8_write", "bl_kv8_read", "bl_attn8_decode", "bl_attn8_prefill"):
         getattr(l, name).restype = ctypes.c_int
     _lib = l
     return l
@@ -198,7 +250,7 @@ def lib():
 
 _calls = None
 # bl_calls.cpp: the `which` of calls().launch
-LAUNCH_GEMV_BATCH, LAUNCH_DECODE_BATCH, LAUNCH_QUANT_BATCH, LAUNCH_DECODE_NORM_BATCH, LAUNCH_TL2_BATCH, LAUNCH_ATTN_DECODE = range(6)
+LAUNCH_GEMV_BATCH, LAUNCH_DECODE_BATCH, LAUNCH_QUANT_BATCH, LAUNCH_DECODE_NORM_BATCH, LAUNCH_TL2_BATCH, LAUNCH_ATTN_DECODE, LAUNCH_ATTN8_DECODE = range(7)
 
 
 def calls():
@@ -230,12 +282,13 @@ def current_stream() -> int:
 
 
 def launch(which: int, items, M: int, workspace_dev: int = 0):
-    """One prepared launch on the current stream: items is the ctypes array of make_*_items (for LAUNCH_ATTN_DECODE the AttnArgs).
+    """One prepared launch on the current stream: items is the ctypes array of make_*_items (for LAUNCH_ATTN_DECODE the AttnArgs,
+    for LAUNCH_ATTN8_DECODE the Attn8Args).
     Anything else goes to the ctypes binding, which takes or refuses it as it always did.  Raises BitLinearError like the
     calls below."""
     of, call, where = _LAUNCHES[which]
     c = calls()
-    if c and (isinstance(items, ctypes.Array) and items._type_ is of or type(items) is AttnArgs is of):
+    if c and (isinstance(items, ctypes.Array) and items._type_ is of or type(items) is of and of in (AttnArgs, Attn8Args)):
         status = c.launch(which, items, M, workspace_dev or 0)
         if status is not None:
             return _check(status, where)
@@ -443,6 +496,51 @@ def bl_attn_prefill(q_lin_dev: int, k_lin_dev: int, v_lin_dev: int, rope_table_d
     _check(lib().bl_attn_prefill(ctypes.byref(args), stream), "bl_attn_prefill")
 
 
+def bl_kv8_code_bytes(n_heads: int, head_dim: int, max_pos: int) -> int:
+    return int(lib().bl_kv8_code_bytes(n_heads, head_dim, max_pos))
+
+
+def bl_kv8_scale_count(n_heads: int, max_pos: int) -> int:
+    return int(lib().bl_kv8_scale_count(n_heads, max_pos))
+
+
+def bl_kv8_write(cache: Kv8Cache, k_dev: int, v_dev: int, rope_table_dev: int, ld: int, dtype: int, sequence: int, pos0: int, M: int,
+                 stream: int = 0):
+    args = Kv8WriteArgs(ctypes.pointer(cache) if cache is not None else None, k_dev or None, v_dev or None, rope_table_dev or None, ld, dtype,
+                        sequence, pos0, M)
+    _check(lib().bl_kv8_write(ctypes.byref(args), stream or None), "bl_kv8_write")
+
+
+def bl_kv8_read(cache: Kv8Cache, k_out_dev: int, v_out_dev: int, ld: int, dtype: int, sequence: int, pos0: int, M: int, stream: int = 0):
+    args = Kv8ReadArgs(ctypes.pointer(cache) if cache is not None else None, k_out_dev or None, v_out_dev or None, ld, dtype, sequence, pos0, M)
+    _check(lib().bl_kv8_read(ctypes.byref(args), stream or None), "bl_kv8_read")
+
+
+def bl_attn8_scratch_bytes(n_q_heads: int, n_heads: int, head_dim: int, max_pos: int, sequences: int, prefix_len: int) -> int:
+    return int(lib().bl_attn8_scratch_bytes(n_q_heads, n_heads, head_dim, max_pos, sequences, prefix_len))
+
+
+def make_attn8_args(q_lin_dev: int, k_lin_dev: int, v_lin_dev: int, pos_dev: int, rope_table_dev: int, out_dev: int, scratch_dev: int,
+                    cache: Kv8Cache, n_q_heads: int, prefix: Kv8Cache = None, prefix_len: int = 0) -> Attn8Args:
+    return Attn8Args(q_lin_dev or None, k_lin_dev or None, v_lin_dev or None, pos_dev or None, rope_table_dev or None, out_dev or None,
+                     scratch_dev or None, cache, prefix if prefix is not None else Kv8Cache(), n_q_heads, prefix_len)
+
+
+def bl_attn8_decode(args: Attn8Args, stream: int = 0):
+    _check(lib().bl_attn8_decode(ctypes.byref(args), stream or None), "bl_attn8_decode")
+
+
+def bl_attn8_prefill_scratch_bytes(n_q_heads: int, n_heads: int, head_dim: int, pos0: int, M: int) -> int:
+    return int(lib().bl_attn8_prefill_scratch_bytes(n_q_heads, n_heads, head_dim, pos0, M))
+
+
+def bl_attn8_prefill(q_lin_dev: int, k_lin_dev: int, v_lin_dev: int, rope_table_dev: int, out_dev: int, scratch_dev: int, cache: Kv8Cache,
+                     n_q_heads: int, sequence: int, pos0: int, M: int, stream: int = 0):
+    args = Attn8PrefillArgs(q_lin_dev or None, k_lin_dev or None, v_lin_dev or None, rope_table_dev or None, out_dev or None,
+                            scratch_dev or None, cache, n_q_heads, sequence, pos0, M)
+    _check(lib().bl_attn8_prefill(ctypes.byref(args), stream or None), "bl_attn8_prefill")
+
+
 def bl_pos_advance(pos_dev: int, stream: int = 0):
     _check(lib().bl_pos_advance(pos_dev, stream), "bl_pos_advance")
 
@@ -486,4 +584,5 @@ _LAUNCHES = (
     (DecodeNormItem, lambda items, M, ws: bl_decode_norm_batch(items, ws, current_stream()), "bl_decode_norm_batch"),
     (GemvItem, lambda items, M, ws: bl_tl2_gemv_batch(items, ws, current_stream()), "bl_tl2_gemv_batch"),
     (AttnArgs, lambda items, M, ws: bl_attn_decode(items, current_stream()), "bl_attn_decode"),
+    (Attn8Args, lambda items, M, ws: bl_attn8_decode(items, current_stream()), "bl_attn8_decode"),
 )

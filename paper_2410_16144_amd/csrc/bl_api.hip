@@ -3,7 +3,7 @@
 #include <stdio.h>
 #include <string.h>
 
-#include "bl_internal.hpp"
+#include "bl_kv8.hpp"
 
 namespace {
 
@@ -567,6 +567,113 @@ bl_status bl_attn_prefill(const bl_attn_prefill_args* a, void* stream) {
         return BL_ERR_ALIGN;
     drop_stale_hip_error();
     return hip_status(bl::launch_attn_prefill(*a, static_cast<hipStream_t>(stream)));
+}
+
+// ---- the 8-bit cache
+
+static bool kv8_shape_ok(int32_t n_heads, int32_t head_dim, int32_t max_pos) {
+    return attn_shape_ok(n_heads, head_dim, max_pos);
+}
+
+uint64_t bl_kv8_code_bytes(int32_t n_heads, int32_t head_dim, int32_t max_pos) {
+    if (!kv8_shape_ok(n_heads, head_dim, max_pos)) return 0;
+    return (uint64_t)n_heads * bl::kv8_chunks(max_pos) * bl::kKv8Chunk * bl::kv8_size(head_dim);
+}
+
+uint64_t bl_kv8_scale_count(int32_t n_heads, int32_t max_pos) {
+    if (!kv8_shape_ok(n_heads, 4, max_pos)) return 0;
+    return (uint64_t)n_heads * bl::kv8_chunks(max_pos) * bl::kKv8Chunk;
+}
+
+static bl_status check_kv8(const bl_kv8_cache& c) {
+    if (!c.k_codes_dev || !c.v_codes_dev || !c.k_scale_dev || !c.v_scale_dev) return BL_ERR_NULL;
+    if (!kv8_shape_ok(c.n_heads, c.head_dim, c.max_pos) || c.sequences < 1) return BL_ERR_SHAPE;
+    if (!aligned(c.k_codes_dev, 16) || !aligned(c.v_codes_dev, 16) || !aligned(c.k_scale_dev, 16) || !aligned(c.v_scale_dev, 16)) return BL_ERR_ALIGN;
+    return BL_OK;
+}
+
+// Rows pos0 .. pos0 + M - 1 of a sequence, and the stride of their other side.
+static bl_status check_kv8_rows(const bl_kv8_cache* c, int64_t ld, int32_t dt, int32_t sequence, int32_t pos0, int32_t M) {
+    const bl_status s = check_kv8(*c);
+    if (s != BL_OK) return s;
+    if (dt != BL_F32 && dt != BL_BF16) return BL_ERR_DTYPE;
+    if (sequence < 0 || sequence >= c->sequences || pos0 < 0 || M < 1 || (int64_t)pos0 + M > c->max_pos || ld < (int64_t)c->n_heads * c->head_dim)
+        return BL_ERR_SHAPE;
+    return BL_OK;
+}
+
+bl_status bl_kv8_write(const bl_kv8_write_args* a, void* stream) {
+    if (!a || !a->cache || !a->k_dev || !a->v_dev) return BL_ERR_NULL;
+    const bl_status s = check_kv8_rows(a->cache, a->ld, a->dt, a->sequence, a->pos0, a->M);
+    if (s != BL_OK) return s;
+    const uintptr_t element = a->dt == BL_BF16 ? 2 : 4;
+    if (!aligned(a->k_dev, element) || !aligned(a->v_dev, element) || !aligned(a->rope_table_dev, 8)) return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return hip_status(bl::launch_kv8_write(*a, nullptr, 0, static_cast<hipStream_t>(stream)));
+}
+
+bl_status bl_kv8_read(const bl_kv8_read_args* a, void* stream) {
+    if (!a || !a->cache || (!a->k_out_dev && !a->v_out_dev)) return BL_ERR_NULL;
+    const bl_status s = check_kv8_rows(a->cache, a->ld, a->dt, a->sequence, a->pos0, a->M);
+    if (s != BL_OK) return s;
+    const uintptr_t element = a->dt == BL_BF16 ? 2 : 4;
+    if (!aligned(a->k_out_dev, element) || !aligned(a->v_out_dev, element)) return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return hip_status(bl::launch_kv8_read(*a, static_cast<hipStream_t>(stream)));
+}
+
+static bool attn8_heads_ok(int32_t n_q_heads, int32_t n_heads) {
+    return n_heads >= 1 && n_q_heads >= 1 && n_q_heads <= 65535 && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_ATTN8_MAX_GROUP;
+}
+
+static bool attn8_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t max_pos, int32_t sequences, int32_t prefix_len) {
+    return kv8_shape_ok(n_heads, head_dim, max_pos) && attn8_heads_ok(n_q_heads, n_heads) && sequences >= 1 && sequences <= BL_ATTN8_MAX_BATCH &&
+           prefix_len >= 0 && (prefix_len == 0 || kv8_shape_ok(n_heads, head_dim, prefix_len));
+}
+
+uint64_t bl_attn8_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t max_pos, int32_t sequences, int32_t prefix_len) {
+    if (!attn8_shape_ok(n_q_heads, n_heads, head_dim, max_pos, sequences, prefix_len)) return 0;
+    return (uint64_t)bl::attn8_scratch_bytes(n_heads, n_q_heads / n_heads, head_dim, max_pos, sequences, prefix_len);
+}
+
+bl_status bl_attn8_decode(const bl_attn8_args* a, void* stream) {
+    if (!a || !a->q_lin_dev || !a->k_lin_dev || !a->v_lin_dev || !a->pos_dev || !a->rope_table_dev || !a->out_dev || !a->scratch_dev) return BL_ERR_NULL;
+    bl_status s = check_kv8(a->cache);
+    if (s != BL_OK) return s;
+    if (!attn8_shape_ok(a->n_q_heads, a->cache.n_heads, a->cache.head_dim, a->cache.max_pos, a->cache.sequences, a->prefix_len)) return BL_ERR_SHAPE;
+    if (a->prefix_len > 0) {
+        s = check_kv8(a->prefix);
+        if (s != BL_OK) return s;
+        if (a->prefix.n_heads != a->cache.n_heads || a->prefix.head_dim != a->cache.head_dim || a->prefix_len > a->prefix.max_pos) return BL_ERR_SHAPE;
+    }
+    if (!aligned(a->q_lin_dev, 4) || !aligned(a->k_lin_dev, 4) || !aligned(a->v_lin_dev, 4) || !aligned(a->pos_dev, 4) ||
+        !aligned(a->rope_table_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
+        return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return hip_status(bl::launch_attn8_decode(*a, static_cast<hipStream_t>(stream)));
+}
+
+static bool attn8_prefill_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M) {
+    return prefill_shape_ok(n_heads, head_dim, pos0, M) && attn8_heads_ok(n_q_heads, n_heads);
+}
+
+uint64_t bl_attn8_prefill_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M) {
+    if (!attn8_prefill_shape_ok(n_q_heads, n_heads, head_dim, pos0, M)) return 0;
+    return (uint64_t)bl::attn8_prefill_scratch_bytes(n_heads, n_q_heads / n_heads, head_dim, pos0, M);
+}
+
+bl_status bl_attn8_prefill(const bl_attn8_prefill_args* a, void* stream) {
+    if (!a || !a->q_lin_dev || !a->k_lin_dev || !a->v_lin_dev || !a->rope_table_dev || !a->out_dev || !a->scratch_dev) return BL_ERR_NULL;
+    const bl_status s = check_kv8(a->cache);
+    if (s != BL_OK) return s;
+    if (!attn8_prefill_shape_ok(a->n_q_heads, a->cache.n_heads, a->cache.head_dim, a->pos0, a->M) || a->sequence < 0 ||
+        a->sequence >= a->cache.sequences || a->pos0 + a->M > a->cache.max_pos)
+        return BL_ERR_SHAPE;
+    if (!aligned(a->q_lin_dev, 4) || !aligned(a->k_lin_dev, 4) || !aligned(a->v_lin_dev, 4) || !aligned(a->rope_table_dev, 8) ||
+        !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
+        return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return hip_status(bl::launch_attn8_prefill(*a, static_cast<hipStream_t>(stream)));
 }
 
 bl_status bl_pos_advance(int32_t* pos_dev, void* stream) {

@@ -292,8 +292,8 @@ PyObject* final_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 // The prepared launches: launch(which, items, M, workspace) -> bl_status, on the current stream; None if `items`, a ctypes array (for
-// the last one the argument struct), does not hold whole ones of that launch's.
-enum { kGemvBatch, kDecodeBatch, kQuantBatch, kDecodeNormBatch, kTl2Batch, kAttnDecode, kLaunches };
+// the last two the argument struct), does not hold whole ones of that launch's.
+enum { kGemvBatch, kDecodeBatch, kQuantBatch, kDecodeNormBatch, kTl2Batch, kAttnDecode, kAttn8Decode, kLaunches };
 
 PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
@@ -302,7 +302,7 @@ PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* workspace = PyLong_AsVoidPtr(args[3]);
     if (PyErr_Occurred()) return nullptr;
     constexpr size_t kSizes[kLaunches] = {sizeof(bl_gemv_item), sizeof(bl_decode_item), sizeof(bl_quant_item),
-                                          sizeof(bl_decode_norm_item), sizeof(bl_gemv_item), sizeof(bl_attn_args)};
+                                          sizeof(bl_decode_norm_item), sizeof(bl_gemv_item), sizeof(bl_attn_args), sizeof(bl_attn8_args)};
     if (which < 0 || which >= kLaunches) Py_RETURN_NONE;
     Memory items(args[1], kSizes[which]);
     if (!items.ok || items.view.len % kSizes[which] != 0 || items.view.len / kSizes[which] > INT32_MAX) Py_RETURN_NONE;
@@ -318,6 +318,7 @@ PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             case kDecodeNormBatch: status = bl_decode_norm_batch(items.as<const bl_decode_norm_item>(), n, workspace, stream); break;
             case kTl2Batch: status = bl_tl2_gemv_batch(items.as<const bl_gemv_item>(), n, workspace, stream); break;
             case kAttnDecode: status = bl_attn_decode(items.as<const bl_attn_args>(), stream); break;
+            case kAttn8Decode: status = bl_attn8_decode(items.as<const bl_attn8_args>(), stream); break;
         }
     }
     return PyLong_FromLong(status);

@@ -291,6 +291,13 @@ hipError_t launch_pos_advance(int32_t* pos, hipStream_t s);
 bool attn_prompt_takes(int n_heads, int head_dim);
 hipError_t launch_attn_prompt(const ::bl_attn_prefill_args& a, hipStream_t s);   // keys and values in the cache already
 hipError_t launch_attn_prefill(const ::bl_attn_prefill_args& a, hipStream_t s);
+// The 8-bit cache (bl_kv8.hip) and the attention over it (bl_attn8.hip).  clear: words that the write's launch sets to zero.
+hipError_t launch_kv8_write(const ::bl_kv8_write_args& a, uint32_t* clear, int64_t clear_count, hipStream_t s);
+hipError_t launch_kv8_read(const ::bl_kv8_read_args& a, hipStream_t s);
+int64_t attn8_scratch_bytes(int n_heads, int group, int head_dim, int max_pos, int sequences, int prefix_len);
+hipError_t launch_attn8_decode(const ::bl_attn8_args& a, hipStream_t s);
+int64_t attn8_prefill_scratch_bytes(int n_heads, int group, int head_dim, int pos0, int M);
+hipError_t launch_attn8_prefill(const ::bl_attn8_prefill_args& a, hipStream_t s);
 
 // The calling thread's most recent product launch: kernel template instance and grid, for tools that label what they
 // time (bl_last_kernel).  Only the pieces are stored at launch time; the text is formatted on request.

@@ -126,6 +126,97 @@ class Attention:
         return self.out
 
 
+class KvCache8:
+    """The 8-bit key/value caches of one layer (bl_kv8_cache): per position and key head head_dim int8 codes and an fp32 scale, for `sequences`
+    sequences of up to max_pos positions.  Layout of the codes: include/bitlinear_decoder.h."""
+
+    def __init__(self, n_heads: int, head_dim: int, max_pos: int, device, sequences: int = 1):
+        bytes_ = B.bl_kv8_code_bytes(n_heads, head_dim, max_pos)
+        if bytes_ == 0 or sequences < 1:
+            raise B.BitLinearError(B.BL_ERR_SHAPE, "KvCache8")
+        self.n_heads, self.head_dim, self.max_pos, self.sequences = n_heads, head_dim, max_pos, sequences
+        self.hidden = n_heads * head_dim
+        self.k_codes, self.v_codes = (torch.zeros((sequences, n_heads, bytes_ // n_heads), dtype=torch.int8, device=device) for _ in range(2))
+        scales = (sequences, n_heads, B.bl_kv8_scale_count(n_heads, max_pos) // n_heads)
+        self.k_scale, self.v_scale = (torch.zeros(scales, dtype=torch.float32, device=device) for _ in range(2))
+        self.args = B.Kv8Cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), n_heads,
+                               head_dim, max_pos, sequences)
+
+    def _here(self, *tensors):
+        """The launch goes to the current device's stream: everything has to be there."""
+        dev = self.k_codes.device
+        assert dev.type == "cuda" and dev.index == torch.cuda.current_device(), "the cache is not on the current device"
+        assert all(t is None or t.device == dev for t in tensors), "tensors and cache on different devices"
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, table: Optional[torch.Tensor] = None, sequence: int = 0):
+        """Rows k, v ([M, n_heads * head_dim] fp32 or bf16; rows may lie apart) into positions pos0 .. pos0 + M - 1.  table: the
+        rotary table by which the keys are rotated first (position p by its row p); None: they are rotated already."""
+        self._here(k, v, table)
+        M = int(k.shape[0])
+        assert k.dim() == 2 and k.shape == v.shape == (M, self.hidden) and k.dtype == v.dtype
+        # (a single row's stride says nothing: one of any tensor's rows may be passed)
+        ld = max(int(k.stride(0)), self.hidden) if M > 1 else self.hidden
+        assert k.stride(1) == 1 and v.stride(1) == 1 and (M <= 1 or k.stride(0) == v.stride(0) >= self.hidden)
+        assert table is None or (table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (self.head_dim // 2, 2) and
+                                 table.shape[0] >= pos0 + M)
+        B.bl_kv8_write(self.args, k.data_ptr(), v.data_ptr(), table.data_ptr() if table is not None else 0, ld, ops._dtype_code(k), sequence, pos0, M,
+                       _stream())
+
+    def read(self, pos0: int, M: int, dtype: torch.dtype = torch.float32, sequence: int = 0):
+        """(keys, values) that positions pos0 .. pos0 + M - 1 stand for, [M, n_heads * head_dim]; keys as stored, rotated."""
+        self._here()
+        k, v = (torch.empty((max(M, 0), self.hidden), dtype=dtype, device=self.k_codes.device) for _ in range(2))
+        B.bl_kv8_read(self.args, k.data_ptr(), v.data_ptr(), self.hidden, ops._dtype_code(k), sequence, pos0, M, _stream())
+        return k, v
+
+
+class Attention8:
+    """A prepared bl_attn8_decode call: one token of each of the cache's sequences, at the positions in pos ([sequences] int32 on the device), over
+    rows 0 .. prefix_len - 1 of a shared cache (prefix) and the sequence's own rows behind them.  q_lin [sequences, n_heads * head_dim]; k_lin
+    and v_lin [sequences, cache.n_heads * head_dim]: the cache's key heads are shared by n_heads / cache.n_heads query heads each.  A
+    sequence with a position outside prefix_len .. prefix_len + cache.max_pos - 1 is left out: its cache and its row of out stay as they are."""
+
+    def __init__(self, n_heads: int, cache: KvCache8, q_lin, k_lin, v_lin, pos: torch.Tensor, table: torch.Tensor,
+                 prefix: Optional[KvCache8] = None, prefix_len: int = 0, out: Optional[torch.Tensor] = None):
+        dev, d, n = q_lin.device, cache.head_dim, cache.sequences
+        cache._here(q_lin, k_lin, v_lin, pos, table, out, prefix.k_codes if prefix is not None else None)
+        self.n_heads, self.cache, self.prefix, self.prefix_len = n_heads, cache, prefix, prefix_len
+        self.out = out if out is not None else torch.empty((n, n_heads * d), dtype=torch.float32, device=dev)
+        for t, width in ((q_lin, n_heads * d), (k_lin, cache.hidden), (v_lin, cache.hidden), (self.out, n_heads * d)):
+            assert t.dtype == torch.float32 and t.numel() == n * width and t.is_contiguous()
+        assert pos.dtype == torch.int32 and pos.numel() == n and pos.is_contiguous()
+        assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (d // 2, 2) and table.shape[0] >= prefix_len + cache.max_pos
+        assert prefix_len == 0 or prefix is not None
+        bytes_ = B.bl_attn8_scratch_bytes(n_heads, cache.n_heads, d, cache.max_pos, n, prefix_len)
+        if bytes_ == 0:
+            raise B.BitLinearError(B.BL_ERR_SHAPE, "Attention8")
+        self.scratch = torch.zeros(bytes_, dtype=torch.uint8, device=dev)
+        self._keep = (q_lin, k_lin, v_lin, pos, table)
+        self.args = B.make_attn8_args(q_lin.data_ptr(), k_lin.data_ptr(), v_lin.data_ptr(), pos.data_ptr(), table.data_ptr(), self.out.data_ptr(),
+                                      self.scratch.data_ptr(), cache.args, n_heads, prefix.args if prefix_len else None, prefix_len)
+
+    def launch(self):
+        B.launch(B.LAUNCH_ATTN8_DECODE, self.args, 1)
+        return self.out
+
+
+def attn_prefill8(q_lin: torch.Tensor, k_lin: torch.Tensor, v_lin: torch.Tensor, cache: KvCache8, table: torch.Tensor, pos0: int,
+                  sequence: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bl_attn8_prefill: M consecutive tokens of one sequence at positions pos0 .. -- their rows into the cache, then token m's attention over
+    rows 0 .. pos0 + m.  q_lin [M, n_heads * head_dim], k_lin, v_lin [M, cache.n_heads * head_dim] fp32; returns [M, n_heads * head_dim]."""
+    cache._here(q_lin, k_lin, v_lin, table, out)
+    M, d = int(q_lin.shape[0]), cache.head_dim
+    n_heads = int(q_lin.shape[1]) // d
+    out = torch.empty_like(q_lin) if out is None else out
+    for t, width in ((q_lin, n_heads * d), (k_lin, cache.hidden), (v_lin, cache.hidden), (out, n_heads * d)):
+        assert t.dtype == torch.float32 and t.shape == (M, width) and t.is_contiguous()
+    assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (d // 2, 2) and table.shape[0] >= pos0 + M
+    scratch = torch.empty(B.bl_attn8_prefill_scratch_bytes(n_heads, cache.n_heads, d, pos0, M) or 16, dtype=torch.uint8, device=q_lin.device)
+    B.bl_attn8_prefill(q_lin.data_ptr(), k_lin.data_ptr(), v_lin.data_ptr(), table.data_ptr(), out.data_ptr(), scratch.data_ptr(), cache.args,
+                       n_heads, sequence, pos0, M, _stream())
+    return out
+
+
 class NormDecodeGroup:
     """A prepared bl_decode_norm_batch launch: RMSNorm (with an optional residual add) folded into the quantizer of
     the products that consume the normalised row.  weights share x / delta / gamma; h_out receives x + delta.

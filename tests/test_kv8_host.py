@@ -1,0 +1,147 @@
+"""The 8-bit cache without a GPU: refusals, sizes, structures as the header has them, the layout's arithmetic and the plan of the launches."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2410_16144_amd import binding as B
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 0x10000   # an aligned address that nobody reads: validation comes first
+
+
+def _st(f, *a):
+    with pytest.raises(B.BitLinearError) as e:
+        f(*a)
+    return e.value.status
+
+
+def _cache(**kw):
+    f = dict(k_codes_dev=P, v_codes_dev=P, k_scale_dev=P, v_scale_dev=P, n_heads=4, head_dim=64, max_pos=100, sequences=2)
+    return B.Kv8Cache(**dict(f, **kw))
+
+
+def test_structures_as_the_header_has_them(tmp_path):
+    names = {"bl_kv8_cache": B.Kv8Cache, "bl_kv8_write_args": B.Kv8WriteArgs, "bl_kv8_read_args": B.Kv8ReadArgs, "bl_attn8_args": B.Attn8Args,
+             "bl_attn8_prefill_args": B.Attn8PrefillArgs}
+    lines = "".join('printf("%%zu", sizeof(%s));' % n + "".join('printf(" %%zu", offsetof(%s, %s));' % (n, f[0]) for f in c._fields_) + 'printf("\\n");'
+                    for n, c in names.items())
+    src = tmp_path / "sizes.c"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "bitlinear_decoder.h"\nint main(void) {' + lines + "return 0;}")
+    exe = str(tmp_path / "sizes")
+    subprocess.check_call(["gcc", "-std=c11", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", exe])
+    for line, (n, c) in zip(subprocess.check_output([exe], text=True).splitlines(), names.items()):
+        assert [int(x) for x in line.split()] == [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_], n
+
+
+def test_sizes_of_the_buffers():
+    assert B.bl_kv8_code_bytes(32, 128, 8192) == 32 * 128 * 8192 and B.bl_kv8_scale_count(32, 8192) == 32 * 8192
+    assert B.bl_kv8_code_bytes(3, 100, 65) == 3 * 112 * 128 and B.bl_kv8_scale_count(3, 65) == 3 * 128
+    assert B.bl_kv8_code_bytes(1, 4, 1) == 16 * 64
+    for bad in ((0, 64, 10), (4, 62, 10), (4, 260, 10), (4, 64, 0), (65536, 64, 10), (4, 64, 64 * 65535 + 1)):
+        assert B.bl_kv8_code_bytes(*bad) == 0
+    assert B.bl_kv8_scale_count(0, 10) == 0 and B.bl_kv8_scale_count(1, 0) == 0
+    assert B.bl_kv8_code_bytes(65535, 256, 64 * 65535) == 65535 * 256 * 64 * 65535    # beyond 32 bits
+
+
+def test_refusals_of_write_and_read():
+    def write(cache=None, **kw):
+        a = dict(k=P, v=P, table=P, ld=256, dt=B.BL_F32, sequence=0, pos0=10, M=5)
+        a.update(kw)
+        return _st(B.bl_kv8_write, cache or _cache(), *a.values())
+
+    def read(cache=None, **kw):
+        a = dict(k=P, v=P, ld=256, dt=B.BL_F32, sequence=0, pos0=10, M=5)
+        a.update(kw)
+        return _st(B.bl_kv8_read, cache or _cache(), *a.values())
+    for f in (write, read):
+        assert f(_cache(k_codes_dev=None)) == f(_cache(v_codes_dev=None)) == f(_cache(k_scale_dev=None)) == f(_cache(v_scale_dev=None)) == B.BL_ERR_NULL
+        for kw in (dict(n_heads=0), dict(head_dim=62), dict(head_dim=0), dict(max_pos=0), dict(sequences=0), dict(n_heads=5)):
+            assert f(_cache(**kw)) == B.BL_ERR_SHAPE, kw
+        for kw in (dict(sequence=2), dict(sequence=-1), dict(pos0=-1), dict(pos0=96), dict(M=0), dict(M=-3), dict(M=91), dict(ld=255), dict(pos0=2147483647)):
+            assert f(**kw) == B.BL_ERR_SHAPE, kw
+        assert f(dt=2) == B.BL_ERR_DTYPE
+        assert f(_cache(k_codes_dev=P + 8)) == f(_cache(v_codes_dev=P + 4)) == f(_cache(k_scale_dev=P + 4)) == f(_cache(v_scale_dev=P + 8)) == B.BL_ERR_ALIGN
+        assert f(k=P + 2) == f(v=P + 2) == f(k=P + 1, dt=B.BL_BF16) == B.BL_ERR_ALIGN
+    assert write(k=0) == write(v=0) == B.BL_ERR_NULL and read(k=0, v=0) == B.BL_ERR_NULL
+    assert write(table=P + 4) == B.BL_ERR_ALIGN
+    assert _st(B.bl_kv8_write, None, P, P, P, 256, 0, 0, 0, 1) == _st(B.bl_kv8_read, None, P, P, 256, 0, 0, 0, 1) == B.BL_ERR_NULL
+
+
+def test_refusals_of_the_token_attention():
+    def call(cache=None, n_q=8, prefix=None, prefix_len=0, **kw):
+        a = dict(q=P, k=P, v=P, pos=P, table=P, out=P, scratch=P)
+        a.update(kw)
+        return _st(B.bl_attn8_decode, B.make_attn8_args(*a.values(), cache or _cache(), n_q, prefix, prefix_len))
+    for name in ("q", "k", "v", "pos", "table", "out", "scratch"):
+        assert call(**{name: 0}) == B.BL_ERR_NULL
+    assert call(_cache(k_codes_dev=None)) == B.BL_ERR_NULL and call(prefix_len=3) == B.BL_ERR_NULL      # a prefix without buffers
+    for n_q in (0, -4, 6, 4 * 65):
+        assert call(n_q=n_q) == B.BL_ERR_SHAPE
+    for kw in (dict(head_dim=6), dict(sequences=0), dict(sequences=B.BL_ATTN8_MAX_BATCH + 1), dict(max_pos=-1)):
+        assert call(_cache(**kw)) == B.BL_ERR_SHAPE
+    assert call(prefix_len=-1) == B.BL_ERR_SHAPE and call(prefix=_cache(), prefix_len=101) == B.BL_ERR_SHAPE
+    assert call(prefix=_cache(n_heads=8), prefix_len=5) == call(prefix=_cache(head_dim=60), prefix_len=5) == B.BL_ERR_SHAPE
+    for name, off in (("q", 2), ("k", 2), ("v", 1), ("pos", 2), ("table", 4), ("out", 4), ("scratch", 8)):
+        assert call(**{name: P + off}) == B.BL_ERR_ALIGN
+    assert call(prefix=_cache(v_scale_dev=P + 4), prefix_len=5) == B.BL_ERR_ALIGN
+
+
+def test_refusals_of_the_prompt_attention():
+    def call(cache=None, n_q=8, sequence=0, pos0=10, M=20, **kw):
+        a = dict(q=P, k=P, v=P, table=P, out=P, scratch=P)
+        a.update(kw)
+        return _st(B.bl_attn8_prefill, *a.values(), cache or _cache(), n_q, sequence, pos0, M)
+    for name in ("q", "k", "v", "table", "out", "scratch"):
+        assert call(**{name: 0}) == B.BL_ERR_NULL
+    assert call(_cache(v_codes_dev=None)) == B.BL_ERR_NULL
+    for kw in (dict(n_q=7), dict(n_q=0), dict(n_q=260), dict(sequence=2), dict(sequence=-1), dict(pos0=-1), dict(pos0=81), dict(M=0), dict(M=65536)):
+        assert call(**kw) == B.BL_ERR_SHAPE, kw
+    for name, off in (("q", 2), ("k", 2), ("v", 2), ("table", 4), ("out", 4), ("scratch", 8)):
+        assert call(**{name: P + off}) == B.BL_ERR_ALIGN
+
+
+def test_scratch_sizes():
+    assert B.bl_attn8_scratch_bytes(32, 32, 128, 64, 1, 0) == 32 * 32 * 4 + 32 * 1 * 65 * 8          # one workgroup per head
+    for bad in ((31, 32, 128, 64, 1, 0), (32, 32, 130, 64, 1, 0), (32, 32, 128, 0, 1, 0), (32, 32, 128, 64, 0, 0), (32, 32, 128, 64, 1, -1)):
+        assert B.bl_attn8_scratch_bytes(*bad) == 0
+    assert B.bl_attn8_prefill_scratch_bytes(8, 4, 64, 0, 0) == B.bl_attn8_prefill_scratch_bytes(8, 3, 64, 0, 5) == 0
+    assert B.bl_attn8_prefill_scratch_bytes(8, 4, 64, 0, 5) > 0
+
+
+def _program(tmp_path, name, text):
+    src = tmp_path / (name + ".cpp")
+    src.write_text(text)
+    exe = str(tmp_path / name)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2410_16144_amd", "csrc"), str(src), "-o", exe])
+    return subprocess.run([exe]).returncode
+
+
+def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
+    """For shapes over the whole range: at most 64 workgroups share a row's walk, every row is in a block, the walk of the last position is
+    in some workgroup, launches that can have the compute units busy twice do, and none is much larger unless every part is one workgroup."""
+    assert _program(tmp_path, "plan", """
+        #include <initializer_list>
+        #include "bl_attn8_plan.hpp"
+        int main() {
+            const int lens[] = {0, 1, 64, 255, 256, 257, 1000, 8001, 65536, 100003, 4194240};
+            for (int heads : {1, 2, 7, 8, 32, 40, 64, 300})
+                for (int group : {1, 2, 4, 5, 8, 16, 21, 64})
+                    for (int tokens : {1, 2, 3, 8, 37, 64, 1024})
+                        for (int shared : lens)
+                            for (int own : lens) {
+                                if (!shared && !own) continue;
+                                const bl::Rows8Plan p = bl::rows8_plan(heads, group, tokens, shared, own);
+                                if (p.block != 4 && p.block != 8 && p.block != 16) return 1;
+                                if ((shared > 0) != (p.shared_splits > 0) || (own > 0) != (p.own_splits > 0)) return 2;
+                                if (p.shared_splits > 64 || p.own_splits > 64) return 3;
+                                if (shared && (int64_t)p.shared_blocks * p.block < (int64_t)tokens * group) return 4;
+                                if (own && p.own_blocks * p.block < group) return 5;
+                                if (p.shared_splits > bl::sets_of(shared) || p.own_splits > bl::sets_of(own)) return 6;
+                                if (shared && p.shared_wgs < (int64_t)heads * p.shared_splits * p.shared_blocks) return 7;
+                                if (p.shared_wgs % 8 || p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 8;
+                                if (p.slots() > 2 * bl::kRows8MaxSplits) return 9;
+                            }
+            return 0;
+        }""") == 0
