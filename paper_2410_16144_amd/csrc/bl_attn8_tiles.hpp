@@ -1,0 +1,335 @@
+// The tiles form of the attention over 8-bit caches: 32 rows (token, query head) that read one key head, against 32 positions at a time.
+//
+// A workgroup's four waves share out the 32-position halves of chunks and merge their running maxima, sums and outputs at the end; a wave
+// brings its own operands and waits for nobody.  Every operand comes from memory as it lies there (bl_kv8.hpp), 16 bytes per lane: no LDS,
+// no transposition.
+//
+// Scores are formed transposed, S^T = K Q^T, by v_mfma_i32_32x32x32_i8 on the codes, with the queries as three signed bytes each (24-bit
+// fixed point relative to a row's largest value, as in the rows form): the lowest byte's sums are rounded to units of the second's and go on
+// as its accumulators (half a unit in sums of typically 2^22 of them), the third's are 256 of those units -- one integer, one conversion.  A
+// lane (query l % 32, half g) then has 16 weights of one query, of positions 16 g .. 16 g + 15 in order: the rows of the K operand are
+// taken from memory so that result register r is position 16 g + r, whose values are byte r of the 16 bytes that the lane with the
+// same g loads for a dim.  So O^T += V^T P^T has its operands in place: 32x32x16 f16 products, codes converted (exactly) in registers, a
+// weight w = p s^v as the sum of two f16 numbers (22 bits), scaled by a power of two over the largest s^v so far, so that moving it is
+// exact.  fp32 accumulation throughout.
+#pragma once
+#include "bl_attn8.hpp"
+
+namespace bl {
+
+constexpr int kTiles8Keys = 32;
+static_assert(kTiles8Set == kAttn8Waves * kTiles8Keys, "a half chunk per wave");
+// A row's reference score moves when a score exceeds it by 2^8: nearly every half has a new maximum for one of 32 queries (2048 tokens: all but
+// a few), and the 64 products that rescale the outputs are a sixth of a half's instructions.  Weights are then up to 2^8 and, scaled by 2^7,
+// 2^15: f16 numbers whose second part is a normal number down to 2^-2.
+constexpr float kTiles8Move = 8.0f;
+constexpr int kTiles8Scale = 7;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ i32x16 tiles8_mfma(const v4i& a, const v4i& b, const i32x16& c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 tiles8_mfma16(const u32x4& a, const u32x4& b, const f32x16& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Four codes as f16: 1024 + (code + 128) by its bits, less 1152 (both exact).
+__device__ __forceinline__ void tiles8_widen(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+    const uint32_t u = codes ^ 0x80808080u;
+    const f16x2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off);
+    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off);
+}
+
+// D32: head size in 32s (rounded up).
+template <int D32>
+struct Tiles8Lds {
+    static constexpr int kDims = 32 * D32;
+    static constexpr int kQPitch = 3 * kDims + 16;                    // bytes per row of queries: rows spread over the banks
+    static constexpr int kQuery = 32 * kQPitch;
+    static constexpr int kOPitch = kDims + 4;                         // floats per row of outputs
+    static constexpr int kMeet = kAttn8Waves * 32 * kOPitch * 4;
+    static constexpr int kMost = 2 * kAttn8MaxSplits;
+    static constexpr int kMerge = 32 * kMost * 8 + kAttn8Threads * 8;
+    static constexpr int kBytes = kQuery > kMeet ? (kQuery > kMerge ? kQuery : kMerge) : kMeet > kMerge ? kMeet : kMerge;
+};
+
+struct Tiles8Shared {
+    float  unit[32];
+    float  scale[kAttn8Waves][2 * kTiles8Keys] __attribute__((aligned(16)));   // a half's key scales, value scales
+    float2 ml[kAttn8Waves][32];                                        // the waves' maxima and sums
+};
+
+template <int D32>
+__device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk& walk_of, uint8_t* lds, Tiles8Shared& shared, Attn8Rows& rows_of) {
+    using L = Tiles8Lds<D32>;
+    const int tid = threadIdx.x, lane = tid & 63, set = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, g = lane >> 5;
+    const int d = p.head_dim, half = d >> 1, size = p.size;
+    const int head = walk_of.head, row0 = walk_of.row0, rows = walk_of.rows, keys = walk_of.keys, lowest = walk_of.lowest, split = walk_of.split,
+              splits = walk_of.splits;
+    const int halves = (keys + kTiles8Keys - 1) / kTiles8Keys;
+    const auto half_of = [&](int i) { return kAttn8Waves * (split + splits * i) + set; };
+    const int mine = walk_of.mine - (half_of(walk_of.mine - 1) >= halves ? 1 : 0);   // halves of this wave
+
+    // ---- requests
+    const float* scales = (g ? walk_of.c.v_scale : walk_of.c.k_scale) + l32;
+    // K operand: lane l32 = 8 i + 4 g' + c has position 16 g' + 4 i + c of the half, row 16 c + 8 T + 4 g' + i of the chunk
+    const int k_row = 16 * (l32 & 3) + (l32 & 4) + (l32 >> 3);
+    uint32_t k_at[D32], v_at[D32];
+#pragma unroll
+    for (int s = 0; s < D32; ++s) {
+        const int left = size - 64 * (s >> 1), width = min(left, 64);   // (a piece beyond the head size: any other; its queries are zero)
+        const int piece = min(2 * (s & 1) + g, (width >> 4) - 1);
+        k_at[s] = (uint32_t)((s >> 1) * 4096 + k_row * width + 16 * piece);
+        v_at[s] = (uint32_t)(min(32 * s + l32, size - 1) * 64 + 16 * g);
+    }
+    v4i k[D32], v[D32];
+    float scale;
+    const auto request_keys = [&](int i) {
+        const int h = half_of(i);
+        const int8_t* base = walk_of.c.k + (int64_t)(h >> 1) * (kKv8Chunk * size);
+#pragma unroll
+        for (int s = 0; s < D32; ++s) {
+            const int width = min(size - 64 * (s >> 1), 64);
+            k[s] = *reinterpret_cast<const v4i*>(base + 8 * (h & 1) * width + k_at[s]);
+        }
+        scale = scales[h * kTiles8Keys];
+    };
+    const auto request_values = [&](int i) {
+        const int h = half_of(i);
+        const int8_t* base = walk_of.c.v + (int64_t)(h >> 1) * (kKv8Chunk * size) + 32 * (h & 1);
+#pragma unroll
+        for (int t = 0; t < D32; ++t) v[t] = *reinterpret_cast<const v4i*>(base + v_at[t]);
+    };
+    if (mine > 0) {
+        request_keys(0);
+        request_values(0);
+    }
+
+    // ---- the rows' queries: rotated, three bytes per element, through LDS.  Eight lanes share a row, two neighbouring elements and their
+    // partners in the other half of the head at a time.
+    {
+        constexpr int kTurns = D32;                       // 16 of at most 16 D32 elements of a half each
+        typedef float f32x2_u __attribute__((ext_vector_type(2), aligned(4)));
+        typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(8)));
+        const int r = tid >> 3, t8 = tid & 7, row = row0 + min(r, rows - 1);   // (rows beyond the last repeat it)
+        const int pos = attn8_position(p, divided(row, p.by_group));
+        const bool there = attn8_takes_part(p, pos);
+        const float* src = p.q + attn8_row_at(p, head, row);
+        const float* angles = reinterpret_cast<const float*>(p.rope + (int64_t)(there ? pos : 0) * half);
+        f32x2 lo[kTurns], hi[kTurns];
+        f32x4 cs[kTurns];
+#pragma unroll
+        for (int m = 0; m < kTurns; ++m) {
+            const int i = 2 * (t8 + 8 * m);
+            lo[m] = hi[m] = f32x2{0.0f, 0.0f};
+            cs[m] = f32x4{1.0f, 0.0f, 1.0f, 0.0f};
+            if (there && i < half) {
+                lo[m] = *reinterpret_cast<const f32x2_u*>(src + i);
+                hi[m] = *reinterpret_cast<const f32x2_u*>(src + half + i);
+                cs[m] = *reinterpret_cast<const f32x4_u*>(angles + 2 * i);
+            }
+        }
+        float amax = 0.0f;
+#pragma unroll
+        for (int m = 0; m < kTurns; ++m)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float a = lo[m][x], b = hi[m][x], c = cs[m][2 * x], s = cs[m][2 * x + 1];
+                lo[m][x] = a * c - b * s;
+                hi[m][x] = a * s + b * c;
+                amax = fmaxf(amax, fmaxf(fabsf(lo[m][x]), fabsf(hi[m][x])));
+            }
+#pragma unroll
+        for (int x = 1; x < 8; x <<= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
+        const float inv = query_inv(amax);
+        if (t8 == 0) shared.unit[r] = amax * (1.0f / kQueryFull) * 256.0f * p.unit;
+        uint8_t* dst = lds + r * L::kQPitch;
+        const auto put = [&](int e, const f32x2& x) {      // byte by byte, both elements' side by side
+            const uint32_t a = query_bytes(x[0], inv), b = query_bytes(x[1], inv);
+            *reinterpret_cast<uint16_t*>(dst + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0400u);
+            *reinterpret_cast<uint16_t*>(dst + L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0501u);
+            *reinterpret_cast<uint16_t*>(dst + 2 * L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0602u);
+        };
+#pragma unroll
+        for (int m = 0; m < kTurns; ++m) {
+            const int i = 2 * (t8 + 8 * m);
+            if (i < half) {
+                put(i, lo[m]);
+                put(half + i, hi[m]);
+            }
+        }
+        for (int e = d + 2 * t8; e < L::kDims; e += 16) put(e, f32x2{0.0f, 0.0f});
+    }
+    if (tid < rows) attn8_count(p, rows_of, tid, row0 + tid, attn8_walked(p, walk_of));
+    __syncthreads();
+    v4i q[3][D32];   // B operands: column l32, dims 32 s + 16 g ...
+#pragma unroll
+    for (int b = 0; b < 3; ++b)
+#pragma unroll
+        for (int s = 0; s < D32; ++s) q[b][s] = *reinterpret_cast<const v4i*>(lds + l32 * L::kQPitch + b * L::kDims + 32 * s + 16 * g);
+    const float unit = shared.unit[l32];
+    const int limit = p.prompt ? min(keys, p.pos0 + divided(row0 + l32, p.by_group) + 1) : keys;   // positions that this lane's query sees
+    float* scales_of = shared.scale[set];
+
+    f32x16 o[D32];
+#pragma unroll
+    for (int t = 0; t < D32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+    float run_m = -INFINITY, run_l = 0.0f;      // run_l: over this lane half's positions only
+    int run_e = -100;                           // exponent of the largest value scale so far, at least (uniform)
+
+    const auto walk = [&](int i, auto which) {
+        constexpr bool kLast = decltype(which)::value;
+        const int first = half_of(i) * kTiles8Keys;
+        // Only a wave's last half can be one that some query does not see all of: such halves are at most two (32 rows), one after
+        // another, of different waves.
+        const bool masked = kLast && first + kTiles8Keys > lowest;   // uniform
+        // the half's scales through LDS: lanes 0-31 brought the keys', lanes 32-63 the values'
+        float own_scale = scale;
+        if (masked && first + l32 >= keys) own_scale = 0.0f;   // what lies behind the last row may be anything
+        const float v_max = wave_max(g ? own_scale : 0.0f);
+        const int e_new = v_max > 0.0f ? max(run_e, __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max))) : run_e;
+        scales_of[lane] = g ? ldexpf(own_scale, kTiles8Scale - e_new) : own_scale;
+        __builtin_amdgcn_wave_barrier();   // (a wave's LDS operations are performed in order)
+        // S^T: 32 positions x 32 queries, in units of 256 of the queries'
+        i32x16 low, high;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) low[r] = 64;   // (an operand that is a constant: a quarter of a unit below the middle)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) high[r] = 0;
+#pragma unroll
+        for (int s = 0; s < D32; ++s) low = tiles8_mfma(k[s], q[0][s], low);
+#pragma unroll
+        for (int s = 0; s < D32; ++s) high = tiles8_mfma(k[s], q[2][s], high);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) low[r] >>= 8;
+#pragma unroll
+        for (int s = 0; s < D32; ++s) low = tiles8_mfma(k[s], q[1][s], low);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kLast) request_keys(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        float x[16];
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 ks = *reinterpret_cast<const f32x4*>(&scales_of[16 * g + 4 * r4]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[4 * r4 + c] = (float)((high[4 * r4 + c] << 8) + low[4 * r4 + c]) * ks[c];
+        }
+        if (masked) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (first + 16 * g + r >= limit) x[r] = -INFINITY;
+        }
+        float mx = x[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+        mx = over_blocks<32>(mx, MaxOp());
+        // (a query whose values are all zero has unit 0; it must not meet an infinity)
+        const float top = kLast && mx == -INFINITY ? mx : mx * unit;
+        if (__any(top > run_m + kTiles8Move) || e_new != run_e) {
+            const float m_new = fmaxf(run_m, top);
+            const float f = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(run_m - m_new);
+            const float fo = ldexpf(f, run_e - e_new);
+#pragma unroll
+            for (int t = 0; t < D32; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][r] *= fo;
+            run_l *= f;
+            run_m = m_new;
+            run_e = e_new;
+        }
+        const float base = kLast && run_m == -INFINITY ? 0.0f : run_m;
+        u32x4 w_hi[2], w_lo[2];
+        float sum = 0.0f;
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const f32x4 vs = *reinterpret_cast<const f32x4*>(&scales_of[kTiles8Keys + 16 * g + 4 * r4]);
+            float w[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float at = x[4 * r4 + c];
+                const float pj = __builtin_amdgcn_exp2f(kLast && at == -INFINITY ? at : fmaf(at, unit, -base));
+                sum += pj;
+                w[c] = pj * vs[c];
+            }
+#pragma unroll
+            for (int c = 0; c < 4; c += 2) {
+                const f16x2 hi = __builtin_convertvector((f32x2{w[c], w[c + 1]}), f16x2);
+                const uint32_t both = __builtin_bit_cast(uint32_t, hi);
+                float rest[2];                             // what the first parts leave: w - hi (exact)
+                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rest[0]) : "v"(both), "v"(w[c]));
+                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(rest[1]) : "v"(both), "v"(w[c + 1]));
+                const f16x2 lo = __builtin_convertvector((f32x2{rest[0], rest[1]}), f16x2);
+                w_hi[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = both;
+                w_lo[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, lo);
+            }
+        }
+        run_l += sum;
+#pragma unroll
+        for (int t = 0; t < D32; ++t) {
+            u32x4 a[2];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t lo, hi;
+                tiles8_widen((uint32_t)v[t][w], lo, hi);
+                a[w >> 1][2 * (w & 1)] = lo;
+                a[w >> 1][2 * (w & 1) + 1] = hi;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                o[t] = tiles8_mfma16(a[h], w_lo[h], o[t]);
+                o[t] = tiles8_mfma16(a[h], w_hi[h], o[t]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!kLast) request_values(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int i = 0; i + 1 < mine; ++i) walk(i, std::false_type{});
+    if (mine > 0) walk(mine - 1, std::true_type{});
+
+    // ---- the waves meet: maxima and sums first, then the outputs, each scaled by its own factor
+    run_l = over_blocks<32>(run_l, AddOp());
+    if (g == 0) shared.ml[set][l32] = make_float2(run_m, run_l);
+    __syncthreads();
+    const auto figure = [&](int r) {
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kAttn8Waves; ++w) m = fmaxf(m, shared.ml[w][r].x);
+        const float ref = m == -INFINITY ? 0.0f : m;       // (a prompt's row whose walk ends before this workgroup's halves)
+#pragma unroll
+        for (int w = 0; w < kAttn8Waves; ++w) l += shared.ml[w][r].y * __builtin_amdgcn_exp2f(shared.ml[w][r].x - ref);
+        return make_float2(m, l);
+    };
+    const float m_all = figure(l32).x;
+    const float f = ldexpf(__builtin_amdgcn_exp2f(run_m - (m_all == -INFINITY ? 0.0f : m_all)), run_e - kTiles8Scale);
+    float* meet = reinterpret_cast<float*>(lds);   // (the barrier above: every wave has its queries)
+#pragma unroll
+    for (int t = 0; t < D32; ++t)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+            *reinterpret_cast<f32x4*>(meet + (set * 32 + l32) * L::kOPitch + 32 * t + 8 * r4 + 4 * g) =
+                f32x4{o[t][4 * r4] * f, o[t][4 * r4 + 1] * f, o[t][4 * r4 + 2] * f, o[t][4 * r4 + 3] * f};
+    __syncthreads();
+    attn8_finish<32, L::kMost>(
+        p, rows_of, lds, head, row0, rows, walk_of.slot,
+        [&](int r, int e) {
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kAttn8Waves; ++w) {
+                const float2 a = *reinterpret_cast<const float2*>(meet + (w * 32 + r) * L::kOPitch + e);
+                sum.x += a.x;
+                sum.y += a.y;
+            }
+            return sum;
+        },
+        figure);
+}
+
+}  // namespace bl

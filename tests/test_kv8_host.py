@@ -119,29 +119,52 @@ def _program(tmp_path, name, text):
 
 
 def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
-    """For shapes over the whole range: at most 64 workgroups share a row's walk, every row is in a block, the walk of the last position is
-    in some workgroup, launches that can have the compute units busy twice do, and none is much larger unless every part is one workgroup."""
+    """For shapes over the whole range: at most 64 workgroups share a row's walk, every row is in a block, no workgroup is without positions
+    of the longest walk, and a launch has more workgroups than it aims at only where its parts cannot be larger."""
     assert _program(tmp_path, "plan", """
         #include <initializer_list>
         #include "bl_attn8_plan.hpp"
         int main() {
-            const int lens[] = {0, 1, 64, 255, 256, 257, 1000, 8001, 65536, 100003, 4194240};
+            const int lens[] = {0, 1, 64, 127, 128, 129, 256, 257, 1000, 8001, 65536, 100003, 4194240};
             for (int heads : {1, 2, 7, 8, 32, 40, 64, 300})
                 for (int group : {1, 2, 4, 5, 8, 16, 21, 64})
                     for (int tokens : {1, 2, 3, 8, 37, 64, 1024})
                         for (int shared : lens)
                             for (int own : lens) {
                                 if (!shared && !own) continue;
-                                const bl::Rows8Plan p = bl::rows8_plan(heads, group, tokens, shared, own);
+                                const bl::Attn8Plan p = bl::attn8_plan(heads, group, tokens, shared, own);
+                                const int64_t rows = (int64_t)tokens * group;
                                 if (p.block != 4 && p.block != 8 && p.block != 16) return 1;
+                                if (p.tiles && (p.block != 4 || rows <= 4 || !shared)) return 10;
                                 if ((shared > 0) != (p.shared_splits > 0) || (own > 0) != (p.own_splits > 0)) return 2;
                                 if (p.shared_splits > 64 || p.own_splits > 64) return 3;
-                                if (shared && (int64_t)p.shared_blocks * p.block < (int64_t)tokens * group) return 4;
+                                const int block = p.tiles ? 32 : p.block;
+                                if (shared && ((int64_t)p.shared_blocks * block < rows || (int64_t)(p.shared_blocks - 1) * block >= rows)) return 4;
                                 if (own && p.own_blocks * p.block < group) return 5;
-                                if (p.shared_splits > bl::sets_of(shared) || p.own_splits > bl::sets_of(own)) return 6;
-                                if (shared && p.shared_wgs < (int64_t)heads * p.shared_splits * p.shared_blocks) return 7;
-                                if (p.shared_wgs % 8 || p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 8;
-                                if (p.slots() > 2 * bl::kRows8MaxSplits) return 9;
+                                if (p.shared_splits > bl::sets_of(shared, p.shared_set) || p.own_splits > bl::sets_of(own, bl::kRows8Set)) return 6;
+                                if (p.shared_set != (p.tiles ? 128 : 256)) return 7;
+                                if (p.shared_wgs % 8 || p.shared_wgs < (int64_t)heads * p.shared_splits * p.shared_blocks) return 8;
+                                if (p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 9;
+                                if ((int64_t)heads * p.shared_splits * p.shared_blocks + p.own_wgs > bl::kAttn8Workgroups &&
+                                    (p.shared_splits > 1 || p.own_splits > 1)) return 11;
                             }
+            return 0;
+        }""") == 0
+
+
+def test_division_by_known_numbers(tmp_path):
+    """Every quotient of numbers up to 2^31 - 1 near the multiples of a divisor, for divisors over the whole range."""
+    assert _program(tmp_path, "divide", """
+        #include "bl_attn8_plan.hpp"
+        int main() {
+            for (int64_t d = 1; d < (1ll << 31); d += d < 3000 ? 1 : d / 7 + 1) {
+                const bl::Divider by = bl::divider((int)d);
+                const int64_t most = ((1ll << 31) - 1) / d;
+                for (int64_t q = 0; q <= most; q += 1 + q / 3 + (q > most / 2 ? most / 40 : 0))
+                    for (int64_t n = q * d - 2; n <= q * d + 2; ++n)
+                        if (n >= 0 && n < (1ll << 31) && bl::divided((int)n, by) != n / d) return 1;
+                for (int64_t n = (1ll << 31) - 1; n > (1ll << 31) - 60; --n)
+                    if (bl::divided((int)n, by) != n / d) return 2;
+            }
             return 0;
         }""") == 0
