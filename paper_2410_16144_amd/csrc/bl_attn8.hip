@@ -10,33 +10,50 @@ namespace bl {
 
 namespace {
 
-template <int KB, int NQ>
-__global__ __launch_bounds__(kAttn8Threads) void attn8_rows_kernel(const Attn8Args p) {
+template <int KB, int NQ, int W, bool STREAM>
+__global__ __launch_bounds__(64 * W) void attn8_rows_kernel(const Attn8Args p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ Rows8Shared shared;
     __shared__ Attn8Rows rows;
     Attn8Walk walk;
     const int wg = blockIdx.x;   // uniform, like the walk
     if (!(wg < p.shared_wgs ? attn8_shared_walk(p, wg, 4 * NQ, walk) : attn8_own_walk(p, wg - p.shared_wgs, 4 * NQ, walk))) return;
-    rows8_walk<KB, NQ>(p, walk, lds, shared, rows);
+    rows8_walk<KB, NQ, W, STREAM>(p, walk, lds, shared, rows);
 }
 
-template <int KB, int NQ>
+template <int KB, int NQ, int W, bool STREAM>
 hipError_t launch_form(const Attn8Args& p, int wgs, hipStream_t s) {
-    using L = Rows8Lds<KB, NQ>;
+    using L = Rows8Lds<KB, NQ, W>;
     static_assert(L::kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
     static LdsCeiling ceiling;   // per instantiation, i.e. per kernel
-    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&attn8_rows_kernel<KB, NQ>), L::kBytes);
+    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&attn8_rows_kernel<KB, NQ, W, STREAM>), L::kBytes);
     if (e != hipSuccess) return e;
-    attn8_rows_kernel<KB, NQ><<<dim3((unsigned)wgs), dim3(kAttn8Threads), L::kBytes, s>>>(p);
+    attn8_rows_kernel<KB, NQ, W, STREAM><<<dim3((unsigned)wgs), dim3(64 * W), L::kBytes, s>>>(p);
     return hipGetLastError();
 }
 
 template <int KB>
-hipError_t launch_block(const Attn8Args& p, int block, int wgs, hipStream_t s) {
-    if (block == 4) return launch_form<KB, 1>(p, wgs, s);
-    if (block == 8) return launch_form<KB, 2>(p, wgs, s);
-    return launch_form<KB, 4>(p, wgs, s);
+hipError_t launch_block(const Attn8Args& p, const Attn8Plan& plan, bool stream, int wgs, hipStream_t s) {
+    static_assert(kRows8Waves == 8 && kRows8ManyWaves == 2 && kRows8FewWaves == 4, "waves as planned");
+    if (plan.block == 8) return launch_form<KB, 2, 4, true>(p, wgs, s);
+    if (plan.block == 16) return launch_form<KB, 4, 4, true>(p, wgs, s);
+    if (plan.waves == 8) return stream ? launch_form<KB, 1, 8, true>(p, wgs, s) : launch_form<KB, 1, 8, false>(p, wgs, s);
+    return stream ? launch_form<KB, 1, 2, true>(p, wgs, s) : launch_form<KB, 1, 2, false>(p, wgs, s);
+}
+
+hipError_t launch_rows(const Attn8Args& p, const Attn8Plan& plan, int wgs, hipStream_t s) {
+    // Caches of 32 MiB and more (the dies' L2s together) by streaming loads.  32 heads of 128, ordinary and streaming, us: 500 positions 6.9 and 7.8, 4000
+    // (33 MB) 12.7 and 12.9, 8000 19.2 and 17.6, 30 000 52.2 and 46.7.
+    const int64_t positions = p.shared_wgs > 0 ? (p.prompt ? p.pos0 + p.tokens : p.shared_len) : 0;
+    const bool stream = 2 * (positions + (int64_t)p.tokens * p.max_pos) * p.n_heads * p.size >= 32 << 20;
+    static_assert(BL_ATTN_MAX_HEAD_DIM == 256, "head sizes up to four blocks of 64");
+    switch ((p.head_dim + 63) / 64) {
+        case 1: return launch_block<1>(p, plan, stream, wgs, s);
+        case 2: return launch_block<2>(p, plan, stream, wgs, s);
+        case 3: return launch_block<3>(p, plan, stream, wgs, s);
+        case 4: return launch_block<4>(p, plan, stream, wgs, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_t s) {
@@ -45,7 +62,7 @@ hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_
     p.unit = 1.4426950408889634f / sqrtf((float)p.head_dim);
     p.counters = static_cast<uint32_t*>(scratch);
     p.figures = reinterpret_cast<float2*>(p.counters + attn8_counters(p.n_heads, p.rows));
-    p.shared_set = plan.shared_set;
+    p.shared_set = plan.shared_set; p.own_set = plan.own_set;
     p.shared_splits = plan.shared_splits; p.shared_blocks = plan.shared_blocks;
     p.own_splits = plan.own_splits; p.own_blocks = plan.own_blocks;
     if (plan.shared_wgs + plan.own_wgs > INT32_MAX) return hipErrorInvalidValue;
@@ -56,24 +73,23 @@ hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_
     p.by_shared_units = divider((p.n_heads * p.shared_splits + 7) / 8 * 8);
     const int found = compute_unit_count(), cus = found > 0 ? found : 256;
     p.paired = wgs > cus && wgs <= 2 * cus;   // all resident: a unit's second block is as short as its first one is long
-    if (plan.tiles) return launch_attn8_tiles(p, wgs, s);
-    static_assert(BL_ATTN_MAX_HEAD_DIM == 256, "head sizes up to four blocks of 64");
-    switch ((p.head_dim + 63) / 64) {
-        case 1: return launch_block<1>(p, plan.block, wgs, s);
-        case 2: return launch_block<2>(p, plan.block, wgs, s);
-        case 3: return launch_block<3>(p, plan.block, wgs, s);
-        case 4: return launch_block<4>(p, plan.block, wgs, s);
+    if (!plan.tiles) return launch_rows(p, plan, wgs, s);
+    p.merges = plan.slots() > 1;
+    hipError_t e = launch_attn8_tiles(p, plan.apart ? p.shared_wgs : wgs, s);
+    if (e == hipSuccess && plan.apart) {
+        p.shared_wgs = 0;
+        e = launch_rows(p, plan, (int)plan.own_wgs, s);
     }
-    return hipErrorInvalidValue;
+    return e == hipSuccess && p.merges ? launch_attn8_merge(p, s) : e;
 }
 
 // A prompt's rows: the write clears the counters of the launch behind it.
-Attn8Plan prompt_plan(int n_heads, int group, int pos0, int M) { return attn8_plan(n_heads, group, M, pos0 + M, 0); }
+Attn8Plan prompt_plan(int n_heads, int group, int head_dim, int pos0, int M) { return attn8_plan(n_heads, group, M, pos0 + M, 0, kv8_size(head_dim)); }
 
 }  // namespace
 
 int64_t attn8_scratch_bytes(int n_heads, int group, int head_dim, int max_pos, int sequences, int prefix_len) {
-    return attn8_scratch(attn8_plan(n_heads, group, sequences, prefix_len, max_pos), n_heads, (int64_t)sequences * group, head_dim);
+    return attn8_scratch(attn8_plan(n_heads, group, sequences, prefix_len, max_pos, kv8_size(head_dim)), n_heads, (int64_t)sequences * group, head_dim);
 }
 
 hipError_t launch_attn8_decode(const ::bl_attn8_args& a, hipStream_t s) {
@@ -87,11 +103,11 @@ hipError_t launch_attn8_decode(const ::bl_attn8_args& a, hipStream_t s) {
     p.tokens = a.cache.sequences; p.shared_len = a.prefix_len; p.max_pos = a.cache.max_pos;
     p.own_codes = p.own.head_bytes * p.n_heads;
     p.own_scales = p.own.head_scales * p.n_heads;
-    return launch(p, attn8_plan(p.n_heads, p.group, p.tokens, p.shared_len, p.max_pos), a.scratch_dev, s);
+    return launch(p, attn8_plan(p.n_heads, p.group, p.tokens, p.shared_len, p.max_pos, kv8_size(p.head_dim)), a.scratch_dev, s);
 }
 
 int64_t attn8_prefill_scratch_bytes(int n_heads, int group, int head_dim, int pos0, int M) {
-    return attn8_scratch(prompt_plan(n_heads, group, pos0, M), n_heads, (int64_t)M * group, head_dim);
+    return attn8_scratch(prompt_plan(n_heads, group, head_dim, pos0, M), n_heads, (int64_t)M * group, head_dim);
 }
 
 hipError_t launch_attn8_prefill(const ::bl_attn8_prefill_args& a, hipStream_t s) {
@@ -102,8 +118,8 @@ hipError_t launch_attn8_prefill(const ::bl_attn8_prefill_args& a, hipStream_t s)
     p.shared = kv8_of(a.cache, a.sequence);
     p.n_heads = a.cache.n_heads; p.group = a.n_q_heads / a.cache.n_heads; p.head_dim = a.cache.head_dim;
     p.tokens = a.M; p.prompt = 1; p.pos0 = a.pos0;
-    const Attn8Plan plan = prompt_plan(p.n_heads, p.group, a.pos0, a.M);
-    const int64_t counters = plan.shared_splits > 1 ? attn8_counters(p.n_heads, (int64_t)a.M * p.group) : 0;   // (one workgroup per row needs none)
+    const Attn8Plan plan = prompt_plan(p.n_heads, p.group, p.head_dim, a.pos0, a.M);
+    const int64_t counters = plan.meets() ? attn8_counters(p.n_heads, (int64_t)a.M * p.group) : 0;
     const ::bl_kv8_write_args w{&a.cache, a.k_lin_dev, a.v_lin_dev, a.rope_table_dev, (int64_t)p.n_heads * p.head_dim, BL_F32, a.sequence, a.pos0, a.M};
     const hipError_t e = launch_kv8_write(w, static_cast<uint32_t*>(a.scratch_dev), counters, s);
     return e != hipSuccess ? e : launch(p, plan, a.scratch_dev, s);

@@ -7,8 +7,6 @@
 
 namespace bl {
 
-constexpr int kAttn8Threads = 64 * kAttn8Waves;
-
 struct Attn8Args {
     const float*   q;
     const float*   k_new;
@@ -26,15 +24,17 @@ struct Attn8Args {
     int32_t        shared_len;  // rows of the prefix
     int32_t        max_pos;     // of a sequence's own cache
     int32_t        shared_wgs, shared_splits, shared_blocks, own_splits, own_blocks;
-    int32_t        shared_set;  // positions of the shared part's sets
+    int32_t        shared_set, own_set;   // positions of a workgroup's sets: 1 << so much
     int32_t        prompt;      // the shared walk is a prompt's: token m sees rows 0 .. pos0 + m
     int32_t        pos0;
+    int32_t        merges;      // a launch follows that merges the figures
     int32_t        paired;      // a prompt's blocks in the order last, ..., middle, first, ..., middle instead of last ... first
     float          unit;        // log2(e) / sqrt(head_dim)
     Divider        by_heads, by_group, by_half, by_tokens, by_own_blocks, by_own_splits, by_shared_splits, by_shared_units;   // (units: padded)
 };
 
 hipError_t launch_attn8_tiles(const Attn8Args& p, int wgs, hipStream_t s);   // bl_attn8_tiles.hip
+hipError_t launch_attn8_merge(const Attn8Args& p, hipStream_t s);
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -62,6 +62,8 @@ __device__ __forceinline__ void leave_figure(float2* at, float x, float y) {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), (unsigned long long)__float_as_uint(x) | (unsigned long long)__float_as_uint(y) << 32,
                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+
+__device__ __forceinline__ int attn8_sets(int positions, int set) { return (positions + (1 << set) - 1) >> set; }
 
 // One workgroup's part of a launch.
 struct Attn8Walk {
@@ -97,8 +99,7 @@ __device__ __forceinline__ bool attn8_shared_walk(const Attn8Args& p, int wg, in
     w.keys = p.prompt ? p.pos0 + divided(w.row0 + w.rows - 1, p.by_group) + 1 : p.shared_len;
     w.lowest = p.prompt ? p.pos0 + divided(w.row0, p.by_group) + 1 : w.keys;
     w.sequence = w.pos = -1;
-    static_assert(kRows8Set == 256 && kTiles8Set == 128, "set sizes by shifts");
-    w.sets = p.shared_set == kRows8Set ? (w.keys + 255) >> 8 : (w.keys + 127) >> 7;
+    w.sets = attn8_sets(w.keys, p.shared_set);
     w.mine = divided(w.sets - w.split + w.splits - 1, p.by_shared_splits);
     w.c = p.shared;
     attn8_to_head(p, w);
@@ -120,7 +121,7 @@ __device__ __forceinline__ bool attn8_own_walk(const Attn8Args& p, int wg, int b
     const int at = w.pos - p.shared_len;
     if (at < 0 || at >= p.max_pos) return false;           // a sequence that takes no part
     w.keys = w.lowest = at + 1;
-    w.sets = (w.keys + 255) >> 8;
+    w.sets = attn8_sets(w.keys, p.own_set);
     w.mine = divided(max(w.sets - w.split + w.splits - 1, 0), p.by_own_splits);
     w.c = p.own;
     w.c.k += w.sequence * p.own_codes;
@@ -133,7 +134,7 @@ __device__ __forceinline__ bool attn8_own_walk(const Attn8Args& p, int wg, int b
 
 // Workgroups that walk the shared part of a row whose walk there has so many sets.
 __device__ __forceinline__ int attn8_walked(const Attn8Args& p, const Attn8Walk& w) {
-    return w.sequence < 0 ? min(w.splits, w.sets) : p.shared_len > 0 ? min(p.shared_splits, sets_of(p.shared_len, p.shared_set)) : 0;
+    return w.sequence < 0 ? min(w.splits, w.sets) : p.shared_len > 0 ? min(p.shared_splits, attn8_sets(p.shared_len, p.shared_set)) : 0;
 }
 
 // Of a workgroup's rows: how many workgroups have figures of each.
@@ -151,7 +152,7 @@ __device__ __forceinline__ void attn8_count(const Attn8Args& p, Attn8Rows& s, in
     const bool active = attn8_takes_part(p, pos);
     s.active[tid] = active;
     s.shared_used[tid] = walked;
-    s.target[tid] = walked + (active && !p.prompt ? min(p.own_splits, sets_of(pos - p.shared_len + 1, kRows8Set)) : 0);
+    s.target[tid] = walked + (active && !p.prompt ? min(p.own_splits, attn8_sets(pos - p.shared_len + 1, p.own_set)) : 0);
 }
 
 // The end of every walk.  pair(r, e): the workgroup's weighted values of dims e, e + 1 of its row r; figure(r): their maximum and sum.  A row
@@ -159,14 +160,15 @@ __device__ __forceinline__ void attn8_count(const Attn8Args& p, Attn8Rows& s, in
 // reads all of them and writes the row.  Nobody waits for anybody: figures travel by device-scope stores, performed past the dies' caches;
 // every thread waits until its own have been performed (stores are outstanding vector memory operations until they are acknowledged, and a
 // barrier alone does not wait for them), then the barrier, then the tickets; the reads are device-scope loads.
-// LDS: kRows * kMost pairs for the merge's factors and kAttn8Threads pairs behind them; pair() may read it until the barrier.
-template <int kRows, int kMost, typename Pair, typename Figure>
+// W: waves.  LDS: kRows * kMost pairs for the merge's factors and 64 W pairs behind them; pair() may read it until the barrier.
+// Where a launch of attn8_merge_kernel follows (p.merges), it does the rest: the figures are left, and nobody draws a ticket.
+template <int kRows, int kMost, int W, typename Pair, typename Figure>
 __device__ __forceinline__ void attn8_finish(const Attn8Args& p, Attn8Rows& s, uint8_t* lds, int head, int row0, int rows, int slot, const Pair& pair,
                                              const Figure& figure) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = p.head_dim >> 1, stride = half + 1, slots = p.shared_splits + p.own_splits;
     const auto figures_of = [&](int r) { return p.figures + ((int64_t)head * p.rows + row0 + r) * slots * stride; };
-    for (int i = tid; i < rows * half; i += kAttn8Threads) {
+    for (int i = tid; i < rows * half; i += (64 * W)) {
         const int r = divided(i, p.by_half), e = 2 * (i - r * half);
         const float2 x = pair(r, e);
         if (s.target[r] == 1) {                            // the only workgroup: nothing is left for anybody
@@ -183,6 +185,8 @@ __device__ __forceinline__ void attn8_finish(const Attn8Args& p, Attn8Rows& s, u
             }
         }
     }
+    if constexpr (kMost == 0) return;                      // (tiles: always followed)
+    if (p.merges) return;                                  // uniform
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     uint32_t* counters = p.counters + (int64_t)head * attn8_padded(p.rows) + row0;
@@ -202,78 +206,85 @@ __device__ __forceinline__ void attn8_finish(const Attn8Args& p, Attn8Rows& s, u
     const int listed = s.count;
     if (listed == 0) return;                               // uniform
 
-    // ---- this workgroup is the last of some rows: their figures become the output.  A read is a trip to memory: the first eight weighted values
-    // of every thread are requested together with the maxima and sums.
+    // ---- this workgroup is the last of some rows: their figures become the output.  A read is a trip to memory: a thread has up to 32 of them under way,
+    // the first of them together with the maxima and sums.
     const int shift = 32 - __clz(s.most - 1);              // of a row's entries below (most >= 2)
     float2* factor = reinterpret_cast<float2*>(lds);       // [row of the list][figure]: (maximum, sum), then (factor, -)
     const auto slot_of = [&](int r, int f) { return f < s.shared_used[r] ? f : p.shared_splits + f - s.shared_used[r]; };
     const int pairs = listed * half;                       // of outputs
-    const int teams = max(1, kAttn8Threads / pairs);       // that share a pair's figures
-    const auto read8 = [&](float2 (&a)[8], int r, int e, int f) {
-        float2* src = figures_of(r) + 1 + e;
-        const int last = s.target[r] - 1;
-#pragma unroll
-        for (int h = 0; h < 8; ++h) a[h] = read_figure(src + (int64_t)slot_of(r, min(f + h * teams, last)) * stride);
-    };
+    const int teams = max(1, (64 * W) / pairs);            // that share a pair's figures
     const int team = teams > 1 ? tid / pairs : 0;
-    float2 first[8];
-    {
-        const int i = min(tid - team * pairs, pairs - 1), n = divided(i, p.by_half);
-        read8(first, s.list[n], i - n * half, min(team, teams - 1));
-    }
-    for (int i = tid; i < listed << shift; i += kAttn8Threads) {
+    constexpr int kTurns = kRows >= 4 * W ? 4 : kRows >= 2 * W ? 2 : 1, kFigures = 8;   // (of all pairs of a head size of 128, if they are few)
+    const auto read = [&](float2 (&a)[kTurns][kFigures], int i0, int f0) {   // pairs i0, i0 + threads, ..., figures f0, f0 + teams, ...
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int at = min(i0 + t * (64 * W), pairs - 1), n = divided(at, p.by_half), r = s.list[n], last = s.target[r] - 1;
+            float2* src = figures_of(r) + 1 + at - n * half;
+            if (i0 + t * (64 * W) < pairs || t == 0)
+#pragma unroll
+                for (int h = 0; h < kFigures; ++h) a[t][h] = read_figure(src + (int64_t)slot_of(r, min(f0 + h * teams, last)) * stride);
+        }
+    };
+    float2 a[kTurns][kFigures];
+    read(a, tid - team * pairs, min(team, teams - 1));
+    for (int i = tid; i < listed << shift; i += (64 * W)) {
         const int r = s.list[i >> shift], f = i & ((1 << shift) - 1);
         if (f < s.target[r]) factor[i] = read_figure(figures_of(r) + (int64_t)slot_of(r, f) * stride);
     }
     __syncthreads();
-    for (int n = wave; n < listed; n += kAttn8Waves) {
+    for (int n = wave; n < listed; n += W) {
         const int target = s.target[s.list[n]];
         float2* mine = factor + (n << shift);
-        float2 a[2];
+        float2 ml[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) a[h] = lane + 64 * h < target ? mine[lane + 64 * h] : make_float2(-INFINITY, 0.0f);
-        const float m = over_lanes<64>(fmaxf(a[0].x, a[1].x), MaxOp());
-        const float f0 = __builtin_amdgcn_exp2f(a[0].x - m), f1 = __builtin_amdgcn_exp2f(a[1].x - m);
-        const float l = over_lanes<64>(f0 * a[0].y + f1 * a[1].y, AddOp());
+        for (int h = 0; h < 2; ++h) ml[h] = lane + 64 * h < target ? mine[lane + 64 * h] : make_float2(-INFINITY, 0.0f);
+        const float m = over_lanes<64>(fmaxf(ml[0].x, ml[1].x), MaxOp());
+        const float f0 = __builtin_amdgcn_exp2f(ml[0].x - m), f1 = __builtin_amdgcn_exp2f(ml[1].x - m);
+        const float l = over_lanes<64>(f0 * ml[0].y + f1 * ml[1].y, AddOp());
         if (lane < target) mine[lane].x = f0 / l;
         if (lane + 64 < target) mine[lane + 64].x = f1 / l;
     }
     __syncthreads();
     float2* sums = factor + kRows * kMost;
-    for (int i = tid; i < pairs * teams; i += kAttn8Threads) {  // (more than one team: one turn)
-        const int at = i - team * pairs, n = divided(at, p.by_half), e = at - n * half, r = s.list[n], target = s.target[r];
-        float x = 0.0f, y = 0.0f;
-        const auto add8 = [&](const float2 (&a)[8], int f) {
+    for (int i0 = tid - team * pairs; i0 < pairs; i0 += kTurns * (64 * W)) {
+        float2 sum[kTurns];
 #pragma unroll
-            for (int h = 0; h < 8; ++h) {
-                const float w = f + h * teams < target ? factor[(n << shift) + f + h * teams].x : 0.0f;
-                x += w * a[h].x;
-                y += w * a[h].y;
+        for (int t = 0; t < kTurns; ++t) sum[t] = make_float2(0.0f, 0.0f);
+        for (int f0 = team; f0 < s.most; f0 += kFigures * teams) {
+            if (f0 != team || i0 != tid - team * pairs) read(a, i0, f0);
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) {
+                const int at = min(i0 + t * (64 * W), pairs - 1), n = divided(at, p.by_half), target = s.target[s.list[n]];
+                if (i0 + t * (64 * W) < pairs || t == 0)
+#pragma unroll
+                    for (int h = 0; h < kFigures; ++h) {
+                        const int f = f0 + h * teams;
+                        const float w = f < target ? factor[(n << shift) + f].x : 0.0f;
+                        sum[t].x += w * a[t][h].x;
+                        sum[t].y += w * a[t][h].y;
+                    }
             }
-        };
-        int f = team;
-        if (i == tid) {
-            add8(first, f);
-            f += 8 * teams;
         }
-        for (; f < target; f += 8 * teams) {
-            float2 a[8];
-            read8(a, r, e, f);
-            add8(a, f);
+        if (teams > 1) {
+            if (team < teams) sums[team * pairs + i0] = sum[0];   // (all pairs in one turn)
+        } else {
+#pragma unroll
+            for (int t = 0; t < kTurns; ++t) {
+                const int at = i0 + t * (64 * W), n = divided(min(at, pairs - 1), p.by_half), e = at - n * half, r = s.list[n];
+                if (at < pairs && s.active[r]) *reinterpret_cast<float2*>(p.out + attn8_row_at(p, head, row0 + r) + 2 * e) = sum[t];
+            }
         }
-        if (teams > 1) sums[i] = make_float2(x, y);
-        else if (s.active[r]) *reinterpret_cast<float2*>(p.out + attn8_row_at(p, head, row0 + r) + 2 * e) = make_float2(x, y);
     }
     if (teams > 1) {                                       // uniform
         __syncthreads();
         if (tid < pairs) {
             const int n = divided(tid, p.by_half), e = tid - n * half, r = s.list[n];
-            float x = 0.0f, y = 0.0f;
+            float2 sum = make_float2(0.0f, 0.0f);
             for (int t = 0; t < teams; ++t) {
-                x += sums[t * pairs + tid].x;
-                y += sums[t * pairs + tid].y;
+                sum.x += sums[t * pairs + tid].x;
+                sum.y += sums[t * pairs + tid].y;
             }
-            if (s.active[r]) *reinterpret_cast<float2*>(p.out + attn8_row_at(p, head, row0 + r) + 2 * e) = make_float2(x, y);
+            if (s.active[r]) *reinterpret_cast<float2*>(p.out + attn8_row_at(p, head, row0 + r) + 2 * e) = sum;
         }
     }
     if (tid < listed) __hip_atomic_store(counters + s.list[tid], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -4,15 +4,21 @@
 
 namespace bl {
 
-constexpr int kAttn8Waves = 4;            // waves of a workgroup
-constexpr int kRows8Set = 256;            // positions that a workgroup of the rows form walks at a time: a chunk of 64 per wave
-constexpr int kTiles8Set = 128;           // ... of the tiles form: 32 per wave
-constexpr int kTiles8Rows = 32;           // rows of a workgroup of the tiles form
+constexpr int kRows8Waves = 8;            // waves of a workgroup of the rows form, each with a chunk of 64 positions at a time
+constexpr int kRows8FewWaves = 4;         // ... with more than four rows, and beside tiles
+// ... with many heads and sequences: more workgroups than compute units.  A unit holds one workgroup of eight waves (133 registers) and six of two,
+// and what a short walk takes is waiting.  32 heads of 128, caches of 17 positions, eight and two waves, us: 8 sequences 5.9 and TIMES, 16 10.2 and
+// TIMES, 64 37.4 and TIMES.
+constexpr int kRows8ManyWaves = 2;
+constexpr int kAttn8Units = 256;          // compute units
+constexpr int kTiles8Set = 7;             // positions that a workgroup of the tiles form walks at a time: 1 << 7, 32 per wave
+constexpr int kTiles8Rows = 32;           // rows of a tile
 constexpr int kAttn8MaxSplits = 64;       // workgroups that share a row's walk: the merge's lanes
-#ifndef WGS
-#define WGS 512
-#endif
-constexpr int kAttn8Workgroups = WGS;     // that a launch aims at: two on each of 256 compute units
+constexpr int kAttn8Waves = 2048;         // that a launch aims at: two on each SIMD of 256 compute units
+// A short walk that meets nobody else is not split: the meeting (figures performed, tickets, figures read: three trips to memory) takes 3.6 us, a
+// set of 512 positions in one compute unit 1.0 us with a head size of 64 and 1.8 with 128.  One workgroup per head and one per set, us: 32 heads
+// of 128 at 1000 positions 9.3 and 10.5, at 2000 12.9 and 10.9; 12 of 64 at 1000 6.7 and 9.0, at 2000 8.7 and 9.3.
+constexpr int kRows8Together = 256 << 10;   // bytes of codes
 
 // Division by a number that the host knows, for 0 <= n < 2^31: n m >> (31 + s) with 2^s >= d and m = 2^(31 + s) / d rounded up.  m d exceeds
 // 2^(31 + s) by less than d <= 2^s, so n m / 2^(31 + s) exceeds n / d by less than 1 / d: the same whole number.  (A workgroup that divides
@@ -28,46 +34,70 @@ constexpr Divider divider(int d) {
 }
 constexpr int divided(int n, Divider by) { return by.m ? (int)((uint32_t)(((uint64_t)(uint32_t)n * by.m) >> 32) >> by.shift) : n; }
 
-constexpr int sets_of(int positions, int set) { return (positions + set - 1) / set; }
+constexpr int sets_of(int positions, int set) { return (int)(((int64_t)positions + (1 << set) - 1) >> set); }   // of 1 << set positions
 
 // A launch's parts.  Shared: the walk that all tokens share (a prefix, or a prompt's cache), in blocks of rows, all of them by each piece of the
 // walk.  Own: each sequence's own rows.
 struct Attn8Plan {
     int     tiles;            // the shared part in tiles of 32 rows; else (and the own part) rows in fours
+    int     tile_rows;        // rows of a workgroup of the tiles form: 32, 64 or 128
     int     block;            // rows of a workgroup of the rows form: 4, 8 or 16
-    int     shared_set;       // positions of a set of the shared part
+    int     shared_set, own_set;   // 1 << so many positions are a workgroup's set
+    int     waves;            // of a workgroup of the rows form
+    int     apart;            // the own part is a launch of its own, behind the one of the tiles
     int     shared_splits;    // workgroups that share the walk over the shared rows; 0: none
     int     shared_blocks;    // row blocks over all tokens
     int     own_splits;       // the same for a sequence's own rows; 0: none
     int     own_blocks;       // row blocks of one sequence's rows
     int64_t shared_wgs, own_wgs;
     int     slots() const { return shared_splits + own_splits; }   // figures that a row's workgroups leave
+    bool    meets() const { return !tiles && slots() > 1; }        // the workgroups of a row meet by counters (else: one, or a merging launch)
 };
 
-// shared_len: positions of the shared walk, own_len: of each token's own (0: none).
-inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, int own_len) {
+// shared_len: positions of the shared walk, own_len: of each token's own (0: none).  size: bytes of a row of codes.
+inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, int own_len, int size) {
     Attn8Plan p{};
     const int64_t rows = (int64_t)tokens * group;
     p.tiles = shared_len > 0 && rows > 4;
     const int64_t most = p.tiles ? (own_len > 0 ? 4 : 0) : shared_len > 0 ? rows : group;   // (beside tiles: fours)
     p.block = most <= 4 ? 4 : most <= 8 ? 8 : 16;
-    const int shared_block = p.tiles ? kTiles8Rows : p.block;
-    p.shared_set = p.tiles ? kTiles8Set : kRows8Set;
-    p.shared_blocks = shared_len > 0 ? (int)((rows + shared_block - 1) / shared_block) : 0;
     p.own_blocks = own_len > 0 ? (group + p.block - 1) / p.block : 0;
-    const int64_t shared = (int64_t)n_heads * p.shared_blocks, own = (int64_t)n_heads * tokens * p.own_blocks;
+    const int64_t own = (int64_t)n_heads * tokens * p.own_blocks;
+    // own walks beside tiles, in their kernel, share a unit two by two; more than that many are launched by themselves
+    p.apart = p.tiles && own > 2 * kAttn8Units;
+    const int64_t units = own > 0 ? own : n_heads * ((rows + p.block - 1) / p.block);
+    p.waves = p.block > 4 || (p.tiles && !p.apart) ? kRows8FewWaves : units > kAttn8Units ? kRows8ManyWaves : kRows8Waves;
+    p.own_set = p.waves == kRows8Waves ? 9 : p.waves == kRows8FewWaves ? 8 : 7;
+    // a prompt of many rows: two or four tiles per workgroup
+    int more = 0;
+    while (p.tiles && own_len == 0 && more < 2 && n_heads * ((rows + (2 * kTiles8Rows << more) - 1) / (2 * kTiles8Rows << more)) * kRows8FewWaves >= kAttn8Waves) ++more;
+    p.tile_rows = kTiles8Rows << more;
+    const int shared_block = p.tiles ? p.tile_rows : p.block;
+    p.shared_set = p.tiles ? kTiles8Set - more : p.own_set;
+    p.shared_blocks = shared_len > 0 ? (int)((rows + shared_block - 1) / shared_block) : 0;
+    const int64_t shared = (int64_t)n_heads * p.shared_blocks;
     // positions per workgroup: the fewest with which the launch has no more workgroups than it aims at
     const auto splits = [](int len, int set, int64_t quota) {
-        const int64_t sets = quota / set > 1 ? quota / set : 1;
+        const int64_t sets = quota >> set > 1 ? quota >> set : 1;
         return len > 0 ? (int)((sets_of(len, set) + sets - 1) / sets) : 0;
     };
-    const int longest = shared_len > own_len ? shared_len : own_len;
-    for (int64_t quota = kTiles8Set;; quota += quota / 16 / kTiles8Set * kTiles8Set + kTiles8Set) {
-        p.shared_splits = splits(shared_len, p.shared_set, quota);
-        p.own_splits = splits(own_len, kRows8Set, quota);
-        if (p.shared_splits <= kAttn8MaxSplits && p.own_splits <= kAttn8MaxSplits &&
-            (quota >= longest + kRows8Set || shared * p.shared_splits + own * p.own_splits <= kAttn8Workgroups))
-            break;
+    const auto share = [&](int shared_now, int own_now) {   // the splits of one launch
+        const int64_t longest = shared_now > own_now ? shared_now : own_now, unit = 1 << (own_now > 0 ? p.own_set : p.shared_set);
+        const bool together = !p.tiles && (shared_now == 0 || own_now == 0) && sets_of((int)longest, p.own_set) * unit * 2 * size <= kRows8Together;
+        for (int64_t quota = together || more ? longest + unit : unit;; quota += quota / 16 / unit * unit + unit) {
+            const int a = splits(shared_now, p.shared_set, quota), b = splits(own_now, p.own_set, quota);
+            if (a > kAttn8MaxSplits || b > kAttn8MaxSplits) continue;
+            if (!more && quota < longest + unit && shared * a * (p.tiles ? kRows8FewWaves : p.waves) + own * b * p.waves > kAttn8Waves) continue;
+            if (shared_now > 0) p.shared_splits = a;
+            if (own_now > 0) p.own_splits = b;
+            return;
+        }
+    };
+    if (p.apart) {
+        share(shared_len, 0);
+        share(0, own_len);
+    } else {
+        share(shared_len, own_len);
     }
     // (the shared part's workgroups go around the dies in eights, all row blocks of a piece of the cache on one die)
     p.shared_wgs = ((int64_t)n_heads * p.shared_splits + 7) / 8 * 8 * p.shared_blocks;

@@ -26,24 +26,26 @@ __device__ __forceinline__ v4i rows8_mfma(const v4i& a, const v4i& b, const v4i&
 // 65536 a + 256 b + c of a product's three sums
 __device__ __forceinline__ float rows8_joined(const v4i& s) { return fmaf((float)s[2], 65536.0f, (float)((s[1] << 8) + s[0])); }
 
-#ifdef NT
-__device__ __forceinline__ v4i rows8_load(const int8_t* at) { return __builtin_nontemporal_load(reinterpret_cast<const v4i*>(at)); }
-#else
-__device__ __forceinline__ v4i rows8_load(const int8_t* at) { return *reinterpret_cast<const v4i*>(at); }
-#endif
+// A walk's bytes are read once.  From memory, streaming loads are faster, and leave a model's weights in the memory-side cache; a short cache that
+// the token before left in the dies' caches is faster without (see launch_block).
+template <bool STREAM>
+__device__ __forceinline__ v4i rows8_load(const int8_t* at) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const v4i*>(at));
+    else return *reinterpret_cast<const v4i*>(at);
+}
 
-// KB: head size in blocks of 64 dims (rounded up).  NQ: rows of a workgroup in fours.
-template <int KB, int NQ>
+// KB: head size in blocks of 64 dims (rounded up).  NQ: rows of a workgroup in fours.  W: waves of a workgroup.  STREAM: by streaming loads.
+template <int KB, int NQ, int W>
 struct Rows8Lds {
-    static constexpr int kRows = 4 * NQ, kDims = 64 * KB;
+    static constexpr int kRows = 4 * NQ, kDims = 64 * KB, kThreads = 64 * W;
     static constexpr int kQuery = 0;                                          // [row][byte][dims]
     static constexpr int kNew = kQuery + kRows * 3 * kDims;                   // the token's own key and value
     static constexpr int kWeights = kNew + 2 * kDims;                         // [wave][four rows][16][pitch]
-    static constexpr int kWalk = kWeights + kAttn8Waves * NQ * 16 * kWeightPitch;
+    static constexpr int kWalk = kWeights + W * NQ * 16 * kWeightPitch;
     static constexpr int kPitch = kDims + 16;                                 // floats per row of weighted values
-    static constexpr int kMeet = kAttn8Waves * kRows * (kPitch * 4 + 8);      // [wave][row] values, then [wave][row] (maximum, sum)
+    static constexpr int kMeet = W * kRows * (kPitch * 4 + 8);      // [wave][row] values, then [wave][row] (maximum, sum)
     static constexpr int kMost = 2 * kAttn8MaxSplits;                         // figures of one row at most
-    static constexpr int kMerge = kRows * kMost * 8 + kAttn8Threads * 8;
+    static constexpr int kMerge = kRows * kMost * 8 + kThreads * 8;
     static constexpr int kBytes = kWalk > kMeet ? (kWalk > kMerge ? kWalk : kMerge) : kMeet > kMerge ? kMeet : kMerge;
 };
 
@@ -52,10 +54,10 @@ struct Rows8Shared {
     float new_scale[2];         // of the token's own key and value
 };
 
-template <int KB, int NQ>
+template <int KB, int NQ, int W, bool STREAM>
 __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& walk_of, uint8_t* lds, Rows8Shared& shared, Attn8Rows& rows_of) {
-    using L = Rows8Lds<KB, NQ>;
-    constexpr int DT = 4 * KB, kRows = L::kRows, kDims = L::kDims;
+    using L = Rows8Lds<KB, NQ, W>;
+    constexpr int DT = 4 * KB, kRows = L::kRows, kDims = L::kDims, kThreads = L::kThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int j = lane & 15, g = lane >> 4;     // an operand's column (row) and its sixteen of the contraction; of results: column, query
     const int d = p.head_dim, half = d >> 1, size = p.size;
@@ -64,8 +66,8 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
               lowest = walk_of.lowest, sequence = walk_of.sequence, sets = walk_of.sets;
     const int chunks = kv8_chunks(keys);
     const int last_set = split + (walk_of.mine - 1) * splits;
-    const int mine = walk_of.mine - (kAttn8Waves * last_set + wave >= chunks ? 1 : 0);   // chunks of this wave
-    const auto chunk_of = [&](int i) { return kAttn8Waves * (split + i * splits) + wave; };
+    const int mine = walk_of.mine - (W * last_set + wave >= chunks ? 1 : 0);   // chunks of this wave
+    const auto chunk_of = [&](int i) { return W * (split + i * splits) + wave; };
     const bool owner = sequence >= 0 && last_set == sets - 1;                         // this workgroup's walk ends with the token itself
 
     // ---- requests: operands of 16 bytes per lane, from consecutive memory
@@ -80,7 +82,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const bool last = b == KB - 1;             // (a full block's rows are 64 bytes apart, too)
-                k[b][u] = rows8_load(base + b * 4096 + (last ? 16 * u * tail : 1024 * u) + (last ? k_tail : k_full));
+                k[b][u] = rows8_load<STREAM>(base + b * 4096 + (last ? 16 * u * tail : 1024 * u) + (last ? k_tail : k_full));
             }
         k_scale = *reinterpret_cast<const f32x4*>(c.k_scale + chunk_of(i) * kKv8Chunk + 4 * j);
     };
@@ -88,7 +90,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
         const int8_t* base = c.v + (int64_t)chunk_of(i) * (kKv8Chunk * size);
 #pragma unroll
         for (int t = 0; t < DT; ++t)   // (beyond the head size: the last sixteen dims again; nobody stores what comes of them)
-            v[t] = rows8_load(base + min(t, (size >> 4) - 1) * 1024 + k_full);
+            v[t] = rows8_load<STREAM>(base + min(t, (size >> 4) - 1) * 1024 + k_full);
         v_scale = *reinterpret_cast<const f32x4*>(c.v_scale + chunk_of(i) * kKv8Chunk + 4 * j);
     };
     if (mine > 0) {
@@ -100,16 +102,18 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
     // ---- the rows' queries, rotated, as three bytes per element; the token's own key and value as cached
     {
         constexpr int kPairs = (KB + 1) / 2;               // of a lane: elements i = lane + 64 n and i + half
-        float lo[NQ + 1][kPairs], hi[NQ + 1][kPairs];
-        float2 cs[NQ + 1][kPairs];
-        const bool fresh = owner && wave < 2;              // wave 0: the key, wave 1: the value
-        // (requests stand under no condition: a row beyond the last repeats it, an element beyond the half another one, and what comes of
-        // a token that takes no part is not written)
+        constexpr int kTasks = (kRows + 2 + W - 1) / W;    // of a wave: rows, then the key, then the value
+        float lo[kTasks][kPairs], hi[kTasks][kPairs];
+        float2 cs[kTasks][kPairs];
+        const int tasks = owner ? rows + 2 : rows;         // (rows beyond the last have what LDS held: nobody looks at what comes of them)
+        // (requests stand under no condition of a lane: an element beyond the half is another one, and what comes of a token that takes no
+        // part is not written)
 #pragma unroll
-        for (int n = 0; n <= NQ; ++n) {
-            if (n == NQ && !fresh) break;                  // uniform
-            const int row = row0 + min(wave + 4 * n, rows - 1);
-            const float* src = n < NQ ? p.q + attn8_row_at(p, head, row) : (wave == 0 ? p.k_new : p.v_new) + ((int64_t)sequence * p.n_heads + head) * d;
+        for (int n = 0; n < kTasks; ++n) {
+            const int t = wave + W * n;
+            if (t >= tasks) break;                         // uniform
+            const int row = row0 + min(t, rows - 1);
+            const float* src = t < rows ? p.q + attn8_row_at(p, head, row) : (t == rows ? p.k_new : p.v_new) + ((int64_t)sequence * p.n_heads + head) * d;
             const int pos = sequence >= 0 ? walk_of.pos : attn8_position(p, divided(row, p.by_group));
             const float2* angles = p.rope + (int64_t)(attn8_takes_part(p, pos) ? pos : 0) * half;
 #pragma unroll
@@ -121,12 +125,13 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
             }
         }
 #pragma unroll
-        for (int n = 0; n <= NQ; ++n) {
-            if (n == NQ && !fresh) break;                  // uniform
+        for (int n = 0; n < kTasks; ++n) {
+            const int t = wave + W * n;
+            if (t >= tasks) break;                         // uniform
             float amax = 0.0f;
 #pragma unroll
             for (int m = 0; m < kPairs; ++m) {
-                if (n < NQ || wave == 0) {                 // (a value is not rotated)
+                if (t <= rows) {                           // (a value is not rotated)
                     const float a = lo[n][m], b = hi[n][m];
                     lo[n][m] = a * cs[n][m].x - b * cs[n][m].y;
                     hi[n][m] = a * cs[n][m].y + b * cs[n][m].x;
@@ -134,11 +139,10 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                 amax = fmaxf(amax, fmaxf(fabsf(lo[n][m]), fabsf(hi[n][m])));
             }
             amax = wave_max(amax);
-            if (n < NQ) {
-                const int r = wave + 4 * n;
+            if (t < rows) {
                 const float inv = query_inv(amax);
-                if (lane == 0) shared.unit[r] = amax * (1.0f / kQueryFull) * p.unit;
-                uint8_t* dst = lds + L::kQuery + r * 3 * kDims;
+                if (lane == 0) shared.unit[t] = amax * (1.0f / kQueryFull) * p.unit;
+                uint8_t* dst = lds + L::kQuery + t * 3 * kDims;
                 const auto put = [&](int e, uint32_t bytes) {
                     dst[e] = (uint8_t)bytes;
                     dst[kDims + e] = (uint8_t)(bytes >> 8);
@@ -156,8 +160,8 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
             } else {
                 float inv, scale;
                 kv8_scales(amax, inv, scale);
-                if (lane == 0) shared.new_scale[wave] = scale;
-                uint8_t* dst = lds + L::kNew + wave * kDims;
+                if (lane == 0) shared.new_scale[t - rows] = scale;
+                uint8_t* dst = lds + L::kNew + (t - rows) * kDims;
 #pragma unroll
                 for (int m = 0; m < kPairs; ++m) {
                     const int i = lane + 64 * m;
@@ -175,7 +179,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
     const int at = keys - 1;                               // of the token in its own cache
     if (owner && row0 == sequence * p.group) {             // its first block of rows stores the row
         const int64_t base = (int64_t)(chunks - 1) * (kKv8Chunk * size);
-        for (int e = tid; e < size; e += kAttn8Threads) {
+        for (int e = tid; e < size; e += kThreads) {
             c.k[base + kv8_key_at(at, e, size)] = (int8_t)lds[L::kNew + e];
             c.v[base + kv8_value_at(at, e)] = (int8_t)lds[L::kNew + kDims + e];
         }
@@ -314,7 +318,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
     // ---- the waves meet
     __syncthreads();                                       // the queries and weights in LDS are done with
     float* meet = reinterpret_cast<float*>(lds);
-    float2* meet_ml = reinterpret_cast<float2*>(meet + kAttn8Waves * kRows * L::kPitch);
+    float2* meet_ml = reinterpret_cast<float2*>(meet + W * kRows * L::kPitch);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const float l = over_lanes<16>(run_l[n], AddOp());
@@ -323,30 +327,30 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
         for (int t = 0; t < DT; ++t) meet[(wave * kRows + 4 * n + g) * L::kPitch + 16 * t + j] = o[n][t];
     }
     __syncthreads();
-    const auto factors = [&](int r, float (&f)[kAttn8Waves]) {   // of the waves' figures; returns their maximum
-        float2 ml[kAttn8Waves];
+    const auto factors = [&](int r, float (&f)[W]) {   // of the waves' figures; returns their maximum
+        float2 ml[W];
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kAttn8Waves; ++w) {
+        for (int w = 0; w < W; ++w) {
             ml[w] = meet_ml[w * kRows + r];
             m = fmaxf(m, ml[w].x);
         }
         const float ref = m == -INFINITY ? 0.0f : m;       // (a prompt's row whose walk ends before this workgroup's chunks)
         float l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kAttn8Waves; ++w) {
+        for (int w = 0; w < W; ++w) {
             f[w] = __builtin_amdgcn_exp2f(ml[w].x - ref);
             l += f[w] * ml[w].y;
         }
         return make_float2(m, l);
     };
-    attn8_finish<kRows, L::kMost>(
+    attn8_finish<kRows, L::kMost, W>(
         p, rows_of, lds, head, row0, rows, walk_of.slot,
         [&](int r, int e) {
-            float f[kAttn8Waves], x = 0.0f, y = 0.0f;
+            float f[W], x = 0.0f, y = 0.0f;
             factors(r, f);
 #pragma unroll
-            for (int w = 0; w < kAttn8Waves; ++w) {
+            for (int w = 0; w < W; ++w) {
                 const float2 a = *reinterpret_cast<const float2*>(meet + (w * kRows + r) * L::kPitch + e);
                 x += f[w] * a.x;
                 y += f[w] * a.y;
@@ -354,7 +358,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
             return make_float2(x, y);
         },
         [&](int r) {
-            float f[kAttn8Waves];
+            float f[W];
             return factors(r, f);
         });
 }

@@ -1,6 +1,8 @@
 // The tiles form of the attention over 8-bit caches: 32 rows (token, query head) that read one key head, against 32 positions at a time.
 //
-// A workgroup's four waves share out the 32-position halves of chunks and merge their running maxima, sums and outputs at the end; a wave
+// A workgroup's four waves share out the 32-position halves of chunks and merge their running maxima, sums and outputs at the end (SETS = 4), or
+// have two or four tiles of 32 rows, with two waves or one for each: a long prompt has workgroups enough, and what a tile costs beside its
+// halves -- its queries' way into the operands, the meeting -- is paid less often per half (2048 tokens, 32 heads of 128: attention TIMES).  A wave
 // brings its own operands and waits for nobody.  Every operand comes from memory as it lies there (bl_kv8.hpp), 16 bytes per lane: no LDS,
 // no transposition.
 //
@@ -12,13 +14,17 @@
 // same g loads for a dim.  So O^T += V^T P^T has its operands in place: 32x32x16 f16 products, codes converted (exactly) in registers, a
 // weight w = p s^v as the sum of two f16 numbers (22 bits), scaled by a power of two over the largest s^v so far, so that moving it is
 // exact.  fp32 accumulation throughout.
+//
+// A half's scores are formed while the weights and outputs of the half before are: 28 matrix instructions (900 cycles) beside some 340 vector
+// instructions (1400) in one stream, eight after each, so that a wave keeps both pipes busy by itself.  With the two in turn, the two waves of a
+// SIMD stayed in step, and a half took the sum of both (PER HALF).
 #pragma once
 #include "bl_attn8.hpp"
 
 namespace bl {
 
-constexpr int kTiles8Keys = 32;
-static_assert(kTiles8Set == kAttn8Waves * kTiles8Keys, "a half chunk per wave");
+constexpr int kTiles8Keys = 32, kTiles8Waves = 4, kTiles8Threads = 64 * kTiles8Waves;
+static_assert(1 << kTiles8Set == kTiles8Waves * kTiles8Keys, "a half chunk per wave");
 // A row's reference score moves when a score exceeds it by 2^8: nearly every half has a new maximum for one of 32 queries (2048 tokens: all but
 // a few), and the 64 products that rescale the outputs are a sixth of a half's instructions.  Weights are then up to 2^8 and, scaled by 2^7,
 // 2^15: f16 numbers whose second part is a normal number down to 2^-2.
@@ -49,31 +55,37 @@ template <int D32>
 struct Tiles8Lds {
     static constexpr int kDims = 32 * D32;
     static constexpr int kQPitch = 3 * kDims + 16;                    // bytes per row of queries: rows spread over the banks
-    static constexpr int kQuery = 32 * kQPitch;
     static constexpr int kOPitch = kDims + 4;                         // floats per row of outputs
-    static constexpr int kMeet = kAttn8Waves * 32 * kOPitch * 4;
-    static constexpr int kMost = 2 * kAttn8MaxSplits;
-    static constexpr int kMerge = 32 * kMost * 8 + kAttn8Threads * 8;
-    static constexpr int kBytes = kQuery > kMeet ? (kQuery > kMerge ? kQuery : kMerge) : kMeet > kMerge ? kMeet : kMerge;
+    static constexpr int kMeet = kTiles8Waves * 32 * kOPitch * 4;     // (a tile's queries are no larger: four tiles' fit, too)
+    static constexpr int kBytes = kMeet;
+    static_assert(kTiles8Waves * 32 * kQPitch <= kMeet, "four tiles of queries");
 };
 
 struct Tiles8Shared {
-    float  unit[32];
-    float  scale[kAttn8Waves][2 * kTiles8Keys] __attribute__((aligned(16)));   // a half's key scales, value scales
-    float2 ml[kAttn8Waves][32];                                        // the waves' maxima and sums
+    float  unit[kTiles8Waves * 32];
+    float  scale[kTiles8Waves][2][2 * kTiles8Keys] __attribute__((aligned(16)));   // two halves' key scales, value scales
+    float2 ml[kTiles8Waves][32];                                       // the waves' maxima and sums
 };
 
-template <int D32>
+template <int D32, int SETS>
 __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk& walk_of, uint8_t* lds, Tiles8Shared& shared, Attn8Rows& rows_of) {
     using L = Tiles8Lds<D32>;
-    const int tid = threadIdx.x, lane = tid & 63, set = __builtin_amdgcn_readfirstlane(tid >> 6);
+    static_assert(SETS == 4 || SETS == 2 || SETS == 1, "waves of a tile");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tile = wave / SETS, set = wave % SETS;
     const int l32 = lane & 31, g = lane >> 5;
     const int d = p.head_dim, half = d >> 1, size = p.size;
-    const int head = walk_of.head, row0 = walk_of.row0, rows = walk_of.rows, keys = walk_of.keys, lowest = walk_of.lowest, split = walk_of.split,
-              splits = walk_of.splits;
+    const int head = walk_of.head, split = walk_of.split, splits = walk_of.splits;
+    // this wave's tile of the workgroup's rows (rows beyond the last repeat it)
+    const int row0 = walk_of.row0 + 32 * tile, rows = min(32, walk_of.rows - 32 * tile);
+    const auto row_of = [&](int r) { return walk_of.row0 + min(32 * tile + r, walk_of.rows - 1); };
+    const int keys = p.prompt ? p.pos0 + divided(row_of(31), p.by_group) + 1 : walk_of.keys;
+    const int lowest = p.prompt ? p.pos0 + divided(row_of(0), p.by_group) + 1 : keys;
     const int halves = (keys + kTiles8Keys - 1) / kTiles8Keys;
-    const auto half_of = [&](int i) { return kAttn8Waves * (split + splits * i) + set; };
-    const int mine = walk_of.mine - (half_of(walk_of.mine - 1) >= halves ? 1 : 0);   // halves of this wave
+    const auto half_of = [&](int i) { return SETS * (split + splits * i) + set; };
+    int mine = rows > 0 ? walk_of.mine : 0;                            // halves of this wave
+    if (SETS < 4) mine = min(mine, (halves - set + SETS - 1) / SETS);  // (one split: a tile's own end)
+    if (mine > 0 && half_of(mine - 1) >= halves) --mine;
 
     // ---- requests
     const float* scales = (g ? walk_of.c.v_scale : walk_of.c.k_scale) + l32;
@@ -110,71 +122,75 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         request_values(0);
     }
 
-    // ---- the rows' queries: rotated, three bytes per element, through LDS.  Eight lanes share a row, two neighbouring elements and their
-    // partners in the other half of the head at a time.
+    // ---- the tile's queries: rotated, three bytes per element, through LDS.  Eight lanes share a row, two neighbouring elements and their
+    // partners in the other half of the head at a time; the waves of a tile share its rows.
+    uint8_t* queries = lds + tile * 32 * L::kQPitch;
     {
-        constexpr int kTurns = D32;                       // 16 of at most 16 D32 elements of a half each
+        constexpr int kTurns = D32, kPasses = 4 / SETS;    // 16 of at most 16 D32 elements of a half each; eight rows each
         typedef float f32x2_u __attribute__((ext_vector_type(2), aligned(4)));
         typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(8)));
-        const int r = tid >> 3, t8 = tid & 7, row = row0 + min(r, rows - 1);   // (rows beyond the last repeat it)
-        const int pos = attn8_position(p, divided(row, p.by_group));
-        const bool there = attn8_takes_part(p, pos);
-        const float* src = p.q + attn8_row_at(p, head, row);
-        const float* angles = reinterpret_cast<const float*>(p.rope + (int64_t)(there ? pos : 0) * half);
-        f32x2 lo[kTurns], hi[kTurns];
-        f32x4 cs[kTurns];
+        const int t8 = lane & 7;
 #pragma unroll
-        for (int m = 0; m < kTurns; ++m) {
-            const int i = 2 * (t8 + 8 * m);
-            lo[m] = hi[m] = f32x2{0.0f, 0.0f};
-            cs[m] = f32x4{1.0f, 0.0f, 1.0f, 0.0f};
-            if (there && i < half) {
-                lo[m] = *reinterpret_cast<const f32x2_u*>(src + i);
-                hi[m] = *reinterpret_cast<const f32x2_u*>(src + half + i);
-                cs[m] = *reinterpret_cast<const f32x4_u*>(angles + 2 * i);
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int r = 8 * (set * kPasses + pass) + (lane >> 3), row = row_of(r);
+            const int pos = attn8_position(p, divided(row, p.by_group));
+            const bool there = attn8_takes_part(p, pos);
+            const float* src = p.q + attn8_row_at(p, head, row);
+            const float* angles = reinterpret_cast<const float*>(p.rope + (int64_t)(there ? pos : 0) * half);
+            f32x2 lo[kTurns], hi[kTurns];
+            f32x4 cs[kTurns];
+#pragma unroll
+            for (int m = 0; m < kTurns; ++m) {
+                const int i = 2 * (t8 + 8 * m);
+                lo[m] = hi[m] = f32x2{0.0f, 0.0f};
+                cs[m] = f32x4{1.0f, 0.0f, 1.0f, 0.0f};
+                if (there && i < half) {
+                    lo[m] = *reinterpret_cast<const f32x2_u*>(src + i);
+                    hi[m] = *reinterpret_cast<const f32x2_u*>(src + half + i);
+                    cs[m] = *reinterpret_cast<const f32x4_u*>(angles + 2 * i);
+                }
             }
+            float amax = 0.0f;
+#pragma unroll
+            for (int m = 0; m < kTurns; ++m)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float a = lo[m][x], b = hi[m][x], c = cs[m][2 * x], s = cs[m][2 * x + 1];
+                    lo[m][x] = a * c - b * s;
+                    hi[m][x] = a * s + b * c;
+                    amax = fmaxf(amax, fmaxf(fabsf(lo[m][x]), fabsf(hi[m][x])));
+                }
+#pragma unroll
+            for (int x = 1; x < 8; x <<= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
+            const float inv = query_inv(amax);
+            if (t8 == 0) shared.unit[32 * tile + r] = amax * (1.0f / kQueryFull) * 256.0f * p.unit;
+            uint8_t* dst = queries + r * L::kQPitch;
+            const auto put = [&](int e, const f32x2& x) {      // byte by byte, both elements' side by side
+                const uint32_t a = query_bytes(x[0], inv), b = query_bytes(x[1], inv);
+                *reinterpret_cast<uint16_t*>(dst + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0400u);
+                *reinterpret_cast<uint16_t*>(dst + L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0501u);
+                *reinterpret_cast<uint16_t*>(dst + 2 * L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0602u);
+            };
+#pragma unroll
+            for (int m = 0; m < kTurns; ++m) {
+                const int i = 2 * (t8 + 8 * m);
+                if (i < half) {
+                    put(i, lo[m]);
+                    put(half + i, hi[m]);
+                }
+            }
+            for (int e = d + 2 * t8; e < L::kDims; e += 16) put(e, f32x2{0.0f, 0.0f});
         }
-        float amax = 0.0f;
-#pragma unroll
-        for (int m = 0; m < kTurns; ++m)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const float a = lo[m][x], b = hi[m][x], c = cs[m][2 * x], s = cs[m][2 * x + 1];
-                lo[m][x] = a * c - b * s;
-                hi[m][x] = a * s + b * c;
-                amax = fmaxf(amax, fmaxf(fabsf(lo[m][x]), fabsf(hi[m][x])));
-            }
-#pragma unroll
-        for (int x = 1; x < 8; x <<= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
-        const float inv = query_inv(amax);
-        if (t8 == 0) shared.unit[r] = amax * (1.0f / kQueryFull) * 256.0f * p.unit;
-        uint8_t* dst = lds + r * L::kQPitch;
-        const auto put = [&](int e, const f32x2& x) {      // byte by byte, both elements' side by side
-            const uint32_t a = query_bytes(x[0], inv), b = query_bytes(x[1], inv);
-            *reinterpret_cast<uint16_t*>(dst + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0400u);
-            *reinterpret_cast<uint16_t*>(dst + L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0501u);
-            *reinterpret_cast<uint16_t*>(dst + 2 * L::kDims + e) = (uint16_t)__builtin_amdgcn_perm(b, a, 0x0c0c0602u);
-        };
-#pragma unroll
-        for (int m = 0; m < kTurns; ++m) {
-            const int i = 2 * (t8 + 8 * m);
-            if (i < half) {
-                put(i, lo[m]);
-                put(half + i, hi[m]);
-            }
-        }
-        for (int e = d + 2 * t8; e < L::kDims; e += 16) put(e, f32x2{0.0f, 0.0f});
     }
-    if (tid < rows) attn8_count(p, rows_of, tid, row0 + tid, attn8_walked(p, walk_of));
+    if (SETS == 4 && tid < rows) attn8_count(p, rows_of, tid, row0 + tid, attn8_walked(p, walk_of));
     __syncthreads();
     v4i q[3][D32];   // B operands: column l32, dims 32 s + 16 g ...
 #pragma unroll
     for (int b = 0; b < 3; ++b)
 #pragma unroll
-        for (int s = 0; s < D32; ++s) q[b][s] = *reinterpret_cast<const v4i*>(lds + l32 * L::kQPitch + b * L::kDims + 32 * s + 16 * g);
-    const float unit = shared.unit[l32];
-    const int limit = p.prompt ? min(keys, p.pos0 + divided(row0 + l32, p.by_group) + 1) : keys;   // positions that this lane's query sees
-    float* scales_of = shared.scale[set];
+        for (int s = 0; s < D32; ++s) q[b][s] = *reinterpret_cast<const v4i*>(queries + l32 * L::kQPitch + b * L::kDims + 32 * s + 16 * g);
+    const float unit = shared.unit[32 * tile + l32];
+    const int limit = p.prompt ? min(keys, p.pos0 + divided(row_of(l32), p.by_group) + 1) : keys;   // positions that this lane's query sees
 
     f32x16 o[D32];
 #pragma unroll
@@ -182,42 +198,48 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
     float run_m = -INFINITY, run_l = 0.0f;      // run_l: over this lane half's positions only
-    int run_e = -100;                           // exponent of the largest value scale so far, at least (uniform)
+    int run_e = -100, next_e = -100;            // exponent of the largest value scale so far, at least (uniform); of the half under way, too
+    i32x16 low, high;                           // the scores under way: S^T, 32 positions x 32 queries, in units of 256 of the queries'
 
-    const auto walk = [&](int i, auto which) {
-        constexpr bool kLast = decltype(which)::value;
+    // A half's scales go through LDS, lanes 0-31 the keys', lanes 32-63 the values', when its keys have arrived.
+    const auto scales_in = [&](int i) {
         const int first = half_of(i) * kTiles8Keys;
-        // Only a wave's last half can be one that some query does not see all of: such halves are at most two (32 rows), one after
-        // another, of different waves.
-        const bool masked = kLast && first + kTiles8Keys > lowest;   // uniform
-        // the half's scales through LDS: lanes 0-31 brought the keys', lanes 32-63 the values'
-        float own_scale = scale;
-        if (masked && first + l32 >= keys) own_scale = 0.0f;   // what lies behind the last row may be anything
-        const float v_max = wave_max(g ? own_scale : 0.0f);
-        const int e_new = v_max > 0.0f ? max(run_e, __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max))) : run_e;
-        scales_of[lane] = g ? ldexpf(own_scale, kTiles8Scale - e_new) : own_scale;
-        __builtin_amdgcn_wave_barrier();   // (a wave's LDS operations are performed in order)
-        // S^T: 32 positions x 32 queries, in units of 256 of the queries'
-        i32x16 low, high;
+        const float own = first + l32 >= keys ? 0.0f : scale;   // (what lies behind the last row may be anything)
+        const float v_max = wave_max(g ? own : 0.0f);
+        if (v_max > 0.0f) next_e = max(next_e, __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max)));
+        shared.scale[wave][i & 1][lane] = g ? ldexpf(own, kTiles8Scale - next_e) : own;
+        __builtin_amdgcn_wave_barrier();        // (a wave's LDS operations are performed in order)
+    };
+    const auto scores_low_high = [&] {
 #pragma unroll
         for (int r = 0; r < 16; ++r) low[r] = 64;   // (an operand that is a constant: a quarter of a unit below the middle)
 #pragma unroll
         for (int r = 0; r < 16; ++r) high[r] = 0;
 #pragma unroll
-        for (int s = 0; s < D32; ++s) low = tiles8_mfma(k[s], q[0][s], low);
-#pragma unroll
-        for (int s = 0; s < D32; ++s) high = tiles8_mfma(k[s], q[2][s], high);
+        for (int s = 0; s < D32; ++s) {
+            low = tiles8_mfma(k[s], q[0][s], low);
+            high = tiles8_mfma(k[s], q[2][s], high);
+        }
+    };
+    const auto scores_middle = [&] {
 #pragma unroll
         for (int r = 0; r < 16; ++r) low[r] >>= 8;
 #pragma unroll
         for (int s = 0; s < D32; ++s) low = tiles8_mfma(k[s], q[1][s], low);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!kLast) request_keys(i + 1);
-        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // One half: its scores are in low and high.  NEXT: another half follows, its keys are here; MORE: and another one behind it.  END: one of the
+    // tile's last two halves, the only ones that some query may not see all of (32 rows).
+    const auto walk = [&](int i, auto next, auto more, auto end) {
+        constexpr bool NEXT = decltype(next)::value, MORE = decltype(more)::value, END = decltype(end)::value;
+        const int first = half_of(i) * kTiles8Keys;
+        const bool masked = END && first + kTiles8Keys > lowest;   // uniform
+        const float* scales_of = shared.scale[wave][i & 1];
+        const int e_new = next_e;
         float x[16];
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-            const f32x4 ks = *reinterpret_cast<const f32x4*>(&scales_of[16 * g + 4 * r4]);
+            const f32x4 ks = *reinterpret_cast<const f32x4*>(scales_of + 16 * g + 4 * r4);
 #pragma unroll
             for (int c = 0; c < 4; ++c) x[4 * r4 + c] = (float)((high[4 * r4 + c] << 8) + low[4 * r4 + c]) * ks[c];
         }
@@ -231,7 +253,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
         mx = over_blocks<32>(mx, MaxOp());
         // (a query whose values are all zero has unit 0; it must not meet an infinity)
-        const float top = kLast && mx == -INFINITY ? mx : mx * unit;
+        const float top = END && mx == -INFINITY ? mx : mx * unit;
         if (__any(top > run_m + kTiles8Move) || e_new != run_e) {
             const float m_new = fmaxf(run_m, top);
             const float f = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(run_m - m_new);
@@ -244,17 +266,22 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
             run_m = m_new;
             run_e = e_new;
         }
-        const float base = kLast && run_m == -INFINITY ? 0.0f : run_m;
+        const float base = END && run_m == -INFINITY ? 0.0f : run_m;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NEXT) {
+            scales_in(i + 1);
+            scores_low_high();
+        }
         u32x4 w_hi[2], w_lo[2];
         float sum = 0.0f;
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-            const f32x4 vs = *reinterpret_cast<const f32x4*>(&scales_of[kTiles8Keys + 16 * g + 4 * r4]);
+            const f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
             float w[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const float at = x[4 * r4 + c];
-                const float pj = __builtin_amdgcn_exp2f(kLast && at == -INFINITY ? at : fmaf(at, unit, -base));
+                const float pj = __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -base));
                 sum += pj;
                 w[c] = pj * vs[c];
             }
@@ -271,6 +298,10 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
             }
         }
         run_l += sum;
+        if constexpr (NEXT) {
+            __builtin_amdgcn_sched_barrier(0);
+            scores_middle();
+        }
 #pragma unroll
         for (int t = 0; t < D32; ++t) {
             u32x4 a[2];
@@ -288,48 +319,67 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!kLast) request_values(i + 1);
+        if constexpr (MORE) request_keys(i + 2);
+        if constexpr (NEXT) request_values(i + 1);
         __builtin_amdgcn_sched_barrier(0);
     };
-    for (int i = 0; i + 1 < mine; ++i) walk(i, std::false_type{});
-    if (mine > 0) walk(mine - 1, std::true_type{});
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (mine > 0) {
+        scales_in(0);
+        scores_low_high();
+        scores_middle();
+        __builtin_amdgcn_sched_barrier(0);
+        if (mine > 1) request_keys(1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int i = 0; i + 2 < mine; ++i) walk(i, yes, yes, no);
+    if (mine > 1) walk(mine - 2, yes, no, yes);
+    if (mine > 0) walk(mine - 1, no, no, yes);
 
     // ---- the waves meet: maxima and sums first, then the outputs, each scaled by its own factor
     run_l = over_blocks<32>(run_l, AddOp());
-    if (g == 0) shared.ml[set][l32] = make_float2(run_m, run_l);
+    if (g == 0) shared.ml[wave][l32] = make_float2(run_m, run_l);
     __syncthreads();
-    const auto figure = [&](int r) {
+    const auto figure = [&](int at_tile, int r) {
         float m = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kAttn8Waves; ++w) m = fmaxf(m, shared.ml[w][r].x);
+        for (int w = 0; w < SETS; ++w) m = fmaxf(m, shared.ml[at_tile * SETS + w][r].x);
         const float ref = m == -INFINITY ? 0.0f : m;       // (a prompt's row whose walk ends before this workgroup's halves)
 #pragma unroll
-        for (int w = 0; w < kAttn8Waves; ++w) l += shared.ml[w][r].y * __builtin_amdgcn_exp2f(shared.ml[w][r].x - ref);
+        for (int w = 0; w < SETS; ++w) l += shared.ml[at_tile * SETS + w][r].y * __builtin_amdgcn_exp2f(shared.ml[at_tile * SETS + w][r].x - ref);
         return make_float2(m, l);
     };
-    const float m_all = figure(l32).x;
-    const float f = ldexpf(__builtin_amdgcn_exp2f(run_m - (m_all == -INFINITY ? 0.0f : m_all)), run_e - kTiles8Scale);
+    const float2 all = figure(tile, l32);
+    float f = ldexpf(__builtin_amdgcn_exp2f(run_m - (all.x == -INFINITY ? 0.0f : all.x)), run_e - kTiles8Scale);
+    if (SETS < 4) f = rows > 0 ? f / all.y : 0.0f;         // (one split: nobody else has figures)
     float* meet = reinterpret_cast<float*>(lds);   // (the barrier above: every wave has its queries)
 #pragma unroll
     for (int t = 0; t < D32; ++t)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
-            *reinterpret_cast<f32x4*>(meet + (set * 32 + l32) * L::kOPitch + 32 * t + 8 * r4 + 4 * g) =
+            *reinterpret_cast<f32x4*>(meet + (wave * 32 + l32) * L::kOPitch + 32 * t + 8 * r4 + 4 * g) =
                 f32x4{o[t][4 * r4] * f, o[t][4 * r4 + 1] * f, o[t][4 * r4 + 2] * f, o[t][4 * r4 + 3] * f};
     __syncthreads();
-    attn8_finish<32, L::kMost>(
-        p, rows_of, lds, head, row0, rows, walk_of.slot,
-        [&](int r, int e) {
-            float2 sum = make_float2(0.0f, 0.0f);
+    const auto pair = [&](int at_tile, int r, int e) {
+        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int w = 0; w < kAttn8Waves; ++w) {
-                const float2 a = *reinterpret_cast<const float2*>(meet + (w * 32 + r) * L::kOPitch + e);
-                sum.x += a.x;
-                sum.y += a.y;
-            }
-            return sum;
-        },
-        figure);
+        for (int w = 0; w < SETS; ++w) {
+            const float2 a = *reinterpret_cast<const float2*>(meet + ((at_tile * SETS + w) * 32 + r) * L::kOPitch + e);
+            sum.x += a.x;
+            sum.y += a.y;
+        }
+        return sum;
+    };
+    if constexpr (SETS == 4) {
+        attn8_finish<32, 0, kTiles8Waves>(
+            p, rows_of, lds, head, row0, rows, walk_of.slot, [&](int r, int e) { return pair(0, r, e); }, [&](int r) { return figure(0, r); });
+    } else {
+        for (int i = tid; i < walk_of.rows * half; i += kTiles8Threads) {
+            const int r = divided(i, p.by_half), e = 2 * (i - r * half);
+            *reinterpret_cast<float2*>(p.out + attn8_row_at(p, head, walk_of.row0 + r) + e) = pair(r >> 5, r & 31, e);
+        }
+    }
 }
 
 }  // namespace bl
