@@ -5,7 +5,7 @@ Every arithmetic step runs in the library's kernels; this module owns buffers (t
 the order of the launches:
 
     decode_norm_batch(q, k, v)    h' = h + delta of the previous layer; the three products of rmsnorm(h', g_in)
-    attn_decode                   rotary embedding, cache append, attention
+    attn_decode                   rotary embedding, cache append, attention (attn8_decode with an 8-bit cache)
     decode_norm_batch(o)          the product of rmsnorm(attention output, g_attn)
     decode_norm_batch(gate_up)    h'' = h' + o; gate and up (interleaved in one matrix) of rmsnorm(h'', g_post); the
                                   epilogue leaves z = silu(gate) * up * g_ffn and the pieces of sum((silu(gate) * up)^2)
@@ -308,12 +308,18 @@ class DecoderLayer:
 
     def __init__(self, w: LayerWeights, n_heads: int, max_pos: int, h_in: torch.Tensor, h_alt: torch.Tensor,
                  delta_in: Optional[torch.Tensor], pos: torch.Tensor, table: torch.Tensor, eps: float = EPS,
-                 use_workspace=True, fold_norm: Optional[bool] = None):
+                 use_workspace=True, fold_norm: Optional[bool] = None, cache: str = "bf16"):
         dev = h_in.device
         hidden = int(h_in.shape[1])
         ffn = w.proj["down"].K
         assert h_in.shape == (1, hidden) and h_alt.shape == (1, hidden) and hidden % n_heads == 0
         self.w, self.eps, self.delta_in = w, eps, delta_in
+        head_dim = hidden // n_heads
+
+        def attention(q, k, v):
+            if cache == "int8":
+                return Attention8(n_heads, KvCache8(n_heads, head_dim, max_pos, dev), q, k, v, pos, table)
+            return Attention(n_heads, head_dim, max_pos, q, k, v, pos, table)
         self.fold = can_fold_norm(hidden) if fold_norm is None else fold_norm
         self.q4 = ops.alloc_quant(1, ffn, dev)
         self.norm_scratch = torch.empty(B.BL_NORM_SCRATCH_BYTES, dtype=torch.uint8, device=dev)
@@ -322,7 +328,7 @@ class DecoderLayer:
             self.h_out = h_in if h_mid is h_alt else h_alt           # ... and after "h += o"
             self.qkv = NormDecodeGroup([w.proj[n] for n in "qkv"], h_in, w.g_in, eps, delta=delta_in,
                                        h_out=h_mid if delta_in is not None else None, use_workspace=use_workspace)
-            self.attn = Attention(n_heads, hidden // n_heads, max_pos, *self.qkv.outs, pos, table)
+            self.attn = attention(*self.qkv.outs)
             self.o = NormDecodeGroup([w.proj["o"]], self.attn.out, w.g_attn, eps, use_workspace=use_workspace)
             # the gated form: gate and up interleaved in one matrix, silu(gate) * up * g_ffn out of the launch's epilogue,
             # and the down projection quantizes that row as it is (rows short enough to live in registers)
@@ -345,7 +351,7 @@ class DecoderLayer:
             self.h, self.h_out = h_in, h_in                           # separate norm launches update the stream in place
             self.q1, self.q2, self.q3 = (ops.alloc_quant(1, hidden, dev) for _ in range(3))
             self.qkv = ops.GemvGroup([w.proj[n] for n in "qkv"], [self.q1] * 3, use_workspace=use_workspace)
-            self.attn = Attention(n_heads, hidden // n_heads, max_pos, *self.qkv.outs, pos, table)
+            self.attn = attention(*self.qkv.outs)
             self.o = ops.GemvGroup([w.proj["o"]], [self.q2], use_workspace=use_workspace)
             self.gate_up = ops.GemvGroup([w.proj["gate"], w.proj["up"]], [self.q3] * 2, use_workspace=use_workspace)
         if not (self.fold and self.gated):
@@ -379,11 +385,15 @@ class DecoderLayer:
 
 class DecoderStack:
     """n layers, one token per step: h (the residual stream, [1, hidden] fp32) goes in, the final-normalised
-    hidden state comes out; the position lives on the device and advances by one per step."""
+    hidden state comes out; the position lives on the device and advances by one per step.  cache: "bf16", or "int8" for the 8-bit
+    key/value cache (KvCache8: half the bytes, and fork())."""
 
     def __init__(self, layers: List[LayerWeights], g_final: torch.Tensor, n_heads: int, max_pos: int, device,
-                 eps: float = EPS, theta: float = ROPE_THETA, use_workspace=True, fold_norm: Optional[bool] = None):
+                 eps: float = EPS, theta: float = ROPE_THETA, use_workspace=True, fold_norm: Optional[bool] = None, cache: str = "bf16"):
+        if cache not in ("bf16", "int8"):
+            raise ValueError("cache: 'bf16' or 'int8'")
         hidden = layers[0].proj["q"].K
+        self.cache, self.theta, self.use_workspace = cache, theta, use_workspace
         self.hidden, self.n_heads, self.max_pos, self.eps = hidden, n_heads, max_pos, eps
         self.h = torch.zeros((1, hidden), dtype=torch.float32, device=device)       # the caller writes the token's input here
         self.h_alt = torch.zeros((1, hidden), dtype=torch.float32, device=device)
@@ -395,7 +405,7 @@ class DecoderStack:
         delta, h_in = None, self.h
         for w in layers:
             h_alt = self.h_alt if h_in is self.h else self.h
-            layer = DecoderLayer(w, n_heads, max_pos, h_in, h_alt, delta, self.pos, self.table, eps, use_workspace, fold_norm)
+            layer = DecoderLayer(w, n_heads, max_pos, h_in, h_alt, delta, self.pos, self.table, eps, use_workspace, fold_norm, cache)
             self.layers.append(layer)
             delta, h_in = layer.delta_out, layer.h_out
         self.h_last = h_in
@@ -437,7 +447,7 @@ class DecoderStack:
     def prefill(self, x: torch.Tensor) -> torch.Tensor:
         """A prompt (or a piece of one): x [M, hidden] fp32, the inputs of M consecutive tokens starting at the present
         position.  Every product runs as a bl_gemm over the M rows (q, k, v in one launch, gate and up in one), the
-        norms as M-row bl_norm_quant launches, the attention as bl_attn_prefill; eager launches, buffers sized to M on
+        norms as M-row bl_norm_quant launches, the attention as bl_attn_prefill (bl_attn8_prefill); eager launches, buffers sized to M on
         the spot.  Fills the caches, advances the
         position by M and returns the final-normalised hidden states [M, hidden].  The layers must hold gate and up
         as separate matrices (the interleaved one serves the one-token launches only)."""
@@ -449,9 +459,10 @@ class DecoderStack:
         dev, d = x.device, self.hidden // self.n_heads
         new = lambda n: torch.empty((M, n), dtype=torch.float32, device=dev)
         A, Y = new(hidden), new(hidden)
-        # (head sizes on the matrix cores do not touch their 16 bytes: no launch to clear them)
-        alloc = torch.empty if d <= B.BL_ATTN_BLOCK_MAX_HEAD_DIM else torch.zeros
-        scratch = alloc(B.bl_attn_prefill_scratch_bytes(self.n_heads, d, pos0, M), dtype=torch.uint8, device=dev)
+        if self.cache == "bf16":
+            # (head sizes on the matrix cores do not touch their 16 bytes: no launch to clear them)
+            alloc = torch.empty if d <= B.BL_ATTN_BLOCK_MAX_HEAD_DIM else torch.zeros
+            scratch = alloc(B.bl_attn_prefill_scratch_bytes(self.n_heads, d, pos0, M), dtype=torch.uint8, device=dev)
         H = delta = None      # the residual stream, from the first layer's attention on; until then it is x
         for layer in self.layers:
             w = layer.w
@@ -460,9 +471,12 @@ class DecoderStack:
             wide = torch.empty(M * B.BL_NORM_SCRATCH_BYTES, dtype=torch.uint8, device=dev)
             q1 = norm_quant(B.BL_NORM_PLAIN, w.g_in, self.eps, a=x) if H is None else norm_quant(B.BL_NORM_RESIDUAL, w.g_in, self.eps, a=delta, h=H)
             ql, kl, vl = ops.gemm_batch([w.proj[n] for n in "qkv"], q1)
-            B.bl_attn_prefill(ql.data_ptr(), kl.data_ptr(), vl.data_ptr(), self.table.data_ptr(), layer.attn.k_cache.data_ptr(),
-                              layer.attn.v_cache.data_ptr(), A.data_ptr(), scratch.data_ptr(), self.n_heads, d, self.max_pos,
-                              pos0, M, _stream())
+            if self.cache == "int8":
+                attn_prefill8(ql, kl, vl, layer.attn.cache, self.table, pos0, out=A)
+            else:
+                B.bl_attn_prefill(ql.data_ptr(), kl.data_ptr(), vl.data_ptr(), self.table.data_ptr(), layer.attn.k_cache.data_ptr(),
+                                  layer.attn.v_cache.data_ptr(), A.data_ptr(), scratch.data_ptr(), self.n_heads, d, self.max_pos,
+                                  pos0, M, _stream())
             o = ops.gemm(w.proj["o"], norm_quant(B.BL_NORM_PLAIN, w.g_attn, self.eps, a=A))
             H, more = (o, x) if H is None else (H, o)      # x stays as it is: the first sum goes where o was
             q3 = norm_quant(B.BL_NORM_RESIDUAL, w.g_post, self.eps, a=more, h=H)
@@ -472,6 +486,11 @@ class DecoderStack:
         final_norm(H, delta, self.g_final, self.eps, Y, self.pos, pos_set=pos0 + M)
         self._next_pos = pos0 + M
         return Y
+
+    def fork(self, n: int, max_new: int) -> "DecoderFork":
+        """n sequences that continue from the present position, each with room for max_new tokens of its own (cache="int8" only).  The
+        stack's rows are read, not copied, and have to stay: the stack may go on from here, but not be set back."""
+        return DecoderFork(self, n, max_new)
 
     def step(self):
         """One token: self.h holds its input; returns self.y.  Raises once the cache is full (the kernels themselves
@@ -486,8 +505,116 @@ class DecoderStack:
         return self.y
 
 
+class _Products:
+    """The products of the same M quantized rows with up to four matrices in one prepared launch: bl_gemv_batch up to eight rows,
+    bl_gemm_batch beyond."""
+
+    def __init__(self, weights, act: ops.QuantAct, use_workspace):
+        self.M = act.M
+        self.group = ops.GemvGroup(weights, [act] * len(weights), use_workspace=use_workspace) if self.M <= B.BL_MAX_GEMV_M else None
+        if self.group is not None:
+            self.outs = self.group.outs
+            return
+        self._keep = (weights, act)
+        self.outs = [torch.empty((self.M, w.N), dtype=torch.float32, device=act.q.device) for w in weights]
+        self.items = B.make_gemv_items((w.blob.data_ptr(), w.desc, act.q.data_ptr(), act.a_scale.data_ptr(), act.q_sum.data_ptr(), o.data_ptr(), 0)
+                                       for w, o in zip(weights, self.outs))
+
+    def launch(self):
+        if self.group is not None:
+            return self.group.launch()
+        B.bl_gemm_batch(self.items, self.M, _stream())
+        return self.outs
+
+
+class DecoderFork:
+    """n sequences behind a stack's first P positions (a prompt that they share): every step takes one token of each through all layers, with the
+    prompt's keys and values read once for all of them (Attention8).  h [n, hidden] receives the tokens' inputs, step() returns y [n, hidden].
+    Everything is prepared: a step may be captured (capture()).  The layers must hold gate and up as separate matrices."""
+
+    def __init__(self, stack: DecoderStack, n: int, max_new: int):
+        if stack.cache != "int8":
+            raise ValueError("fork() needs a stack with cache='int8'")
+        if n < 1 or max_new < 1:
+            raise ValueError("a fork has at least one sequence and room for one token")
+        dev, hidden, d = stack.h.device, stack.hidden, stack.hidden // stack.n_heads
+        P = stack._next_pos
+        self.stack, self.n, self.max_new, self.prefix_len = stack, n, max_new, P
+        self.h = torch.zeros((n, hidden), dtype=torch.float32, device=dev)
+        self.y = torch.empty((n, hidden), dtype=torch.float32, device=dev)
+        self.pos = torch.full((n,), P, dtype=torch.int32, device=dev)
+        self.live = torch.ones((n,), dtype=torch.int32, device=dev)      # what every step adds to pos
+        self.table = rope_table(d, P + max_new, dev, stack.theta)
+        self.q1, self.q2, self.q3 = (ops.alloc_quant(n, hidden, dev) for _ in range(3))
+        self.attn_out = torch.zeros((n, hidden), dtype=torch.float32, device=dev)   # (a stopped sequence's row is never written)
+        self.layers = []
+        ws = stack.use_workspace
+        for layer in stack.layers:
+            w = layer.w
+            assert "gate" in w.proj and "up" in w.proj, "a fork needs gate and up as separate matrices"
+            qkv = _Products([w.proj[k] for k in "qkv"], self.q1, ws)
+            attn = Attention8(stack.n_heads, KvCache8(stack.n_heads, d, max_new, dev, sequences=n), *qkv.outs, self.pos, self.table,
+                              prefix=layer.attn.cache if P else None, prefix_len=P, out=self.attn_out)
+            ffn = w.proj["down"].K
+            q4 = ops.alloc_quant(n, ffn, dev)
+            wide = torch.empty(n * B.BL_NORM_SCRATCH_BYTES, dtype=torch.uint8, device=dev)
+            self.layers.append((w, qkv, attn, _Products([w.proj["o"]], self.q2, ws), _Products([w.proj["gate"], w.proj["up"]], self.q3, ws), q4, wide,
+                                _Products([w.proj["down"]], q4, ws)))
+        self.steps, self.graph = 0, None
+
+    def stop(self, sequence: int):
+        """The sequence takes no part from now on: nothing of it is read or written, its row of y means nothing."""
+        self.live[sequence] = 0
+        self.pos[sequence] = -1
+
+    def launch(self):
+        """All launches of one step on the current stream."""
+        eps, delta = self.stack.eps, None
+        for w, qkv, attn, o, gate_up, q4, wide, down in self.layers:
+            norm_quant(B.BL_NORM_RESIDUAL, w.g_in, eps, a=delta, h=self.h, out=self.q1)
+            qkv.launch()
+            attn.launch()
+            norm_quant(B.BL_NORM_PLAIN, w.g_attn, eps, a=self.attn_out, out=self.q2)
+            o.launch()
+            norm_quant(B.BL_NORM_RESIDUAL, w.g_post, eps, a=o.outs[0], h=self.h, out=self.q3)
+            gate_up.launch()
+            norm_quant(B.BL_NORM_GATED, w.g_ffn, eps, a=gate_up.outs[0], b=gate_up.outs[1], out=q4, scratch=wide)
+            down.launch()
+            delta = down.outs[0]
+        norm_quant(B.BL_NORM_RESIDUAL, self.stack.g_final, eps, a=delta, h=self.h, y=self.y, quantize=False)
+        self.pos.add_(self.live)
+        return self.y
+
+    def capture(self):
+        """Capture launch() into a HIP graph.  One step is run first and undone (its cache rows are rewritten by the first real one)."""
+        h0, pos0 = self.h.clone(), self.pos.clone()
+        self.launch()
+        torch.cuda.synchronize()
+        self.h.copy_(h0)
+        self.pos.copy_(pos0)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(s):
+            with torch.cuda.graph(self.graph, stream=s):
+                self.launch()
+        torch.cuda.current_stream().wait_stream(s)
+        return self.graph
+
+    def step(self):
+        """One token of every sequence that has not been stopped: self.h holds their inputs; returns self.y."""
+        if self.steps >= self.max_new:
+            raise RuntimeError("the sequences' caches hold %d positions and are full" % self.max_new)
+        self.steps += 1
+        if self.graph is not None:
+            self.graph.replay()
+        else:
+            self.launch()
+        return self.y
+
+
 def make_stack(name: str, max_pos: int, device, config: int = 7, n_layers: Optional[int] = None,
-               use_workspace=True, gated: bool = True) -> DecoderStack:
+               use_workspace=True, gated: bool = True, cache: str = "bf16") -> DecoderStack:
     """A dummy model of Appendix A's shape `name` (as in the paper: random ternary weights, drawn on the device from
     the seed rule of synth.seed_for), norm weights uniform in [0.5, 1.5]."""
     from . import synth
@@ -516,4 +643,4 @@ def make_stack(name: str, max_pos: int, device, config: int = 7, n_layers: Optio
         ws.append(LayerWeights(proj, *gam, s_up=s_up))
     g.manual_seed(synth.seed_for(config, n_layers, 8))
     return DecoderStack(ws, torch.rand(hidden, device=device, generator=g) + 0.5, synth.PAPER_HEADS[name], max_pos, device,
-                        use_workspace=use_workspace)
+                        use_workspace=use_workspace, cache=cache)
