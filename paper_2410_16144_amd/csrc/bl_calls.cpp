@@ -291,6 +291,119 @@ PyObject* final_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// The 8-bit cache: `cache` is the bl_kv8_cache, `codes` a tensor of it.  Everything is where the launch goes: on the current stream's device.
+struct Cache8 {
+    Memory memory;
+    const at::Tensor* codes;
+    void* stream;
+    bool ok;
+    Cache8(PyObject* cache, PyObject* tensor) : memory(cache, sizeof(bl_kv8_cache)), codes(plain(tensor)) {
+        const c10::hip::HIPStream now = c10::hip::getCurrentHIPStream();
+        stream = now.stream();
+        ok = memory.ok && codes && codes->get_device() == now.device_index();
+    }
+    const bl_kv8_cache& c() const { return *memory.as<const bl_kv8_cache>(); }
+    int64_t hidden() const { return (int64_t)c().n_heads * c().head_dim; }
+    bool here(const at::Tensor* t) const { return t && t->get_device() == codes->get_device(); }
+    // a rotary table that reaches position `end`
+    const at::Tensor* table(PyObject* o, int64_t end) const {
+        const at::Tensor* t = plain(o, at::kFloat);
+        return here(t) && t->dim() == 3 && t->size(0) >= end && t->size(1) == c().head_dim / 2 && t->size(2) == 2 ? t : nullptr;
+    }
+    bool in_range(int64_t pos0, int64_t M) const { return pos0 >= 0 && M >= 1 && pos0 + M <= c().max_pos; }
+};
+
+// kv8_write(cache, codes, k, v, pos0, table or None, sequence) -> True
+PyObject* kv8_write(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    BL_NEEDS(7)
+    const long pos0 = PyLong_AsLong(args[4]), sequence = PyLong_AsLong(args[6]);
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    const Cache8 cache(args[0], args[1]);
+    const at::Tensor *k = plain(args[2]), *v = plain(args[3]), *table = nullptr;
+    if (!cache.ok || !cache.here(k) || !cache.here(v) || k->dim() != 2 || k->sizes() != v->sizes() || k->scalar_type() != v->scalar_type()) Py_RETURN_NONE;
+    const int64_t M = k->size(0), hidden = cache.hidden(), ld = M > 1 ? k->stride(0) : hidden;
+    if (!cache.in_range(pos0, M) || sequence < 0 || sequence >= cache.c().sequences || k->size(1) != hidden || k->stride(1) != 1 || v->stride(1) != 1 ||
+        (M > 1 && (v->stride(0) != ld || ld < hidden)))
+        Py_RETURN_NONE;
+    if (k->scalar_type() != at::kFloat && k->scalar_type() != at::kBFloat16) Py_RETURN_NONE;
+    if (args[5] != Py_None && !(table = cache.table(args[5], pos0 + M))) Py_RETURN_NONE;
+    const bl_kv8_write_args p{&cache.c(), k->data_ptr(), v->data_ptr(), table ? static_cast<const float*>(table->data_ptr()) : nullptr, ld,
+                              k->scalar_type() == at::kFloat ? BL_F32 : BL_BF16, (int32_t)sequence, (int32_t)pos0, (int32_t)M};
+    bl_status status;
+    {
+        WithoutGil release;
+        status = bl_kv8_write(&p, cache.stream);
+    }
+    if (status != BL_OK) return PyLong_FromLong(status);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv8_read(cache, codes, pos0, M, bf16, sequence) -> (k, v)
+PyObject* kv8_read(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    BL_NEEDS(6)
+    const long pos0 = PyLong_AsLong(args[2]), M = PyLong_AsLong(args[3]), sequence = PyLong_AsLong(args[5]);
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    const Cache8 cache(args[0], args[1]);
+    if (!cache.ok || !cache.in_range(pos0, M) || sequence < 0 || sequence >= cache.c().sequences) Py_RETURN_NONE;
+    const bool bf16 = args[4] == Py_True;
+    at::Tensor out[2];
+    for (at::Tensor& t : out) t = fresh({M, cache.hidden()}, bf16 ? at::kBFloat16 : at::kFloat, *cache.codes);
+    const bl_kv8_read_args p{&cache.c(), out[0].data_ptr(), out[1].data_ptr(), cache.hidden(), bf16 ? BL_BF16 : BL_F32, (int32_t)sequence, (int32_t)pos0,
+                             (int32_t)M};
+    bl_status status;
+    {
+        WithoutGil release;
+        status = bl_kv8_read(&p, cache.stream);
+    }
+    if (status != BL_OK) return PyLong_FromLong(status);
+    PyObject* r = PyTuple_New(2);
+    if (!r) return nullptr;
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(out[i]));
+    return r;
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_prefill8(cache, codes, q, k, v, table, pos0, sequence, out or None) -> out
+PyObject* attn_prefill8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    BL_NEEDS(9)
+    const long pos0 = PyLong_AsLong(args[6]), sequence = PyLong_AsLong(args[7]);
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    const Cache8 cache(args[0], args[1]);
+    if (!cache.ok) Py_RETURN_NONE;
+    const at::Tensor *q = plain(args[2], at::kFloat), *k = plain(args[3], at::kFloat), *v = plain(args[4], at::kFloat);
+    if (!cache.here(q) || !cache.here(k) || !cache.here(v) || q->dim() != 2 || k->dim() != 2 || k->sizes() != v->sizes()) Py_RETURN_NONE;
+    const int64_t M = q->size(0), d = cache.c().head_dim, n_heads = q->size(1) / d;
+    if (!cache.in_range(pos0, M) || sequence < 0 || sequence >= cache.c().sequences || q->size(1) != n_heads * d || n_heads > INT32_MAX || k->size(0) != M ||
+        k->size(1) != cache.hidden())
+        Py_RETURN_NONE;
+    const at::Tensor* table = cache.table(args[5], pos0 + M);
+    const uint64_t bytes = bl_attn8_prefill_scratch_bytes((int32_t)n_heads, cache.c().n_heads, (int32_t)d, (int32_t)pos0, (int32_t)M);
+    if (!table || bytes == 0) Py_RETURN_NONE;
+    at::Tensor out;
+    if (args[8] == Py_None) {
+        out = fresh({M, n_heads * d}, at::kFloat, *q);
+    } else {
+        const at::Tensor* given = plain(args[8], at::kFloat);
+        if (!cache.here(given) || given->sizes() != q->sizes()) Py_RETURN_NONE;
+        out = *given;
+    }
+    const at::Tensor scratch = fresh({(int64_t)bytes}, at::kByte, *q);
+    const bl_attn8_prefill_args p{static_cast<const float*>(q->data_ptr()), static_cast<const float*>(k->data_ptr()), static_cast<const float*>(v->data_ptr()),
+                                  static_cast<const float*>(table->data_ptr()), static_cast<float*>(out.data_ptr()), scratch.data_ptr(), cache.c(),
+                                  (int32_t)n_heads, (int32_t)sequence, (int32_t)pos0, (int32_t)M};
+    bl_status status;
+    {
+        WithoutGil release;
+        status = bl_attn8_prefill(&p, cache.stream);
+    }
+    return status == BL_OK ? THPVariable_Wrap(out) : PyLong_FromLong(status);
+    END_HANDLE_TH_ERRORS
+}
+
 // The prepared launches: launch(which, items, M, workspace) -> bl_status, on the current stream; None if `items`, a ctypes array (for
 // the last two the argument struct), does not hold whole ones of that launch's.
 enum { kGemvBatch, kDecodeBatch, kQuantBatch, kDecodeNormBatch, kTl2Batch, kAttnDecode, kAttn8Decode, kLaunches };
@@ -332,7 +445,8 @@ PyObject* stream(PyObject*, PyObject*) {
 }
 
 #define BL_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {BL_FAST(quant_act), BL_FAST(product), BL_FAST(gemm_batch), BL_FAST(norm_quant), BL_FAST(final_norm), BL_FAST(launch),
+PyMethodDef methods[] = {BL_FAST(quant_act), BL_FAST(product), BL_FAST(gemm_batch), BL_FAST(norm_quant), BL_FAST(final_norm), BL_FAST(kv8_write), BL_FAST(kv8_read),
+                         BL_FAST(attn_prefill8), BL_FAST(launch),
                          {"stream", stream, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

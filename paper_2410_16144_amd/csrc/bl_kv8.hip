@@ -2,8 +2,10 @@
 //
 // One workgroup per (chunk of 64 positions, key head, keys or values).  A write is a stream of projections in and a quarter of their bytes
 // (half, from bf16) out: every row's largest value stays in the registers of the lanes that hold the row -- one read -- and the
-// codes are put into the cache's order in LDS, since a value's neighbours in memory are the same dim's of other positions.  A chunk that the
-// call covers in part is written row by row (keys) and byte by byte (values): the bytes between belong to other positions.
+// codes are put into the cache's order in LDS, since a value's neighbours in memory are the same dim's of other positions.  Four rows
+// are a thread's, so that both orders are written and read by words (2000 bf16 rows, 32 heads of 128, written and read back, 49 MB each way: byte
+// by byte 31.5 us, by words 24.6; copying as many bytes at the card's 5.2 TB/s: 19).  A chunk that the call covers in part is written row
+// by row (keys) and byte by byte (values): the bytes between belong to other positions.
 #include "bl_kv8.hpp"
 #include "bl_lanes.hpp"
 
@@ -12,7 +14,11 @@ namespace bl {
 namespace {
 
 constexpr int kKv8Threads = 256;
-constexpr int kValuePitch = 64 + 16;   // bytes of a dim's positions in LDS: the dims of a write spread over the banks
+// A chunk's values in LDS: the 64 positions of a dim, 80 bytes on from the next dim's, its four pieces of 16 moved about by the dim.  Sixteen
+// lanes with a word of every fourth dim then meet sixteen banks (of four positions beside each other: all 64), and a piece stays whole.
+constexpr int kValuePitch = 64 + 16;
+__device__ __forceinline__ int value_piece(int dim, int piece) { return dim * kValuePitch + (piece ^ (dim >> 4 & 3)) * 16; }
+__device__ __forceinline__ int value_word(int dim, int quad) { return value_piece(dim, quad >> 2) + (quad & 3) * 4; }   // positions 4 quad ..
 
 struct WriteArgs {
     Kv8           cache;
@@ -34,11 +40,15 @@ __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // L lanes share a row, each with V elements of the head's lower half and their partners in the upper half (V divides half the head
-// size, V L reaches it).  All rows of a thread are requested before the first is used.
+// size, V L reaches it), of at least four rows in order: a dim's codes of four positions are a word.  All rows of a thread are requested before
+// the first is used.
+template <int L> constexpr int kWriteThreads = 16 * L < kKv8Threads ? 16 * L : kKv8Threads;
+
 template <bool BF16, int V, int L>
-__global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const WriteArgs p) {
+__global__ __launch_bounds__(kWriteThreads<L>) void kv8_write_kernel(const WriteArgs p) {
     typedef typename RowVec<BF16, V>::type vec_t;
-    constexpr int kRows = kKv8Threads / L, kTurns = kKv8Chunk / kRows;
+    constexpr int kThreads = kWriteThreads<L>, kTurns = kKv8Chunk / (kThreads / L);
+    static_assert(kTurns % 4 == 0, "rows in fours");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int tid = threadIdx.x, l = tid % L, d = p.head_dim, half = d >> 1, size = p.size;
     const int head = blockIdx.y, chunk = p.pos0 / kKv8Chunk + (int)blockIdx.x, first = chunk * kKv8Chunk;
@@ -46,10 +56,10 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const WriteArgs 
     const int lo = max(p.pos0, first), hi = min(p.pos0 + p.M, first + kKv8Chunk);   // rows of this workgroup
     if (p.clear) {
         const int64_t wgs = (int64_t)gridDim.x * gridDim.y * gridDim.z;
-        for (int64_t i = ((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * kKv8Threads + tid; i < p.clear_count; i += wgs * kKv8Threads)
+        for (int64_t i = ((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * kThreads + tid; i < p.clear_count; i += wgs * kThreads)
             p.clear[i] = 0;
     }
-    const int at = l * V;
+    const int at = l * V, r0 = tid / L * kTurns;
     const bool mine = at < half;
     vec_t a[kTurns], b[kTurns];
     typedef float pair_t __attribute__((ext_vector_type(2 * V), aligned(8)));   // V pairs (cosine, sine)
@@ -58,60 +68,69 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const WriteArgs 
     const auto* x = static_cast<const typename std::conditional<BF16, uint16_t, float>::type*>(p.x[value]);
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
-        const int row = min(max(first + tid / L + t * kRows, lo), hi - 1), e = mine ? at : 0;   // (any row of the call where there is none)
+        const int row = min(max(first + r0 + t, lo), hi - 1), e = mine ? at : 0;   // (any row of the call where there is none)
         const auto* src = x + (int64_t)(row - p.pos0) * p.ld + head * d + e;
         a[t] = *reinterpret_cast<const vec_t*>(src);
         b[t] = *reinterpret_cast<const vec_t*>(src + half);
         if (rotate) cs[t] = *reinterpret_cast<const pair_t*>(p.rope + (int64_t)row * half + e);
     }
 #pragma unroll
-    for (int t = 0; t < kTurns; ++t) {
-        const int row = first + tid / L + t * kRows, r = row - first;
-        float u[V], w[V], amax = 0.0f;
+    for (int t4 = 0; t4 < kTurns; t4 += 4) {
+        uint32_t words[2][V] = {};   // of four positions
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            u[i] = widen(a[t][i]);
-            w[i] = widen(b[t][i]);
-            if (rotate) {   // each operation rounded on its own (the library is compiled without contraction)
-                const float c = cs[t][2 * i], s = cs[t][2 * i + 1], f = u[i], g = w[i];
-                u[i] = f * c - g * s;
-                w[i] = f * s + g * c;
-            }
-            if (mine) amax = fmaxf(amax, fmaxf(fabsf(u[i]), fabsf(w[i])));
-        }
+        for (int j = 0; j < 4; ++j) {
+            const int t = t4 + j, r = r0 + t, row = first + r;
+            float u[V], w[V], amax = 0.0f;
 #pragma unroll
-        for (int o = 1; o < L; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-        float inv, scale;
-        kv8_scales(amax, inv, scale);
-        if (row >= lo && row < hi) {
-            if (l == 0) (value ? p.cache.v_scale : p.cache.k_scale)[head * p.cache.head_scales + row] = scale;
-            if (mine) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const uint8_t cu = (uint8_t)kv8_code(u[i], inv), cw = (uint8_t)kv8_code(w[i], inv);
-                    if (value) {
-                        lds[(at + i) * kValuePitch + r] = cu;
-                        lds[(half + at + i) * kValuePitch + r] = cw;
-                    } else {
-                        const int base = kv8_key_row(r) * (size + 16) + at + i;
-                        lds[base] = cu;
-                        lds[base + half] = cw;
-                    }
+            for (int i = 0; i < V; ++i) {
+                u[i] = widen(a[t][i]);
+                w[i] = widen(b[t][i]);
+                if (rotate) {   // each operation rounded on its own (the library is compiled without contraction)
+                    const float c = cs[t][2 * i], s = cs[t][2 * i + 1], f = u[i], g = w[i];
+                    u[i] = f * c - g * s;
+                    w[i] = f * s + g * c;
                 }
+                if (mine) amax = fmaxf(amax, fmaxf(fabsf(u[i]), fabsf(w[i])));
+            }
+            amax = over_lanes<L>(amax, MaxOp());
+            float inv, scale;
+            kv8_scales(amax, inv, scale);
+            if (l == 0 && row >= lo && row < hi) (value ? p.cache.v_scale : p.cache.k_scale)[head * p.cache.head_scales + row] = scale;
+            uint32_t row_u = 0, row_w = 0;   // a key row's bytes side by side
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t cu = (uint8_t)kv8_code(u[i], inv), cw = (uint8_t)kv8_code(w[i], inv);
+                row_u |= cu << 8 * i;
+                row_w |= cw << 8 * i;
+                words[0][i] |= cu << 8 * j;
+                words[1][i] |= cw << 8 * j;
+            }
+            if (!value && mine) {
+                typedef typename std::conditional<V == 4, uint32_t, uint16_t>::type part_t;
+                uint8_t* to = lds + kv8_key_row(r) * (size + 16) + at;
+                *reinterpret_cast<part_t*>(to) = (part_t)row_u;
+                *reinterpret_cast<part_t*>(to + half) = (part_t)row_w;   // (V divides half the head size)
+            }
+        }
+        if (value && mine) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                *reinterpret_cast<uint32_t*>(lds + value_word(at + i, (r0 + t4) >> 2)) = words[0][i];
+                *reinterpret_cast<uint32_t*>(lds + value_word(half + at + i, (r0 + t4) >> 2)) = words[1][i];
             }
         }
     }
     __syncthreads();
     int8_t* dst = (value ? p.cache.v : p.cache.k) + head * p.cache.head_bytes + (int64_t)chunk * kKv8Chunk * size;
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    for (int piece = tid; piece < 4 * size; piece += kKv8Threads) {   // of 16 bytes
+    for (int piece = tid; piece < 4 * size; piece += kThreads) {   // of 16 bytes
         if (value) {
-            const int e = piece >> 2, r = (piece & 3) * 16;
-            const u32x4 codes = e < d ? *reinterpret_cast<const u32x4*>(lds + e * kValuePitch + r) : u32x4{0, 0, 0, 0};
+            const int e = piece >> 2, r = (piece & 3) * 16, from = value_piece(e, piece & 3);
+            const u32x4 codes = e < d ? *reinterpret_cast<const u32x4*>(lds + from) : u32x4{0, 0, 0, 0};
             if (first + r >= lo && first + r + 16 <= hi) *reinterpret_cast<u32x4*>(dst + e * 64 + r) = codes;
             else
                 for (int i = 0; i < 16; ++i)
-                    if (first + r + i >= lo && first + r + i < hi) dst[e * 64 + r + i] = (int8_t)(e < d ? lds[e * kValuePitch + r + i] : 0);
+                    if (first + r + i >= lo && first + r + i < hi) dst[e * 64 + r + i] = (int8_t)(e < d ? lds[from + i] : 0);
         } else {
             const int off = piece * 16, block = off >> 12, width = min(64, size - 64 * block), in = off & 4095;
             const int row = in / width, e = 64 * block + in % width, r = 4 * (row & 15) + (row >> 4);
@@ -147,31 +166,46 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_read_kernel(const ReadArgs p)
         const u32x4 codes = *reinterpret_cast<const u32x4*>(src + piece * 16);
         const int off = piece * 16;
         if (value) {
-            *reinterpret_cast<u32x4*>(lds + (piece >> 2) * kValuePitch + (piece & 3) * 16) = codes;
+            *reinterpret_cast<u32x4*>(lds + value_piece(piece >> 2, piece & 3)) = codes;
         } else {
             const int block = off >> 12, width = min(64, size - 64 * block), in = off & 4095;
             *reinterpret_cast<u32x4*>(lds + in / width * (size + 16) + 64 * block + in % width) = codes;
         }
     }
     __syncthreads();
-    const int quads = d >> 2;
-    for (int i = tid; i < (hi - lo) * quads; i += kKv8Threads) {
-        const int row = lo + i / quads, e = 4 * (i % quads), r = row - first;
-        const float scale = scales[row];
-        float x[4];
+    // four positions by four dims at a time: words of the keys are rows', of the values dims'
+    const int quads = d >> 2, group0 = (lo - first) >> 2, groups = ((hi - 1 - first) >> 2) - group0 + 1;
+    for (int i = tid; i < groups * quads; i += kKv8Threads) {
+        const int group = group0 + i / quads, e = 4 * (i % quads);
+        uint32_t words[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            words[j] = *reinterpret_cast<const uint32_t*>(lds + (value ? value_word(e + j, group) : kv8_key_row(4 * group + j) * (size + 16) + e));
+        if (value) {
+            const uint32_t a = __builtin_amdgcn_perm(words[1], words[0], 0x05010400u), b = __builtin_amdgcn_perm(words[3], words[2], 0x05010400u);
+            const uint32_t c = __builtin_amdgcn_perm(words[1], words[0], 0x07030602u), f = __builtin_amdgcn_perm(words[3], words[2], 0x07030602u);
+            words[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+            words[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            words[2] = __builtin_amdgcn_perm(f, c, 0x05040100u);
+            words[3] = __builtin_amdgcn_perm(f, c, 0x07060302u);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int8_t code = (int8_t)(value ? lds[(e + j) * kValuePitch + r] : lds[kv8_key_row(r) * (size + 16) + e + j]);
-            x[j] = (float)code * scale;
-        }
-        const int64_t at = (int64_t)(row - p.pos0) * p.ld + head * d + e;
-        if constexpr (BF16) {
-            typedef __bf16 b4 __attribute__((ext_vector_type(4), aligned(2)));
-            typedef float f4 __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<b4*>(static_cast<__bf16*>(p.out[value]) + at) = __builtin_convertvector((f4{x[0], x[1], x[2], x[3]}), b4);
-        } else {
-            typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-            *reinterpret_cast<f4*>(static_cast<float*>(p.out[value]) + at) = f4{x[0], x[1], x[2], x[3]};
+            const int row = first + 4 * group + j;
+            if (row < lo || row >= hi) continue;
+            const float scale = scales[row];
+            float x[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) x[n] = (float)(int8_t)(words[j] >> 8 * n) * scale;
+            const int64_t at = (int64_t)(row - p.pos0) * p.ld + head * d + e;
+            if constexpr (BF16) {
+                typedef __bf16 b4 __attribute__((ext_vector_type(4), aligned(2)));
+                typedef float f4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<b4*>(static_cast<__bf16*>(p.out[value]) + at) = __builtin_convertvector((f4{x[0], x[1], x[2], x[3]}), b4);
+            } else {
+                typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+                *reinterpret_cast<f4*>(static_cast<float*>(p.out[value]) + at) = f4{x[0], x[1], x[2], x[3]};
+            }
         }
     }
 }
@@ -185,7 +219,7 @@ dim3 chunk_grid(int pos0, int M, int n_heads, int sides) {
 
 template <bool BF16, int V, int L>
 hipError_t launch_write(const WriteArgs& p, hipStream_t s) {
-    kv8_write_kernel<BF16, V, L><<<chunk_grid(p.pos0, p.M, p.n_heads, 2), dim3(kKv8Threads), lds_bytes(p.size), s>>>(p);
+    kv8_write_kernel<BF16, V, L><<<chunk_grid(p.pos0, p.M, p.n_heads, 2), dim3(kWriteThreads<L>), lds_bytes(p.size), s>>>(p);
     return hipGetLastError();
 }
 

@@ -5,7 +5,7 @@
 
 namespace bl {
 
-// Sum or maximum over groups of L neighbouring lanes (16, 32 or 64), on the vector ALU's lane moves instead of a trip through LDS per
+// Sum or maximum over groups of L neighbouring lanes (8 to 64), on the vector ALU's lane moves instead of a trip through LDS per
 // step (ds_bpermute): lane ^ 1 and ^ 2 by quad permutation, the other half of eight and of sixteen lanes by their mirror images -- whose
 // lanes all hold their quad's or half's result by then -- and the 16- and 32-lane blocks by the swaps of two registers.  Every step
 // adds the two halves' figures (in either order the same bits), so every lane gets the same result.
@@ -24,11 +24,11 @@ __device__ __forceinline__ float over_blocks(float v, Op op) {   // lane and lan
 }
 template <int L, typename Op>
 __device__ __forceinline__ float over_lanes(float v, Op op) {
-    static_assert(L == 16 || L == 32 || L == 64, "whole rows of sixteen lanes");
+    static_assert(L == 8 || L == 16 || L == 32 || L == 64, "half a row of sixteen lanes, or whole ones");
     v = op(v, BL_LANES(v, 0xb1));    // quad_perm [1, 0, 3, 2]
     v = op(v, BL_LANES(v, 0x4e));    // quad_perm [2, 3, 0, 1]
     v = op(v, BL_LANES(v, 0x141));   // row_half_mirror
-    v = op(v, BL_LANES(v, 0x140));   // row_mirror
+    if constexpr (L >= 16) v = op(v, BL_LANES(v, 0x140));   // row_mirror
     if constexpr (L >= 32) v = over_blocks<16>(v, op);
     if constexpr (L >= 64) v = over_blocks<32>(v, op);
     return v;

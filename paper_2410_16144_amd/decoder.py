@@ -151,6 +151,12 @@ class KvCache8:
     def write(self, k: torch.Tensor, v: torch.Tensor, pos0: int, table: Optional[torch.Tensor] = None, sequence: int = 0):
         """Rows k, v ([M, n_heads * head_dim] fp32 or bf16; rows may lie apart) into positions pos0 .. pos0 + M - 1.  table: the
         rotary table by which the keys are rotated first (position p by its row p); None: they are rotated already."""
+        c = B.calls()
+        r = c.kv8_write(self.args, self.k_codes, k, v, pos0, table, sequence) if c else None
+        if r:
+            if type(r) is int:
+                raise B.BitLinearError(r, "bl_kv8_write")
+            return
         self._here(k, v, table)
         M = int(k.shape[0])
         assert k.dim() == 2 and k.shape == v.shape == (M, self.hidden) and k.dtype == v.dtype
@@ -164,8 +170,14 @@ class KvCache8:
 
     def read(self, pos0: int, M: int, dtype: torch.dtype = torch.float32, sequence: int = 0):
         """(keys, values) that positions pos0 .. pos0 + M - 1 stand for, [M, n_heads * head_dim]; keys as stored, rotated."""
+        c = B.calls()
+        r = c.kv8_read(self.args, self.k_codes, pos0, M, dtype == torch.bfloat16, sequence) if c and dtype in (torch.float32, torch.bfloat16) else None
+        if r:
+            if type(r) is int:
+                raise B.BitLinearError(r, "bl_kv8_read")
+            return r
         self._here()
-        k, v = (torch.empty((max(M, 0), self.hidden), dtype=dtype, device=self.k_codes.device) for _ in range(2))
+        k, v = (torch.empty((min(max(M, 0), self.max_pos), self.hidden), dtype=dtype, device=self.k_codes.device) for _ in range(2))
         B.bl_kv8_read(self.args, k.data_ptr(), v.data_ptr(), self.hidden, ops._dtype_code(k), sequence, pos0, M, _stream())
         return k, v
 
@@ -204,6 +216,12 @@ def attn_prefill8(q_lin: torch.Tensor, k_lin: torch.Tensor, v_lin: torch.Tensor,
                   sequence: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """bl_attn8_prefill: M consecutive tokens of one sequence at positions pos0 .. -- their rows into the cache, then token m's attention over
     rows 0 .. pos0 + m.  q_lin [M, n_heads * head_dim], k_lin, v_lin [M, cache.n_heads * head_dim] fp32; returns [M, n_heads * head_dim]."""
+    c = B.calls()
+    r = c.attn_prefill8(cache.args, cache.k_codes, q_lin, k_lin, v_lin, table, pos0, sequence, out) if c else None
+    if r is not None:
+        if type(r) is int:
+            raise B.BitLinearError(r, "bl_attn8_prefill")
+        return r
     cache._here(q_lin, k_lin, v_lin, table, out)
     M, d = int(q_lin.shape[0]), cache.head_dim
     n_heads = int(q_lin.shape[1]) // d

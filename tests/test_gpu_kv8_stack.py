@@ -278,3 +278,50 @@ def test_a_captured_prompt(dev, mods):
             torch.cuda.synchronize()
             assert torch.equal(out, want)
             torch.randn(500, 500, device=dev).sum().item()
+
+
+def test_native_calls_are_the_ctypes_ones(dev, mods, monkeypatch):
+    """write, read and attn_prefill8 in native code beside the Python path that they stand in for: the same bits, and for what they do not
+    take as it is the same result or the same refusal."""
+    B, dec, ops = mods
+    assert B.calls()
+    r = T._rng(85000)
+    n, dim, M = 2, 96, 40
+    wide = T._t(_rows(r, M, 2 * n * dim), dev)
+    k, v, q = (T._t(_rows(r, M, w * n * dim), dev) for w in (1, 1, 3))
+    table = T._t(_table(dim, 100), dev)
+    half = wide.half()
+
+    def outcomes():
+        cache = dec.KvCache8(n, dim, 90, dev, sequences=2)
+        calls = [
+            lambda: cache.write(k, v, 3, table), lambda: cache.write(k.bfloat16(), v.bfloat16(), 50, sequence=1),
+            lambda: cache.write(wide[:, :n * dim], wide[:, n * dim:], 47, table), lambda: cache.write(k[:1], v[:1], 89, table),
+            lambda: cache.write(k, v, 51, table), lambda: cache.write(k, v, 0, table[:39]), lambda: cache.write(half[:, :n * dim], half[:, n * dim:], 0),
+            lambda: cache.write(k, v, 0, table, 2), lambda: cache.write(k, v[:, :96], 0), lambda: cache.write(k[:0], v[:0], 0), lambda: cache.write(k, v.cpu(), 0),
+            lambda: cache.write(k, v.bfloat16(), 0),
+            lambda: cache.read(0, 90), lambda: cache.read(33, 50, torch.bfloat16, 1), lambda: cache.read(0, 91), lambda: cache.read(-1, 2), lambda: cache.read(0, 2, sequence=2),
+            lambda: cache.read(0, 10 ** 9), lambda: cache.read(0, 4, torch.float16),
+            lambda: dec.attn_prefill8(q, k, v, cache, table, 20), lambda: dec.attn_prefill8(q, k, v, cache, table, 50, 1, torch.zeros_like(q)),
+            lambda: dec.attn_prefill8(q, k, v, cache, table, 51), lambda: dec.attn_prefill8(q[:, :96].contiguous(), k, v, cache, table, 0),
+            lambda: dec.attn_prefill8(q[:, :100].contiguous(), k, v, cache, table, 0), lambda: dec.attn_prefill8(q, k[:39], v[:39], cache, table, 0),
+            lambda: dec.attn_prefill8(q, k, v, cache, table[:59], 20), lambda: dec.attn_prefill8(q, k, v, cache, table, 0, 2),
+            lambda: dec.attn_prefill8(q, k, v, cache, table, 0, 0, q[:39]), lambda: dec.attn_prefill8(q[:0], k[:0], v[:0], cache, table, 0)]
+        got = []
+        for call in calls:
+            try:
+                out = call()
+                torch.cuda.synchronize()
+                out = [t.clone() for t in (out if isinstance(out, tuple) else (out,)) if t is not None]
+                got.append([t.cpu() for t in out + [cache.k_codes, cache.v_codes, cache.k_scale, cache.v_scale]])
+            except Exception as e:      # noqa: BLE001 -- the kind and the words are what is compared
+                got.append((type(e).__name__, str(e)))
+        return got
+
+    native = outcomes()
+    monkeypatch.setattr(B, "_calls", False)
+    for i, (a, b) in enumerate(zip(native, outcomes(), strict=True)):
+        assert type(a) is type(b), (i, a, b)
+        assert a == b if isinstance(a, tuple) else all(x.dtype == y.dtype and torch.equal(x, y) for x, y in zip(a, b, strict=True)), i
+    refused = [isinstance(a, tuple) for a in native]
+    assert refused == [False] * 4 + [True] * 8 + [False] * 2 + [True] * 5 + [False] * 2 + [True] * 8     # (one query head does not share out over two key heads)
