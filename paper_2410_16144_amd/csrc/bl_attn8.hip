@@ -2,7 +2,7 @@
 //
 // One token of each of several sequences, each behind a prefix that they share; a prompt's tokens behind a cache.  A launch has a shared part --
 // all tokens' rows against the prefix, or a prompt's cache -- and an own part, each sequence's rows against its own cache; the workgroups of a row
-// meet in scratch memory (attn8_finish).  The rows form (bl_attn8_rows.hpp) takes up to four shared rows and all own ones, the tiles form
+// meet in scratch memory (attn8_finish).  The rows form (bl_attn8_rows.hpp) takes up to eight shared rows and all own ones, the tiles form
 // (bl_attn8_tiles.hpp) more shared ones; both parts are in one launch.
 #include "bl_attn8_rows.hpp"
 
@@ -35,8 +35,13 @@ hipError_t launch_form(const Attn8Args& p, int wgs, hipStream_t s) {
 template <int KB>
 hipError_t launch_block(const Attn8Args& p, const Attn8Plan& plan, bool stream, int wgs, hipStream_t s) {
     static_assert(kRows8Waves == 8 && kRows8ManyWaves == 2 && kRows8FewWaves == 4, "waves as planned");
-    if (plan.block == 8) return launch_form<KB, 2, 4, true>(p, wgs, s);
-    if (plan.block == 16) return launch_form<KB, 4, 4, true>(p, wgs, s);
+    if (plan.block == 8) return plan.waves == 8 ? launch_form<KB, 2, 8, true>(p, wgs, s) : launch_form<KB, 2, 4, true>(p, wgs, s);
+    if (plan.block == 16) {
+        if constexpr (KB <= 2) {
+            if (plan.waves == 8) return launch_form<KB, 4, 8, true>(p, wgs, s);
+        }
+        return launch_form<KB, 4, 4, true>(p, wgs, s);
+    }
     if (plan.waves == 8) return stream ? launch_form<KB, 1, 8, true>(p, wgs, s) : launch_form<KB, 1, 8, false>(p, wgs, s);
     return stream ? launch_form<KB, 1, 2, true>(p, wgs, s) : launch_form<KB, 1, 2, false>(p, wgs, s);
 }

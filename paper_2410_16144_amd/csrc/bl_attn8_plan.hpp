@@ -4,17 +4,29 @@
 
 namespace bl {
 
-constexpr int kRows8Waves = 8;            // waves of a workgroup of the rows form, each with a chunk of 64 positions at a time
-constexpr int kRows8FewWaves = 4;         // ... with more than four rows, and beside tiles
-// ... with many heads and sequences: more workgroups than compute units.  A unit holds one workgroup of eight waves (133 registers) and six of two,
-// and what a short walk takes is waiting.  32 heads of 128, caches of 17 positions, eight and two waves, us: 8 sequences 5.9 and TIMES, 16 10.2 and
-// TIMES, 64 37.4 and TIMES.
-constexpr int kRows8ManyWaves = 2;
 constexpr int kAttn8Units = 256;          // compute units
+// Rows that share a walk and go without tiles.  32 heads of 128, rows and tiles, us: 5 tokens behind 8000 22.9 and 26.8, 8 behind 500 13.4 and 14.2;
+// 16 (in sixteens) 32.7 and 27.7, 21.6 and 15.6.
+constexpr int kRows8Most = 8;
+// Waves of a workgroup of the rows form, each with a chunk of 64 positions at a time: eight, with many heads and sequences fewer: more workgroups than
+// compute units.  A unit holds one workgroup of eight waves (133 registers) and six of two, and what a short walk takes is waiting.  Rows in fours,
+// 32 heads of 128, caches of 17 positions, eight waves and two, us: 16 sequences 10.2 and 7.2, 32 20.1 and 10.3, 64 37.4 and 17.5.  In eights, eight
+// waves and four: a token at 100 000, 64 heads on 8, 41.6 and 49.2; 40 sequences of 64 on 8 at 300 positions 15.1 and 12.5.  In sixteens: 64 on 4 at
+// 20 000 22.8 and 29.5, 96 sequences at 300 22.3 and 19.4; head sizes above 128 have no room for eight such waves' sums.
+constexpr int kRows8Waves = 8;
+constexpr int kRows8FewWaves = 4;         // in eights and sixteens, and beside tiles
+constexpr int kRows8ManyWaves = 2;        // in fours
+// Own walks beside tiles, in their kernel, share a unit two by two with them and run while the tiles do; more of them are launched by themselves.  32
+// heads of 128 behind a prefix of 100, 300 own positions, in one launch and in two, us: 40 sequences 24.4 and 32.2, 64 36.6 and 41.4, 80 45.0 and 46.9, 128
+// 66.0 and 63.2; 20 own positions: 40 21.3 and 23.7, 64 30.6 and 29.2, 128 49.5 and 41.9.
+constexpr int kAttn8Beside = 8 * kAttn8Units;
 constexpr int kTiles8Set = 7;             // positions that a workgroup of the tiles form walks at a time: 1 << 7, 32 per wave
 constexpr int kTiles8Rows = 32;           // rows of a tile
 constexpr int kAttn8MaxSplits = 64;       // workgroups that share a row's walk: the merge's lanes
 constexpr int kAttn8Waves = 2048;         // that a launch aims at: two on each SIMD of 256 compute units
+// ... and, where the own walks alone are as many, that the walk of the prefix has all the same.  Sixteen sequences of 32 heads behind 8000 positions, 20 of
+// their own: 25.7 us, with half as many 32.0, without 84.
+constexpr int kAttn8SharedWaves = 1024;
 // A short walk that meets nobody else is not split: the meeting (figures performed, tickets, figures read: three trips to memory) takes 3.6 us, a
 // set of 512 positions in one compute unit 1.0 us with a head size of 64 and 1.8 with 128.  One workgroup per head and one per set, us: 32 heads
 // of 128 at 1000 positions 9.3 and 10.5, at 2000 12.9 and 10.9; 12 of 64 at 1000 6.7 and 9.0, at 2000 8.7 and 9.3.
@@ -58,15 +70,16 @@ struct Attn8Plan {
 inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, int own_len, int size) {
     Attn8Plan p{};
     const int64_t rows = (int64_t)tokens * group;
-    p.tiles = shared_len > 0 && rows > 4;
+    p.tiles = shared_len > 0 && rows > kRows8Most;
     const int64_t most = p.tiles ? (own_len > 0 ? 4 : 0) : shared_len > 0 ? rows : group;   // (beside tiles: fours)
     p.block = most <= 4 ? 4 : most <= 8 ? 8 : 16;
     p.own_blocks = own_len > 0 ? (group + p.block - 1) / p.block : 0;
     const int64_t own = (int64_t)n_heads * tokens * p.own_blocks;
-    // own walks beside tiles, in their kernel, share a unit two by two; more than that many are launched by themselves
-    p.apart = p.tiles && own > 2 * kAttn8Units;
-    const int64_t units = own > 0 ? own : n_heads * ((rows + p.block - 1) / p.block);
-    p.waves = p.block > 4 || (p.tiles && !p.apart) ? kRows8FewWaves : units > kAttn8Units ? kRows8ManyWaves : kRows8Waves;
+    p.apart = p.tiles && own > kAttn8Beside;
+    const bool many = (own > 0 ? own : n_heads * ((rows + p.block - 1) / p.block)) > kAttn8Units;
+    if (p.tiles && !p.apart) p.waves = kRows8FewWaves;
+    else if (p.block == 4) p.waves = many ? kRows8ManyWaves : kRows8Waves;
+    else p.waves = many || (p.block == 16 && size > 128) ? kRows8FewWaves : kRows8Waves;
     p.own_set = p.waves == kRows8Waves ? 9 : p.waves == kRows8FewWaves ? 8 : 7;
     // a prompt of many rows: two or four tiles per workgroup
     int more = 0;
@@ -87,7 +100,9 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
         for (int64_t quota = together || more ? longest + unit : unit;; quota += quota / 16 / unit * unit + unit) {
             const int a = splits(shared_now, p.shared_set, quota), b = splits(own_now, p.own_set, quota);
             if (a > kAttn8MaxSplits || b > kAttn8MaxSplits) continue;
-            if (!more && quota < longest + unit && shared * a * (p.tiles ? kRows8FewWaves : p.waves) + own * b * p.waves > kAttn8Waves) continue;
+            const int64_t shared_waves = shared * a * (p.tiles ? kRows8FewWaves : p.waves);
+            const bool fits = shared_waves + own * b * p.waves <= kAttn8Waves || (b == 1 && shared_waves <= kAttn8SharedWaves);
+            if (!more && quota < longest + unit && !fits) continue;
             if (shared_now > 0) p.shared_splits = a;
             if (own_now > 0) p.own_splits = b;
             return;

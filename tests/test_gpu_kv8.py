@@ -395,3 +395,19 @@ def test_prompt_then_tokens(dev, mods):
         assert float((one - whole[m]).norm()) <= 1e-5 * float(whole[m].norm())
     for name in ("k_codes", "v_codes", "k_scale", "v_scale"):
         assert torch.equal(getattr(a, name), getattr(b, name))
+
+
+@pytest.mark.parametrize("heads,n,dim,pos0,M", [(32, 32, 128, 900, 5), (3, 3, 64, 1500, 8), (2, 2, 96, 2000, 9), (8, 2, 120, 1100, 2), (4, 1, 256, 700, 2), (16, 2, 256, 300, 1),
+                                                (5, 5, 128, 0, 8), (2, 2, 36, 60, 7)])
+def test_prompts_of_few_rows(dev, mods, heads, n, dim, pos0, M):
+    """Up to eight rows of a key head, which go without tiles, and one more."""
+    _check_prompt(mods, dev, heads, n, dim, pos0, M, 61000 + pos0 + M)
+
+
+@pytest.mark.parametrize("heads,n,dim,prefix_len,lengths", [(32, 32, 64, 1500, [3, 0, 80, 64, 17, 300, 1, 2] * 2), (40, 40, 64, 900, [9] * 14 + [200]), (64, 64, 64, 300, [5, 70] * 17),
+                                                            (33, 33, 64, 130, [2] * 63), (32, 32, 128, 2000, [7, 100, 0, 64, 65] * 1), (64, 8, 64, 500, [10, 200] * 5),
+                                                            (32, 32, 128, 1000, [30] * 8), (64, 8, 128, 0, [40] * 33), (64, 4, 64, 0, [600, 1] * 3), (96, 6, 64, 0, [70] * 43)])
+def test_batches_of_many_own_walks(dev, mods, heads, n, dim, prefix_len, lengths):
+    """Own walks that alone fill the device beside the prefix's walk, and more than go into one launch with it; rows in eights and sixteens by
+    eight waves and by four."""
+    test_sequences_behind_a_prefix(dev, mods, heads, n, dim, prefix_len, lengths)

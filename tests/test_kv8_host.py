@@ -135,7 +135,7 @@ def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
                                 const bl::Attn8Plan p = bl::attn8_plan(heads, group, tokens, shared, own, 16 * (1 + (heads + shared + own) % 16));
                                 const int64_t rows = (int64_t)tokens * group;
                                 if (p.block != 4 && p.block != 8 && p.block != 16) return 1;
-                                if (p.tiles && (p.block != 4 || rows <= 4 || !shared)) return 10;
+                                if (p.tiles && (p.block != 4 || rows <= bl::kRows8Most || !shared)) return 10;
                                 if ((shared > 0) != (p.shared_splits > 0) || (own > 0) != (p.own_splits > 0)) return 2;
                                 if (p.shared_splits > 64 || p.own_splits > 64) return 3;
                                 const int block = p.tiles ? p.tile_rows : p.block;
@@ -144,11 +144,13 @@ def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
                                 if (own && p.own_blocks * p.block < group) return 5;
                                 if (p.shared_splits > bl::sets_of(shared, p.shared_set) || p.own_splits > bl::sets_of(own, p.own_set)) return 6;
                                 if (p.shared_set != (p.tiles ? (p.tile_rows == 128 ? 5 : p.tile_rows == 64 ? 6 : 7) : p.own_set) || p.own_set != (p.waves == 8 ? 9 : p.waves == 4 ? 8 : 7)) return 7;
-                                if ((p.waves != 4) != (p.block == 4 && (!p.tiles || p.apart)) || (p.apart && !p.tiles)) return 12;
+                                if (p.waves != 8 && p.waves != (p.block == 4 && (!p.tiles || p.apart) ? 2 : 4)) return 12;
+                                if ((p.tiles && !p.apart && p.waves != 4) || (p.apart && !p.tiles)) return 15;
                                 if (p.shared_wgs % 8 || p.shared_wgs < (int64_t)heads * p.shared_splits * p.shared_blocks) return 8;
                                 if (p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 9;
                                 const int64_t a = (int64_t)heads * p.shared_splits * p.shared_blocks * (p.tiles ? 4 : p.waves), b = p.own_wgs * p.waves;
-                                if (!p.apart && a + b > bl::kAttn8Waves && (p.shared_splits > 1 || p.own_splits > 1)) return 11;
+                                const bool least = p.own_splits == 1 && a <= bl::kAttn8SharedWaves;   // the shared walk's share beside many own ones
+                                if (!p.apart && a + b > bl::kAttn8Waves && (p.shared_splits > 1 || p.own_splits > 1) && !least) return 11;
                                 if (p.apart && ((a > bl::kAttn8Waves && p.shared_splits > 1) || (b > bl::kAttn8Waves && p.own_splits > 1))) return 14;
                             }
             return 0;
