@@ -77,7 +77,8 @@ hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_
     p.by_own_blocks = divider(p.own_blocks); p.by_own_splits = divider(p.own_splits); p.by_shared_splits = divider(p.shared_splits);
     p.by_shared_units = divider((p.n_heads * p.shared_splits + 7) / 8 * 8);
     const int found = compute_unit_count(), cus = found > 0 ? found : 256;
-    p.paired = wgs > cus && wgs <= 2 * cus;   // all resident: a unit's second block is as short as its first one is long
+    p.folded = plan.folded;
+    p.paired = !plan.folded && wgs > cus && wgs <= 2 * cus;   // all resident: a unit's second block is as short as its first one is long
     if (!plan.tiles) return launch_rows(p, plan, wgs, s);
     p.merges = plan.slots() > 1;
     hipError_t e = launch_attn8_tiles(p, plan.apart ? p.shared_wgs : wgs, s);

@@ -28,6 +28,7 @@ struct Attn8Args {
     int32_t        prompt;      // the shared walk is a prompt's: token m sees rows 0 .. pos0 + m
     int32_t        pos0;
     int32_t        merges;      // a launch follows that merges the figures
+    int32_t        folded;      // a workgroup takes two of a prompt's blocks, from both ends
     int32_t        paired;      // a prompt's blocks in the order last, ..., middle, first, ..., middle instead of last ... first
     float          unit;        // log2(e) / sqrt(head_dim)
     Divider        by_heads, by_group, by_half, by_tokens, by_own_blocks, by_own_splits, by_shared_splits, by_shared_units;   // (units: padded)
@@ -84,12 +85,14 @@ __device__ __forceinline__ void attn8_to_head(const Attn8Args& p, Attn8Walk& w) 
 }
 
 // False: nothing to do for this workgroup.  The index goes by blocks of rows first, then by pieces of the cache (padded to whole rounds of the
-// dies, so that a piece's workgroups are on one die); a prompt's later blocks walk more and are launched first.
-__device__ __forceinline__ bool attn8_shared_walk(const Attn8Args& p, int wg, int block_rows, Attn8Walk& w) {
+// dies, so that a piece's workgroups are on one die); a prompt's later blocks walk more and are launched first.  again: the second of a folded
+// prompt's blocks.
+__device__ __forceinline__ bool attn8_shared_walk(const Attn8Args& p, int wg, int block_rows, Attn8Walk& w, bool again = false) {
     const int units = p.n_heads * p.shared_splits, turn = divided(wg, p.by_shared_units), unit = wg - turn * ((units + 7) & ~7);
     if (unit >= units) return false;
     const int first_half = (p.shared_blocks + 1) >> 1;
-    const int block = !p.prompt ? turn : p.paired && turn >= first_half ? turn - first_half : p.shared_blocks - 1 - turn;
+    if (again && 2 * turn == p.shared_blocks - 1) return false;   // (the block in the middle)
+    const int block = !p.prompt || again ? turn : p.paired && turn >= first_half ? turn - first_half : p.shared_blocks - 1 - turn;
     w.split = divided(unit, p.by_heads);
     w.head = unit - w.split * p.n_heads;
     w.splits = p.shared_splits;

@@ -53,6 +53,7 @@ constexpr int sets_of(int positions, int set) { return (int)(((int64_t)positions
 struct Attn8Plan {
     int     tiles;            // the shared part in tiles of 32 rows; else (and the own part) rows in fours
     int     tile_rows;        // rows of a workgroup of the tiles form: 32, 64 or 128
+    int     folded;           // a workgroup takes two of a prompt's blocks, from both ends: all walk as much, to the launch's end
     int     block;            // rows of a workgroup of the rows form: 4, 8 or 16
     int     shared_set, own_set;   // 1 << so many positions are a workgroup's set
     int     waves;            // of a workgroup of the rows form
@@ -81,9 +82,15 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
     else if (p.block == 4) p.waves = many ? kRows8ManyWaves : kRows8Waves;
     else p.waves = many || (p.block == 16 && size > 128) ? kRows8FewWaves : kRows8Waves;
     p.own_set = p.waves == kRows8Waves ? 9 : p.waves == kRows8FewWaves ? 8 : 7;
-    // a prompt of many rows: two or four tiles per workgroup
-    int more = 0;
-    while (p.tiles && own_len == 0 && more < 2 && n_heads * ((rows + (2 * kTiles8Rows << more) - 1) / (2 * kTiles8Rows << more)) * kRows8FewWaves >= kAttn8Waves) ++more;
+    // A prompt of many rows: two or four tiles per workgroup, and folded where that leaves enough of them: unfolded, a compute unit's last long
+    // block runs alone.  32 heads of 128, unfolded and folded, us: 2048 tokens 114 and 106, behind 16 000 1107 and 1060, 4096 325 and 311; with one tile
+    // per workgroup it cost (1024 tokens: two tiles unfolded 43, one folded 49).
+    const auto enough = [&](int more, int fold) {
+        const int64_t blocks = (rows + (kTiles8Rows << more) - 1) / (kTiles8Rows << more);
+        return p.tiles && own_len == 0 && n_heads * ((blocks + fold - 1) / fold) * kRows8FewWaves >= kAttn8Waves;
+    };
+    p.folded = enough(1, 2);
+    const int more = enough(2, 2) ? 2 : enough(1, 1) ? 1 : 0;
     p.tile_rows = kTiles8Rows << more;
     const int shared_block = p.tiles ? p.tile_rows : p.block;
     p.shared_set = p.tiles ? kTiles8Set - more : p.own_set;
@@ -115,7 +122,7 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
         share(shared_len, own_len);
     }
     // (the shared part's workgroups go around the dies in eights, all row blocks of a piece of the cache on one die)
-    p.shared_wgs = ((int64_t)n_heads * p.shared_splits + 7) / 8 * 8 * p.shared_blocks;
+    p.shared_wgs = ((int64_t)n_heads * p.shared_splits + 7) / 8 * 8 * (p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks);
     p.own_wgs = own * p.own_splits;
     return p;
 }

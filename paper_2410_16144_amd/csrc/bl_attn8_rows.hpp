@@ -27,7 +27,7 @@ __device__ __forceinline__ v4i rows8_mfma(const v4i& a, const v4i& b, const v4i&
 __device__ __forceinline__ float rows8_joined(const v4i& s) { return fmaf((float)s[2], 65536.0f, (float)((s[1] << 8) + s[0])); }
 
 // A walk's bytes are read once.  From memory, streaming loads are faster, and leave a model's weights in the memory-side cache; a short cache that
-// the token before left in the dies' caches is faster without (see launch_block).
+// the token before left in the dies' caches is faster without (see launch_rows).
 template <bool STREAM>
 __device__ __forceinline__ v4i rows8_load(const int8_t* at) {
     if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const v4i*>(at));

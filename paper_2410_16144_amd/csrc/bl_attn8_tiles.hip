@@ -8,14 +8,21 @@ namespace {
 
 constexpr int max_of(int a, int b) { return a > b ? a : b; }
 
-// SETS: waves of a tile.  OWN: whether there is an own part (a prompt has none; without it the kernel is smaller).
-template <int D32, int SETS, bool OWN>
+// SETS: waves of a tile.  OWN: whether there is an own part (a prompt has none; without it the kernel is smaller).  FOLD: a prompt's blocks by twos
+// (a form of its own: the loop costs seven registers more than there are).
+template <int D32, int SETS, bool OWN, bool FOLD>
 __global__ __launch_bounds__(kTiles8Threads, D32 <= 4 ? 2 : 1) void attn8_tiles_kernel(const Attn8Args p) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ Attn8Rows rows;
     Attn8Walk walk;
     const int wg = blockIdx.x;   // uniform, like the walk
-    if (!OWN || wg < p.shared_wgs) {
+    if constexpr (!OWN) {
+        __shared__ Tiles8Shared shared;
+        for (int again = 0; again <= (FOLD ? 1 : 0); ++again) {
+            if (again) __syncthreads();   // (everybody has what the first block left in LDS)
+            if (attn8_shared_walk(p, wg, kTiles8Rows * kTiles8Waves / SETS, walk, again)) tiles8_walk<D32, SETS>(p, walk, lds, shared, rows);
+        }
+    } else if (wg < p.shared_wgs) {
         __shared__ Tiles8Shared shared;
         if (attn8_shared_walk(p, wg, kTiles8Rows * kTiles8Waves / SETS, walk)) tiles8_walk<D32, SETS>(p, walk, lds, shared, rows);
     } else {
@@ -24,27 +31,27 @@ __global__ __launch_bounds__(kTiles8Threads, D32 <= 4 ? 2 : 1) void attn8_tiles_
     }
 }
 
-template <int D32, int SETS, bool OWN>
+template <int D32, int SETS, bool OWN, bool FOLD = false>
 hipError_t launch_form(const Attn8Args& p, int wgs, hipStream_t s) {
     constexpr int kBytes = OWN ? max_of(Tiles8Lds<D32>::kBytes, Rows8Lds<(D32 + 1) / 2, 1, kTiles8Waves>::kBytes) : Tiles8Lds<D32>::kBytes;
     static_assert(kBytes + 4096 <= 160 * 1024, "fits a compute unit");
     static LdsCeiling ceiling;   // per instantiation, i.e. per kernel
-    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&attn8_tiles_kernel<D32, SETS, OWN>), kBytes);
+    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&attn8_tiles_kernel<D32, SETS, OWN, FOLD>), kBytes);
     if (e != hipSuccess) return e;
-    attn8_tiles_kernel<D32, SETS, OWN><<<dim3((unsigned)wgs), dim3(kTiles8Threads), kBytes, s>>>(p);
+    attn8_tiles_kernel<D32, SETS, OWN, FOLD><<<dim3((unsigned)wgs), dim3(kTiles8Threads), kBytes, s>>>(p);
     return hipGetLastError();
 }
 
 template <int D32>
 hipError_t launch_size(const Attn8Args& p, int wgs, hipStream_t s) {
     if (wgs > p.shared_wgs) return launch_form<D32, 4, true>(p, wgs, s);
-    if (p.shared_set == 5) return launch_form<D32, 1, false>(p, wgs, s);
+    if (p.folded) return p.shared_set == 5 ? launch_form<D32, 1, false, true>(p, wgs, s) : launch_form<D32, 2, false, true>(p, wgs, s);
     return p.shared_set == 6 ? launch_form<D32, 2, false>(p, wgs, s) : launch_form<D32, 4, false>(p, wgs, s);
 }
 
 // What the workgroups of a row left behind a launch of tiles: one workgroup per (row, key head), the row's figures shared out among its waves.
 // A launch of its own, because the last workgroup of 32 rows reads their figures a trip to memory at a time: 77 tokens behind 1001, 32 heads of 120,
-// five workgroups per row 31.5 us with tickets, of which the reading 10, TIMES so; one token's rows are few, and meet without (attn8_finish).
+// five workgroups per row 31.5 us with tickets, of which the reading 10, 25.7 so; one token's rows are few, and meet without (attn8_finish).
 __global__ __launch_bounds__(kTiles8Threads) void attn8_merge_kernel(const Attn8Args p) {
     __shared__ float2 s_sum[kTiles8Waves][kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -2,9 +2,9 @@
 //
 // A workgroup's four waves share out the 32-position halves of chunks and merge their running maxima, sums and outputs at the end (SETS = 4), or
 // have two or four tiles of 32 rows, with two waves or one for each: a long prompt has workgroups enough, and what a tile costs beside its
-// halves -- its queries' way into the operands, the meeting -- is paid less often per half (2048 tokens, 32 heads of 128: attention TIMES).  A wave
-// brings its own operands and waits for nobody.  Every operand comes from memory as it lies there (bl_kv8.hpp), 16 bytes per lane: no LDS,
-// no transposition.
+// halves -- its queries' way into the operands, the meeting -- is paid less often per half (32 heads of 128, 1024 tokens, one tile and two: 47.6 and
+// 42.8 us).  A wave brings its own operands and waits for nobody.  Every operand comes from memory as it lies there (bl_kv8.hpp), 16 bytes per
+// lane: no LDS, no transposition.
 //
 // Scores are formed transposed, S^T = K Q^T, by v_mfma_i32_32x32x32_i8 on the codes, with the queries as three signed bytes each (24-bit
 // fixed point relative to a row's largest value, as in the rows form): the lowest byte's sums are rounded to units of the second's and go on
@@ -15,9 +15,11 @@
 // weight w = p s^v as the sum of two f16 numbers (22 bits), scaled by a power of two over the largest s^v so far, so that moving it is
 // exact.  fp32 accumulation throughout.
 //
-// A half's scores are formed while the weights and outputs of the half before are: 28 matrix instructions (900 cycles) beside some 340 vector
-// instructions (1400) in one stream, eight after each, so that a wave keeps both pipes busy by itself.  With the two in turn, the two waves of a
-// SIMD stayed in step, and a half took the sum of both (PER HALF).
+// A half is 28 matrix instructions (900 cycles) and some 340 vector instructions (1400): the vector ALU bounds a long walk, at 1.0 us per half and
+// SIMD with two waves there (cycles with a vector instruction 67 %, with a matrix one 43 %).  A half's scores are formed beside the weights and
+// outputs of the half before, so that either pipe has work in one wave's stream; by itself that changed nothing (512 tokens behind 16 000, 32 heads of 128:
+// 285 us, in turn 281), with the wave's priority raised while the products are formed 270: the other wave then has the phase that this one has not.  Head
+// sizes to 64 have half the products and do without (12 heads of 64, 2048 tokens 38.6 us, raised 41.5).
 #pragma once
 #include "bl_attn8.hpp"
 
@@ -267,6 +269,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
             run_e = e_new;
         }
         const float base = END && run_m == -INFINITY ? 0.0f : run_m;
+        if constexpr (D32 > 2) __builtin_amdgcn_s_setprio(1);   // until the products are out
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (NEXT) {
             scales_in(i + 1);
@@ -318,6 +321,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
                 o[t] = tiles8_mfma16(a[h], w_hi[h], o[t]);
             }
         }
+        if constexpr (D32 > 2) __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (MORE) request_keys(i + 2);
         if constexpr (NEXT) request_values(i + 1);

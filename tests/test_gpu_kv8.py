@@ -411,3 +411,9 @@ def test_batches_of_many_own_walks(dev, mods, heads, n, dim, prefix_len, lengths
     """Own walks that alone fill the device beside the prefix's walk, and more than go into one launch with it; rows in eights and sixteens by
     eight waves and by four."""
     test_sequences_behind_a_prefix(dev, mods, heads, n, dim, prefix_len, lengths)
+
+
+@pytest.mark.parametrize("heads,n,dim,pos0,M", [(64, 64, 64, 0, 1000), (64, 64, 64, 33, 2080), (130, 130, 32, 10, 500), (64, 8, 128, 70, 300), (300, 300, 64, 0, 130), (256, 256, 48, 5, 65)])
+def test_prompts_of_many_tiles(dev, mods, heads, n, dim, pos0, M):
+    """Two and four tiles per workgroup, a workgroup's blocks from both ends, an odd number of blocks, ends inside a tile."""
+    _check_prompt(mods, dev, heads, n, dim, pos0, M, 63000 + pos0 + M, sample=sorted({0, 1, 31, 32, M // 2, min(M // 2 + 33, M - 1), M - 34, M - 1}))

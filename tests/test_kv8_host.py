@@ -146,7 +146,9 @@ def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
                                 if (p.shared_set != (p.tiles ? (p.tile_rows == 128 ? 5 : p.tile_rows == 64 ? 6 : 7) : p.own_set) || p.own_set != (p.waves == 8 ? 9 : p.waves == 4 ? 8 : 7)) return 7;
                                 if (p.waves != 8 && p.waves != (p.block == 4 && (!p.tiles || p.apart) ? 2 : 4)) return 12;
                                 if ((p.tiles && !p.apart && p.waves != 4) || (p.apart && !p.tiles)) return 15;
-                                if (p.shared_wgs % 8 || p.shared_wgs < (int64_t)heads * p.shared_splits * p.shared_blocks) return 8;
+                                const int64_t turns = p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks;
+                                if (p.shared_wgs % 8 || p.shared_wgs < heads * p.shared_splits * turns) return 8;
+                                if (p.folded && (!p.tiles || own || p.shared_splits != 1 || heads * turns * 4 < bl::kAttn8Waves)) return 16;
                                 if (p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 9;
                                 const int64_t a = (int64_t)heads * p.shared_splits * p.shared_blocks * (p.tiles ? 4 : p.waves), b = p.own_wgs * p.waves;
                                 const bool least = p.own_splits == 1 && a <= bl::kAttn8SharedWaves;   // the shared walk's share beside many own ones
