@@ -345,14 +345,19 @@ bl_status bl_kv8_read(const bl_kv8_read_args *args, void *stream);
  *   q_lin_dev [sequences, n_q_heads * head_dim] fp32; k_lin_dev, v_lin_dev [sequences, cache.n_heads * head_dim] fp32; rows contiguous
  *   pos_dev        [sequences] int32
  *   rope_table_dev rows 0 .. prefix_len + cache.max_pos - 1
- *   prefix         NULL with prefix_len 0, or a cache of the same heads and head size whose first sequence holds rows 0 .. prefix_len - 1
+ *   prefix         not read with prefix_len 0; else a cache of the same heads and head size, in memory of its own, whose first sequence holds
+ *                  rows 0 .. prefix_len - 1
  *   scratch_dev    bl_attn8_scratch_bytes(...) bytes, 16-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
  *                  the next.  Calls that may overlap in time must not share it.
- * Arithmetic: the queries enter as 24-bit fixed-point numbers (relative to their row's largest value), the weights as fixed-point numbers of
- * at least 22 bits (relative to their chunk's largest), the codes as they are; integer sums are exact, everything else is fp32.
- * Nobody waits for anybody: the workgroups of a row leave their figures in scratch_dev, the last one adds them up, in a fixed order:
- * a call repeated gives the same bits.
- * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache.n_heads, a prefix of another shape), BL_ERR_ALIGN, BL_ERR_HIP.
+ * Arithmetic: the queries enter as 24-bit fixed-point numbers (relative to their row's largest value), the codes as they are, with exact integer
+ * sums.  A softmax weight times its value's scale enters as a 23-bit fixed-point number relative to its row's largest one in a chunk of 64 positions
+ * (exact sums again), or, where more than eight rows share a prefix, as the sum of two f16 numbers (22 bits).  Everything else is fp32.  A query with a NaN
+ * or an infinity makes its own row NaN.
+ * Up to three launches: up to eight rows (sequence, query head) of a key head take one, in which the workgroups of a row leave their figures in
+ * scratch_dev and the last one adds them up; more rows behind a prefix take the prefix in tiles of 32, many sequences' own rows in a launch of
+ * their own, and a last one adds the figures up.  Nobody waits for anybody, and figures are added in a fixed order: a call repeated gives the same bits.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache.n_heads, a prefix of another shape or in the sequences' memory),
+ *         BL_ERR_ALIGN, BL_ERR_HIP.
  */
 typedef struct bl_attn8_args {
     const float        *q_lin_dev;
@@ -376,7 +381,8 @@ bl_status bl_attn8_decode(const bl_attn8_args *args, void *stream);
 
 /*
  * bl_attn_prefill over an 8-bit cache: M consecutive tokens of one sequence at positions pos0 .. pos0 + M - 1 go into the cache
- * (bl_kv8_write's bytes), then token m attends to rows 0 .. pos0 + m.  Two launches.
+ * (bl_kv8_write's bytes), then token m attends to rows 0 .. pos0 + m, with bl_attn8_decode's arithmetic.  Two launches, or three
+ * (where several workgroups of 32 rows share a walk).
  *   q_lin_dev [M, n_q_heads * head_dim], k_lin_dev, v_lin_dev [M, cache->n_heads * head_dim] fp32, rows contiguous
  *   out_dev      [M, n_q_heads * head_dim] fp32
  *   scratch_dev  bl_attn8_prefill_scratch_bytes(...) bytes, 16-byte aligned, contents free

@@ -645,6 +645,11 @@ bl_status bl_attn8_decode(const bl_attn8_args* a, void* stream) {
         s = check_kv8(a->prefix);
         if (s != BL_OK) return s;
         if (a->prefix.n_heads != a->cache.n_heads || a->prefix.head_dim != a->cache.head_dim || a->prefix_len > a->prefix.max_pos) return BL_ERR_SHAPE;
+        // the sequences write their caches while others still read the prefix
+        const int64_t own = (int64_t)bl_kv8_code_bytes(a->cache.n_heads, a->cache.head_dim, a->cache.max_pos) * a->cache.sequences;
+        const int64_t shared = (int64_t)bl_kv8_code_bytes(a->prefix.n_heads, a->prefix.head_dim, a->prefix.max_pos);
+        const auto meet = [&](const int8_t* x, const int8_t* y) { return x < y + shared && y < x + own; };
+        if (meet(a->cache.k_codes_dev, a->prefix.k_codes_dev) || meet(a->cache.v_codes_dev, a->prefix.v_codes_dev)) return BL_ERR_SHAPE;
     }
     if (!aligned(a->q_lin_dev, 4) || !aligned(a->k_lin_dev, 4) || !aligned(a->v_lin_dev, 4) || !aligned(a->pos_dev, 4) ||
         !aligned(a->rope_table_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))

@@ -127,11 +127,11 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
     return p;
 }
 
-// The scratch memory: a counter per (key head, row), a head's in lines of their own, then the figures.
+// The scratch memory: a counter per (key head, row), a head's in lines of their own, then the figures (none where a row has one workgroup).
 constexpr int64_t attn8_padded(int64_t rows) { return (rows + 31) / 32 * 32; }
 inline int64_t attn8_counters(int n_heads, int64_t rows) { return n_heads * attn8_padded(rows); }
 inline int64_t attn8_scratch(const Attn8Plan& p, int n_heads, int64_t rows, int head_dim) {
-    return attn8_counters(n_heads, rows) * 4 + n_heads * rows * p.slots() * (head_dim / 2 + 1) * 8;
+    return attn8_counters(n_heads, rows) * 4 + (p.slots() > 1 ? n_heads * rows * p.slots() * (head_dim / 2 + 1) * 8 : 0);
 }
 
 }  // namespace bl

@@ -136,9 +136,9 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                     lo[n][m] = a * cs[n][m].x - b * cs[n][m].y;
                     hi[n][m] = a * cs[n][m].y + b * cs[n][m].x;
                 }
-                amax = fmaxf(amax, fmaxf(fabsf(lo[n][m]), fabsf(hi[n][m])));
+                amax = MaxBitsOp()(amax, MaxBitsOp()(fabsf(lo[n][m]), fabsf(hi[n][m])));   // (a NaN becomes the row's unit)
             }
-            amax = wave_max(amax);
+            amax = over_lanes<64>(amax, MaxBitsOp());
             if (t < rows) {
                 const float inv = query_inv(amax);
                 if (lane == 0) shared.unit[t] = amax * (1.0f / kQueryFull) * p.unit;

@@ -160,10 +160,9 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
                     const float a = lo[m][x], b = hi[m][x], c = cs[m][2 * x], s = cs[m][2 * x + 1];
                     lo[m][x] = a * c - b * s;
                     hi[m][x] = a * s + b * c;
-                    amax = fmaxf(amax, fmaxf(fabsf(lo[m][x]), fabsf(hi[m][x])));
+                    amax = MaxBitsOp()(amax, MaxBitsOp()(fabsf(lo[m][x]), fabsf(hi[m][x])));   // (a NaN becomes the row's unit)
                 }
-#pragma unroll
-            for (int x = 1; x < 8; x <<= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
+            amax = over_lanes<8>(amax, MaxBitsOp());
             const float inv = query_inv(amax);
             if (t8 == 0) shared.unit[32 * tile + r] = amax * (1.0f / kQueryFull) * 256.0f * p.unit;
             uint8_t* dst = queries + r * L::kQPitch;

@@ -35,6 +35,10 @@ __device__ __forceinline__ float over_lanes(float v, Op op) {
 }
 #undef BL_LANES
 struct AddOp { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+// Of numbers without a sign, a NaN above all others (their bits' order).
+struct MaxBitsOp {
+    __device__ __forceinline__ float operator()(float a, float b) const { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }
+};
 struct MaxOp { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 }  // namespace bl

@@ -208,6 +208,7 @@ class Attention8:
                                       self.scratch.data_ptr(), cache.args, n_heads, prefix.args if prefix_len else None, prefix_len)
 
     def launch(self):
+        assert torch.cuda.current_device() == self.out.device.index, "the cache is not on the current device"
         B.launch(B.LAUNCH_ATTN8_DECODE, self.args, 1)
         return self.out
 
@@ -507,7 +508,8 @@ class DecoderStack:
 
     def fork(self, n: int, max_new: int) -> "DecoderFork":
         """n sequences that continue from the present position, each with room for max_new tokens of its own (cache="int8" only).  The
-        stack's rows are read, not copied, and have to stay: the stack may go on from here, but not be set back."""
+        stack's rows are read, not copied, and have to stay: the stack may go on from here, but not be set back.  Its workspace is the
+        fork's, too: steps of the two, or of two forks, must not overlap in time unless use_workspace is False."""
         return DecoderFork(self, n, max_new)
 
     def step(self):

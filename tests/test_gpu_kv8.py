@@ -417,3 +417,33 @@ def test_batches_of_many_own_walks(dev, mods, heads, n, dim, prefix_len, lengths
 def test_prompts_of_many_tiles(dev, mods, heads, n, dim, pos0, M):
     """Two and four tiles per workgroup, a workgroup's blocks from both ends, an odd number of blocks, ends inside a tile."""
     _check_prompt(mods, dev, heads, n, dim, pos0, M, 63000 + pos0 + M, sample=sorted({0, 1, 31, 32, M // 2, min(M // 2 + 33, M - 1), M - 34, M - 1}))
+
+
+@pytest.mark.parametrize("form", ["token", "rows", "tiles", "prefix in tiles"])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_a_query_that_is_not_finite(dev, mods, form, what):
+    """Its own row becomes NaN, in whichever element it stands; every other row keeps its bits."""
+    B, dec, ops = mods
+    r = _rng(14000)
+    heads, n, dim = 4, 2, 96
+    M, pos0 = {"token": (1, 700), "rows": (3, 900), "tiles": (40, 300), "prefix in tiles": (7, 1000)}[form]
+    table = _table(dim, pos0 + M + 1)
+    q, k, v = _rows(r, M, heads * dim), _rows(r, M, n * dim), _rows(r, M, n * dim)
+    cache, _ = _filled(dec, dev, r, n, dim, pos0 + M + 1, [pos0], table)
+
+    def out(q):
+        if form in ("rows", "tiles"):
+            return dec.attn_prefill8(_t(q, dev), _t(k, dev), _t(v, dev), cache, _t(table, dev), pos0)
+        if form == "token":
+            return dec.Attention8(heads, cache, _t(q, dev), _t(k, dev), _t(v, dev), _t(np.array([pos0], np.int32), dev), _t(table, dev)).launch()
+        own = dec.KvCache8(n, dim, 1, dev, sequences=M)
+        return dec.Attention8(heads, own, _t(q, dev), _t(k, dev), _t(v, dev), _t(np.full(M, pos0, np.int32), dev), _t(table, dev), prefix=cache, prefix_len=pos0).launch()
+    clean = out(q).cpu().reshape(M, heads, dim)
+    assert bool(torch.isfinite(clean).all())
+    for m, h, e in ((0, 1, 0), (M - 1, 3, dim - 1), (M // 2, 0, dim // 2 + 3)):
+        bad = q.copy()
+        bad[m, h * dim + e] = what
+        got = out(bad).cpu().reshape(M, heads, dim)
+        assert bool(torch.isnan(got[m, h]).all())
+        got[m, h] = clean[m, h]
+        assert torch.equal(got, clean)

@@ -83,6 +83,8 @@ def test_refusals_of_the_token_attention():
         assert call(_cache(**kw)) == B.BL_ERR_SHAPE
     assert call(prefix_len=-1) == B.BL_ERR_SHAPE and call(prefix=_cache(), prefix_len=101) == B.BL_ERR_SHAPE
     assert call(prefix=_cache(n_heads=8), prefix_len=5) == call(prefix=_cache(head_dim=60), prefix_len=5) == B.BL_ERR_SHAPE
+    for kw in ({}, dict(k_codes_dev=P + (1 << 30)), dict(k_codes_dev=P + 2048, v_codes_dev=P + (1 << 30)), dict(k_codes_dev=P - 4096, v_codes_dev=P + (1 << 30))):
+        assert call(prefix=_cache(**kw), prefix_len=5) == B.BL_ERR_SHAPE      # a prefix in the memory of the sequences' own rows
     for name, off in (("q", 2), ("k", 2), ("v", 1), ("pos", 2), ("table", 4), ("out", 4), ("scratch", 8)):
         assert call(**{name: P + off}) == B.BL_ERR_ALIGN
     assert call(prefix=_cache(v_scale_dev=P + 4), prefix_len=5) == B.BL_ERR_ALIGN
@@ -103,7 +105,7 @@ def test_refusals_of_the_prompt_attention():
 
 
 def test_scratch_sizes():
-    assert B.bl_attn8_scratch_bytes(32, 32, 128, 64, 1, 0) == 32 * 32 * 4 + 32 * 1 * 65 * 8          # one workgroup per head
+    assert B.bl_attn8_scratch_bytes(32, 32, 128, 64, 1, 0) == 32 * 32 * 4                            # one workgroup per head
     for bad in ((31, 32, 128, 64, 1, 0), (32, 32, 130, 64, 1, 0), (32, 32, 128, 0, 1, 0), (32, 32, 128, 64, 0, 0), (32, 32, 128, 64, 1, -1)):
         assert B.bl_attn8_scratch_bytes(*bad) == 0
     assert B.bl_attn8_prefill_scratch_bytes(8, 4, 64, 0, 0) == B.bl_attn8_prefill_scratch_bytes(8, 3, 64, 0, 5) == 0
