@@ -44,7 +44,8 @@ def parse_args():
                     help="few launches per measurement (no clock ramp, no spread): for a profiler that collects counters "
                          "and slows every dispatch; the times such a run prints are not results")
     ap.add_argument("--models", default="", help="with --only tokens: comma-separated Appendix-A model names (default: all 12)")
-    ap.add_argument("--only", default="", help="run only one extra section (copy|ceilings|prefill|config1|config2|config3|decode100b|paper100b|appendixa|tokens|tokens8k|prompt|prompt2k|tl2) and print it")
+    ap.add_argument("--only", default="", help="run only one extra section (copy|ceilings|prefill|config1|config2|config3|decode100b|paper100b|appendixa|tokens|tokens8k|prompt|prompt2k|fork|tl2) and print it")
+    ap.add_argument("--cache", choices=("bf16", "int8"), default="bf16", help="with --only tokens|tokens8k|prompt|prompt2k: the key/value cache")
     return ap.parse_args()
 
 
@@ -550,10 +551,10 @@ def extra_appendix_a(torch, use_graph):
     return rows
 
 
-def extra_decoder_tokens(torch, models, max_pos=512, tokens=64):
+def extra_decoder_tokens(torch, models, max_pos=512, tokens=64, cache="bf16"):
     """Whole-model token rate in the paper's own unit (Section 3's tables: tokens/s) on Appendix A's shapes with
     dummy weights as in the paper: every token passes through ALL layers -- norms, the seven products, rotary
-    embedding, attention over the bf16 cache, gate, residuals -- as ONE captured graph per token (10 launches
+    embedding, attention over the cache (bf16 or int8), gate, residuals -- as ONE captured graph per token (10 launches
     per layer).  No embedding lookup, output head or sampling: the paper gives no vocabulary.  Timed at a short
     context (positions 0 .. tokens-1) and at a longer one (the last `tokens` positions below max_pos)."""
     from paper_2410_16144_amd import decoder, synth
@@ -561,10 +562,10 @@ def extra_decoder_tokens(torch, models, max_pos=512, tokens=64):
     rows = []
     for name in models or list(synth.PAPER_MODELS):
         hidden, ffn, n_layers = synth.PAPER_MODELS[name]
-        stack = decoder.make_stack(name, max_pos, dev)
+        stack = decoder.make_stack(name, max_pos, dev, cache=cache)
         stack.capture()
         x = torch.randn((tokens, 1, hidden), device=dev, generator=torch.Generator(device=dev).manual_seed(1))
-        row = {"model": name, "hidden": hidden, "ffn": ffn, "layers": n_layers, "heads": synth.PAPER_HEADS[name],
+        row = {"model": name, "hidden": hidden, "ffn": ffn, "layers": n_layers, "heads": synth.PAPER_HEADS[name], "cache": cache,
                "packed_GB": round(sum(p.packed_bytes for p in synth.layer_projections(hidden, ffn)) * n_layers / 1e9, 3)}
         for label, start in (("context_0", 0), ("context_%d" % (max_pos - tokens), max_pos - tokens)):
             def run():
@@ -599,27 +600,64 @@ def extra_decoder_tokens(torch, models, max_pos=512, tokens=64):
     return rows
 
 
-def extra_prompt(torch, models, M=512, max_pos=1024):
+def extra_prompt(torch, models, M=512, max_pos=1024, cache="bf16"):
     """Prompt processing through the same decoder block: M tokens at once, the products as bl_gemm / bl_gemm_batch over
-    the M rows, attention as bl_attn_prefill (eager launches).  Prompt tokens per second, first at positions 0..M-1,
+    the M rows, attention as bl_attn_prefill or bl_attn8_prefill (eager launches).  Prompt tokens per second, first at positions 0..M-1,
     then for a second piece at M..2M-1."""
     from paper_2410_16144_amd import decoder, synth
     dev = torch.device("cuda:0")
     rows = []
     for name in models or ["700M", "7B"]:
         hidden, ffn, n_layers = synth.PAPER_MODELS[name]
-        stack = decoder.make_stack(name, max_pos, dev, gated=False)
+        stack = decoder.make_stack(name, max_pos, dev, gated=False, cache=cache)
         x = torch.randn((2 * M, hidden), device=dev, generator=torch.Generator(device=dev).manual_seed(2))
-        row = {"model": name, "hidden": hidden, "ffn": ffn, "layers": n_layers, "prompt_tokens": M}
+        row = {"model": name, "hidden": hidden, "ffn": ffn, "layers": n_layers, "cache": cache, "prompt_tokens": M}
         for label, start in (("positions_0", 0), ("positions_%d" % M, M)):
             piece = x[start:start + M].contiguous()
             stack.set_position(start)
             stack.prefill(piece)           # untimed pass
             stack.set_position(start)
             ms, wall = timed(torch, lambda: stack.prefill(piece))
-            assert bool(torch.isfinite(stack.layers[-1].attn.v_cache[start + M - 1].float()).all())
+            attn = stack.layers[-1].attn
+            last = attn.v_cache[start + M - 1].float() if cache == "bf16" else attn.cache.read(start + M - 1, 1)[1]
+            assert bool(torch.isfinite(last).all())
             row[label] = {"ms": round(ms, 3), "prompt_tokens_per_s": round(M * 1e3 / ms, 1),
                           "us_per_layer": round(ms * 1e3 / n_layers, 1), "wall_ms": round(wall, 3)}
+        rows.append(row)
+        del stack
+        torch.cuda.empty_cache()
+    return rows
+
+
+def extra_fork(torch, models, sequences=(2, 8, 32), prompt=8000, tokens=64):
+    """Several sequences behind one prompt in the 8-bit cache (DecoderStack.fork): every step takes one token of each as one captured graph,
+    products over as many rows, the prompt's keys and values read once for all of them.  Tokens per second of all sequences together."""
+    from paper_2410_16144_amd import decoder, synth
+    dev = torch.device("cuda:0")
+    rows = []
+    for name in models or ["7B"]:
+        hidden, ffn, n_layers = synth.PAPER_MODELS[name]
+        stack = decoder.make_stack(name, prompt, dev, gated=False, cache="int8")
+        g = torch.Generator(device=dev).manual_seed(3)
+        for start in range(0, prompt, 2000):
+            stack.prefill(torch.randn((min(2000, prompt - start), hidden), device=dev, generator=g))
+        row = {"model": name, "hidden": hidden, "ffn": ffn, "layers": n_layers, "prompt": prompt}
+        for n in sequences:
+            fork = stack.fork(n, tokens)
+            fork.capture()
+            x = torch.randn((tokens, n, hidden), device=dev, generator=g)
+
+            def run():
+                for t in range(tokens):
+                    fork.h.copy_(x[t])
+                    fork.graph.replay()
+            run()                              # untimed pass
+            fork.pos.fill_(prompt)
+            ms, _ = timed(torch, run)
+            assert bool(torch.isfinite(fork.y).all())
+            row["sequences_%d" % n] = {"ms_per_step": round(ms / tokens, 4), "tokens_per_s": round(n * tokens * 1e3 / ms, 1),
+                                       "us_per_layer": round(ms * 1e3 / tokens / n_layers, 2)}
+            del fork
         rows.append(row)
         del stack
         torch.cuda.empty_cache()
@@ -843,11 +881,12 @@ def sections(torch, np, args, use_graph):
         "decode100b": lambda: extra_decode_shape(torch, "100B-shape", 12288, 33792, 1, 6, 120, use_graph),
         "paper100b": lambda: extra_decode_shape(torch, "Appendix-A 100B", 8192, 45568, 1, 6, 120, use_graph),
         "appendixa": lambda: extra_appendix_a(torch, use_graph),
-        "tokens": lambda: {"gpu": extra_decoder_tokens(torch, models),
+        "tokens": lambda: {"gpu": extra_decoder_tokens(torch, models, cache=args.cache),
                            "cpu_baseline": None if args.no_cpu else decoder_cpu_baseline()},
-        "tokens8k": lambda: extra_decoder_tokens(torch, models or ["7B"], max_pos=8192),
-        "prompt": lambda: extra_prompt(torch, models),
-        "prompt2k": lambda: extra_prompt(torch, models or ["7B"], M=2048, max_pos=4096),
+        "tokens8k": lambda: extra_decoder_tokens(torch, models or ["7B"], max_pos=8192, cache=args.cache),
+        "prompt": lambda: extra_prompt(torch, models, cache=args.cache),
+        "prompt2k": lambda: extra_prompt(torch, models or ["7B"], M=2048, max_pos=4096, cache=args.cache),
+        "fork": lambda: extra_fork(torch, models),
         "tl2": lambda: extra_tl2(torch, use_graph),
     }
 
