@@ -203,12 +203,12 @@ class Attention8:
         if bytes_ == 0:
             raise B.BitLinearError(B.BL_ERR_SHAPE, "Attention8")
         self.scratch = torch.zeros(bytes_, dtype=torch.uint8, device=dev)
-        self._keep = (q_lin, k_lin, v_lin, pos, table)
+        self._keep, self._device = (q_lin, k_lin, v_lin, pos, table), dev.index
         self.args = B.make_attn8_args(q_lin.data_ptr(), k_lin.data_ptr(), v_lin.data_ptr(), pos.data_ptr(), table.data_ptr(), self.out.data_ptr(),
                                       self.scratch.data_ptr(), cache.args, n_heads, prefix.args if prefix_len else None, prefix_len)
 
     def launch(self):
-        assert torch.cuda.current_device() == self.out.device.index, "the cache is not on the current device"
+        assert torch.cuda.current_device() == self._device, "the cache is not on the current device"
         B.launch(B.LAUNCH_ATTN8_DECODE, self.args, 1)
         return self.out
 

@@ -447,3 +447,35 @@ def test_a_query_that_is_not_finite(dev, mods, form, what):
         assert bool(torch.isnan(got[m, h]).all())
         got[m, h] = clean[m, h]
         assert torch.equal(got, clean)
+
+
+def test_offsets_beyond_32_bits(dev, mods):
+    """Sequences of a million positions, the last one's rows more than 2^32 bytes behind the first one's: writes at both ends, reads, a token's
+    attention and a prompt's."""
+    B, dec, ops = mods
+    r = _rng(15000)
+    heads, n, dim, most, seqs = 4, 4, 128, 1000000, 10
+    assert (seqs - 1) * n * most * dim > 2 ** 32
+    cache = dec.KvCache8(n, dim, most, dev, sequences=seqs)
+    k, v = _rows(r, 70, n * dim), _rows(r, 70, n * dim)
+    cache.write(_t(k, dev), _t(v, dev), most - 70, sequence=seqs - 1)
+    for got, x in zip(cache.read(most - 70, 70, sequence=seqs - 1), (k, v)):
+        codes, scale = _codes(x, dim)
+        np.testing.assert_array_equal(got.cpu().numpy().reshape(70, n, dim), codes.astype(np.float32) * scale[..., None])
+    assert not bool(cache.read(most - 140, 70, sequence=seqs - 1)[0].any()) and not bool(cache.read(most - 70, 70, sequence=seqs - 2)[0].any())
+    small, table = dec.KvCache8(n, dim, 200, dev), _table(dim, 200)
+    grown = torch.zeros((most, dim // 2, 2), device=dev)
+    grown[:200] = _t(table, dev)
+    q, k, v = (_t(_rows(r, 150, n * dim), dev) for _ in range(3))
+    a = dec.attn_prefill8(q, k, v, cache, grown, 0, sequence=seqs - 1)
+    b = dec.attn_prefill8(q, k, v, small, _t(table, dev), 0)
+    assert torch.equal(a, b)                                    # (a prompt's plan does not depend on the cache's size)
+    tokens = [_t(_rows(r, seqs, n * dim), dev) for _ in range(3)]
+    pos = torch.full((seqs,), -1, dtype=torch.int32, device=dev)
+    pos[-1] = 150
+    out = dec.Attention8(heads, cache, *tokens, pos, grown).launch()[-1]
+    one = dec.Attention8(heads, small, *(t[-1:].contiguous() for t in tokens), pos[-1:].contiguous(), _t(table, dev)).launch()[0]
+    for x, y in zip(cache.read(0, 151, sequence=seqs - 1), small.read(0, 151)):
+        assert torch.equal(x, y)
+    # two orders of one sum, each within eight times the other tests' mean distance from the exact one
+    assert float((out - one).abs().max()) <= 2 * 2.6e-6 * 8 * float(small.read(0, 151)[1].abs().max())
