@@ -32,6 +32,11 @@ constexpr int kAttn8SharedWaves = 1024;
 // of 128 at 1000 positions 9.3 and 10.5, at 2000 12.9 and 10.9; 12 of 64 at 1000 6.7 and 9.0, at 2000 8.7 and 9.3.
 constexpr int kRows8Together = 256 << 10;   // bytes of codes
 
+// What splitting a prompt's walk in tiles takes and saves, in tenths of a microsecond (32 heads of 128): a set of 128 positions with one wave on a SIMD and
+// with two; the merging launch; 100 rows' figures, out and in.  As planned and in one piece, us: 256 tokens behind 600 32.8 and 25.1, 200 behind none 22.3
+// and 16.6, behind 1500 35.6 and 32.0; the other way 20 tokens behind 1000 17.4 and 22.7, 40 behind 2000 22.4 and 32.7; 77 behind 1000 24.1 and 25.0.
+constexpr int kTiles8SetAlone = 14, kTiles8SetBeside = 20, kTiles8Merge = 40;
+
 // Division by a number that the host knows, for 0 <= n < 2^31: n m >> (31 + s) with 2^s >= d and m = 2^(31 + s) / d rounded up.  m d exceeds
 // 2^(31 + s) by less than d <= 2^s, so n m / 2^(31 + s) exceeds n / d by less than 1 / d: the same whole number.  (A workgroup that divides
 // its index by unknown numbers spends some forty instructions on each, one after another, ahead of its first request.)
@@ -120,6 +125,11 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
         share(0, own_len);
     } else {
         share(shared_len, own_len);
+    }
+    if (p.tiles && own_len == 0 && p.shared_splits > 1) {
+        const int64_t sets = sets_of(shared_len, p.shared_set), most = (sets + p.shared_splits - 1) / p.shared_splits, wide = size > 128 ? size : 128;
+        const int64_t set = shared * p.shared_splits > kAttn8Units ? kTiles8SetBeside : kTiles8SetAlone;
+        if (sets * kTiles8SetAlone * wide / 128 <= most * set * wide / 128 + kTiles8Merge + n_heads * rows / 100 * wide / 128) p.shared_splits = 1;
     }
     // (the shared part's workgroups go around the dies in eights, all row blocks of a piece of the cache on one die)
     p.shared_wgs = ((int64_t)n_heads * p.shared_splits + 7) / 8 * 8 * (p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks);
