@@ -68,14 +68,14 @@ hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_
     p.counters = static_cast<uint32_t*>(scratch);
     p.figures = reinterpret_cast<float2*>(p.counters + attn8_counters(p.n_heads, p.rows));
     p.shared_set = plan.shared_set; p.own_set = plan.own_set;
-    p.shared_splits = plan.shared_splits; p.shared_blocks = plan.shared_blocks;
+    p.shared_splits = plan.shared_splits; p.shared_blocks = plan.shared_blocks; p.shared_units = (int32_t)plan.shared_units; p.strips = plan.strips;
     p.own_splits = plan.own_splits; p.own_blocks = plan.own_blocks;
     if (plan.shared_wgs + plan.own_wgs > INT32_MAX) return hipErrorInvalidValue;
     p.shared_wgs = (int32_t)plan.shared_wgs;
     const int wgs = (int)(plan.shared_wgs + plan.own_wgs);
     p.by_heads = divider(p.n_heads); p.by_group = divider(p.group); p.by_half = divider(p.head_dim / 2); p.by_tokens = divider(p.tokens);
     p.by_own_blocks = divider(p.own_blocks); p.by_own_splits = divider(p.own_splits); p.by_shared_splits = divider(p.shared_splits);
-    p.by_shared_units = divider((p.n_heads * p.shared_splits + 7) / 8 * 8);
+    p.by_shared_units = divider((int)plan.shared_units); p.by_pieces = divider(p.n_heads * p.shared_splits);
     const int found = compute_unit_count(), cus = found > 0 ? found : 256;
     p.folded = plan.folded;
     p.paired = !plan.folded && wgs > cus && wgs <= 2 * cus;   // all resident: a unit's second block is as short as its first one is long

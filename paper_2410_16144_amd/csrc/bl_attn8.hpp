@@ -23,7 +23,7 @@ struct Attn8Args {
     int32_t        rows;        // tokens * group: a row is one query head of one token, of one key head
     int32_t        shared_len;  // rows of the prefix
     int32_t        max_pos;     // of a sequence's own cache
-    int32_t        shared_wgs, shared_splits, shared_blocks, own_splits, own_blocks;
+    int32_t        shared_wgs, shared_splits, shared_blocks, shared_units, strips, own_splits, own_blocks;
     int32_t        shared_set, own_set;   // positions of a workgroup's sets: 1 << so much
     int32_t        prompt;      // the shared walk is a prompt's: token m sees rows 0 .. pos0 + m
     int32_t        pos0;
@@ -31,7 +31,7 @@ struct Attn8Args {
     int32_t        folded;      // a workgroup takes two of a prompt's blocks, from both ends
     int32_t        paired;      // a prompt's blocks in the order last, ..., middle, first, ..., middle instead of last ... first
     float          unit;        // log2(e) / sqrt(head_dim)
-    Divider        by_heads, by_group, by_half, by_tokens, by_own_blocks, by_own_splits, by_shared_splits, by_shared_units;   // (units: padded)
+    Divider        by_heads, by_group, by_half, by_tokens, by_own_blocks, by_own_splits, by_shared_splits, by_shared_units, by_pieces;   // (pieces: n_heads * shared_splits)
 };
 
 hipError_t launch_attn8_tiles(const Attn8Args& p, int wgs, hipStream_t s);   // bl_attn8_tiles.hip
@@ -84,17 +84,26 @@ __device__ __forceinline__ void attn8_to_head(const Attn8Args& p, Attn8Walk& w) 
     w.c.v_scale += w.head * w.c.head_scales;
 }
 
-// False: nothing to do for this workgroup.  The index goes by blocks of rows first, then by pieces of the cache (padded to whole rounds of the
-// dies, so that a piece's workgroups are on one die); a prompt's later blocks walk more and are launched first.  again: the second of a folded
-// prompt's blocks.
+// False: nothing to do for this workgroup.  The index goes by blocks of rows first, then by pieces of the cache (padded to whole rounds of the dies, so
+// that a piece's workgroups are on one die); a prompt's later blocks walk more and are launched first.  again: the second of a folded prompt's
+// blocks.  PROMPT: a prompt in tiles, whose blocks may go by strips (the index costs a batch's kernel half a microsecond).
+template <bool PROMPT = false>
 __device__ __forceinline__ bool attn8_shared_walk(const Attn8Args& p, int wg, int block_rows, Attn8Walk& w, bool again = false) {
-    const int units = p.n_heads * p.shared_splits, turn = divided(wg, p.by_shared_units), unit = wg - turn * ((units + 7) & ~7);
-    if (unit >= units) return false;
+    const int pieces = p.n_heads * p.shared_splits, round = divided(wg, p.by_shared_units);
+    int piece = wg - round * p.shared_units, turn = round;
+    if constexpr (PROMPT) {
+        const int strip = divided(piece, p.by_pieces);
+        piece -= strip * pieces;
+        turn = round * p.strips + strip;
+        if (strip >= p.strips || turn >= (p.folded ? (p.shared_blocks + 1) >> 1 : p.shared_blocks)) return false;
+        if (again && 2 * turn == p.shared_blocks - 1) return false;   // (the block in the middle)
+    } else if (piece >= pieces) {
+        return false;
+    }
     const int first_half = (p.shared_blocks + 1) >> 1;
-    if (again && 2 * turn == p.shared_blocks - 1) return false;   // (the block in the middle)
     const int block = !p.prompt || again ? turn : p.paired && turn >= first_half ? turn - first_half : p.shared_blocks - 1 - turn;
-    w.split = divided(unit, p.by_heads);
-    w.head = unit - w.split * p.n_heads;
+    w.split = divided(piece, p.by_heads);
+    w.head = piece - w.split * p.n_heads;
     w.splits = p.shared_splits;
     w.slot = w.split;
     w.row0 = block * block_rows;

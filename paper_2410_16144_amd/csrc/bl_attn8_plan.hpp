@@ -67,6 +67,8 @@ struct Attn8Plan {
     int     shared_blocks;    // row blocks over all tokens
     int     own_splits;       // the same for a sequence's own rows; 0: none
     int     own_blocks;       // row blocks of one sequence's rows
+    int     strips;           // dies that a piece of the shared walk's row blocks go to
+    int64_t shared_units;     // workgroups of one block in every strip of every piece, in whole rounds of the dies
     int64_t shared_wgs, own_wgs;
     int     slots() const { return shared_splits + own_splits; }   // figures that a row's workgroups leave
     bool    meets() const { return !tiles && slots() > 1; }        // the workgroups of a row meet by counters (else: one, or a merging launch)
@@ -131,8 +133,16 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
         const int64_t set = shared * p.shared_splits > kAttn8Units ? kTiles8SetBeside : kTiles8SetAlone;
         if (sets * kTiles8SetAlone * wide / 128 <= most * set * wide / 128 + kTiles8Merge + n_heads * rows / 100 * wide / 128) p.shared_splits = 1;
     }
-    // (the shared part's workgroups go around the dies in eights, all row blocks of a piece of the cache on one die)
-    p.shared_wgs = ((int64_t)n_heads * p.shared_splits + 7) / 8 * 8 * (p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks);
+    // The shared part's workgroups go around the dies in eights, all row blocks of a piece of the cache to one die.  A prompt with few pieces, not a multiple
+    // of eight, would leave dies without work: there two, four or eight dies take a piece's blocks in turn.  300 tokens, 16 heads of 256 on 2, us:
+    // 64.5 and 32.4, 1500 404 and 114; 1500, 28 of 128 on 4 87.7 and 54.6; with 32 pieces and more it costs (100 behind 3000, 12 of 64, 19.6 and 20.5).
+    const int64_t turns = p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks, pieces = (int64_t)n_heads * p.shared_splits;
+    p.strips = 1;
+    if (p.tiles && own_len == 0 && pieces < 32)
+        while (pieces * p.strips % 8 != 0) p.strips *= 2;
+    if (turns < p.strips) p.strips = 1;
+    p.shared_units = (pieces * p.strips + 7) / 8 * 8;
+    p.shared_wgs = p.shared_units * ((turns + p.strips - 1) / p.strips);
     p.own_wgs = own * p.own_splits;
     return p;
 }

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kTiles8Threads, D32 <= 4 ? 2 : 1) void attn8_tiles_
         __shared__ Tiles8Shared shared;
         for (int again = 0; again <= (FOLD ? 1 : 0); ++again) {
             if (again) __syncthreads();   // (everybody has what the first block left in LDS)
-            if (attn8_shared_walk(p, wg, kTiles8Rows * kTiles8Waves / SETS, walk, again)) tiles8_walk<D32, SETS>(p, walk, lds, shared, rows);
+            if (attn8_shared_walk<true>(p, wg, kTiles8Rows * kTiles8Waves / SETS, walk, again)) tiles8_walk<D32, SETS>(p, walk, lds, shared, rows);
         }
     } else if (wg < p.shared_wgs) {
         __shared__ Tiles8Shared shared;

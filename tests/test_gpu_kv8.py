@@ -479,3 +479,9 @@ def test_offsets_beyond_32_bits(dev, mods):
         assert torch.equal(x, y)
     # two orders of one sum, each within eight times the other tests' mean distance from the exact one
     assert float((out - one).abs().max()) <= 2 * 2.6e-6 * 8 * float(small.read(0, 151)[1].abs().max())
+
+
+@pytest.mark.parametrize("heads,n,dim,pos0,M", [(3, 3, 64, 0, 300), (10, 5, 36, 20, 500), (28, 4, 128, 0, 130), (16, 2, 256, 5, 75), (12, 12, 64, 0, 900), (21, 7, 64, 0, 1500), (4, 1, 64, 100, 700)])
+def test_prompts_of_few_key_heads(dev, mods, heads, n, dim, pos0, M):
+    """Numbers of key heads that are no multiple of the dies: a head's blocks by strips, and what is left over at their ends."""
+    _check_prompt(mods, dev, heads, n, dim, pos0, M, 64000 + pos0 + M, sample=sorted({0, 1, 31, 32, 33, M // 3, M // 2, M - 34, M - 2, M - 1}))

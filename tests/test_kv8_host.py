@@ -149,7 +149,11 @@ def test_plan_covers_every_row_and_fits_its_merge(tmp_path):
                                 if (p.waves != 8 && p.waves != (p.block == 4 && (!p.tiles || p.apart) ? 2 : 4)) return 12;
                                 if ((p.tiles && !p.apart && p.waves != 4) || (p.apart && !p.tiles)) return 15;
                                 const int64_t turns = p.folded ? (p.shared_blocks + 1) / 2 : p.shared_blocks;
-                                if (p.shared_wgs % 8 || p.shared_wgs < heads * p.shared_splits * turns) return 8;
+                                if (p.shared_wgs % 8 || p.shared_units % 8 || p.shared_wgs < heads * p.shared_splits * turns || p.shared_wgs % (p.shared_units ? p.shared_units : 1)) return 8;
+                                if (p.strips > 1 && (!p.tiles || own)) return 20;
+                                if (p.strips != 1 && p.strips != 2 && p.strips != 4 && p.strips != 8) return 17;
+                                if (shared && p.shared_wgs >= heads * p.shared_splits * turns + 8 * turns && p.strips == 1) return 18;
+                                if (p.strips > 1 && p.shared_wgs >= heads * p.shared_splits * (turns + p.strips)) return 19;
                                 if (p.folded && (!p.tiles || own || p.shared_splits != 1 || heads * turns * 4 < bl::kAttn8Waves)) return 16;
                                 if (p.own_wgs != (int64_t)heads * tokens * p.own_blocks * p.own_splits) return 9;
                                 const int64_t a = (int64_t)heads * p.shared_splits * p.shared_blocks * (p.tiles ? 4 : p.waves), b = p.own_wgs * p.waves;
