@@ -12,8 +12,8 @@
 // lane (query l % 32, half g) then has 16 weights of one query, of positions 16 g .. 16 g + 15 in order: the rows of the K operand are
 // taken from memory so that result register r is position 16 g + r, whose values are byte r of the 16 bytes that the lane with the
 // same g loads for a dim.  So O^T += V^T P^T has its operands in place: 32x32x16 f16 products, codes converted (exactly) in registers, a
-// weight w = p s^v as the sum of two f16 numbers (22 bits), scaled by a power of two over the largest s^v so far, so that moving it is
-// exact.  fp32 accumulation throughout.
+// weight w = p s^v as the sum of two f16 numbers (22 bits) -- relative to the row's own largest weight, see kTiles8Top.  fp32 accumulation
+// throughout.
 //
 // A half is 28 matrix instructions (900 cycles) and some 340 vector instructions (1400): the vector ALU bounds a long walk, at 1.0 us per half and
 // SIMD with two waves there (cycles with a vector instruction 67 %, with a matrix one 43 %).  A half's scores are formed beside the weights and
@@ -27,11 +27,19 @@ namespace bl {
 
 constexpr int kTiles8Keys = 32, kTiles8Waves = 4, kTiles8Threads = 64 * kTiles8Waves;
 static_assert(1 << kTiles8Set == kTiles8Waves * kTiles8Keys, "a half chunk per wave");
-// A row's reference score moves when a score exceeds it by 2^8: nearly every half has a new maximum for one of 32 queries (2048 tokens: all but
-// a few), and the 64 products that rescale the outputs are a sixth of a half's instructions.  Weights are then up to 2^8 and, scaled by 2^7,
-// 2^15: f16 numbers whose second part is a normal number down to 2^-2.
-constexpr float kTiles8Move = 8.0f;
-constexpr int kTiles8Scale = 7;
+// What keeps a row's weights within f16.  A row has a reference score, p = exp2(score - reference), and a wave an exponent E above those of all
+// value scales that it has met; weights, and with them the outputs, are w = p s^v 2^(60 - E).  The reference is set so that the row's largest weight so far
+// is between 2^6 and 2^7 (2^3 at least, see alike): weights down to 2^-3 then have 22 bits, smaller ones are rounded to 2^-25, 2^-28 of the largest.
+// By the largest score alone, a value that a row does not see, or gives no weight, would take the bits of those that it does: E is all rows'.  The
+// reference is looked at again where score and scales of a half would allow a weight of 2^15, and rises if a weight of the row's own is above 2^7
+// by then: nearly every half has a new maximum for one of 32 queries, and the 64 products that rescale the outputs are a sixth of a half's
+// instructions.  It is never further than 2^96 below a half's largest score, so that 4 million sums of p stay below 2^119: a row that weighs values
+// 2^-140 times as large as what others see has all bits of them.  Nor is it more than 2^53 above one: p down to 2^-73 are in the sums.
+constexpr int kTiles8Top = 15, kTiles8Set0 = 7, kTiles8Far = 96;
+constexpr int kTiles8Scale = 60;           // 2^60: between what the sums' range leaves for large p and for small ones
+constexpr int kTiles8Above = 2;            // E is set so far above a scale's exponent: the next, slightly larger ones leave it (2048 tokens 108.8 and 106.7 us)
+constexpr int kTiles8Sum = 100;            // a sum of p above 2^100 is not scaled up any more
+constexpr int kTiles8NoScale = -140;       // below every scale's exponent
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
@@ -44,6 +52,7 @@ __device__ __forceinline__ i32x16 tiles8_mfma(const v4i& a, const v4i& b, const 
 __device__ __forceinline__ f32x16 tiles8_mfma16(const u32x4& a, const u32x4& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+__device__ __forceinline__ int exponent_above(float x) { return (int)(__float_as_uint(x) >> 23) - 126; }   // x < 2^this, for x >= 0 (0: -126)
 // Four codes as f16: 1024 + (code + 128) by its bits, less 1152 (both exact).
 __device__ __forceinline__ void tiles8_widen(uint32_t codes, uint32_t& lo, uint32_t& hi) {
     const uint32_t u = codes ^ 0x80808080u;
@@ -198,8 +207,10 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     for (int t = 0; t < D32; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-    float run_m = -INFINITY, run_l = 0.0f;      // run_l: over this lane half's positions only
-    int run_e = -100, next_e = -100;            // exponent of the largest value scale so far, at least (uniform); of the half under way, too
+    float run_m = -INFINITY, run_l = 0.0f;      // the reference score; run_l: over this lane half's positions only
+    int run_e = kTiles8NoScale, next_e = run_e; // E (uniform); with the half under way
+    bool alike = false;                         // the first half's value scales are within a factor of 16 (uniform)
+    int next_room = 0;                          // of the half under way: how far its scores may be above the reference for weights below 2^15
     i32x16 low, high;                           // the scores under way: S^T, 32 positions x 32 queries, in units of 256 of the queries'
 
     // A half's scales go through LDS, lanes 0-31 the keys', lanes 32-63 the values', when its keys have arrived.
@@ -207,7 +218,12 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         const int first = half_of(i) * kTiles8Keys;
         const float own = first + l32 >= keys ? 0.0f : scale;   // (what lies behind the last row may be anything)
         const float v_max = wave_max(g ? own : 0.0f);
-        if (v_max > 0.0f) next_e = max(next_e, __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max)));
+        next_room = kTiles8Far;
+        if (v_max > 0.0f) {
+            const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max));
+            if (e > next_e) next_e = e + kTiles8Above;
+            next_room = min(kTiles8Top - kTiles8Scale + next_e - e, kTiles8Far);
+        }
         shared.scale[wave][i & 1][lane] = g ? ldexpf(own, kTiles8Scale - next_e) : own;
         __builtin_amdgcn_wave_barrier();        // (a wave's LDS operations are performed in order)
     };
@@ -237,6 +253,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         const bool masked = END && first + kTiles8Keys > lowest;   // uniform
         const float* scales_of = shared.scale[wave][i & 1];
         const int e_new = next_e;
+        const float room = (float)next_room;
         float x[16];
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
@@ -255,17 +272,43 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         mx = over_blocks<32>(mx, MaxOp());
         // (a query whose values are all zero has unit 0; it must not meet an infinity)
         const float top = END && mx == -INFINITY ? mx : mx * unit;
-        if (__any(top > run_m + kTiles8Move) || e_new != run_e) {
-            const float m_new = fmaxf(run_m, top);
-            const float f = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(run_m - m_new);
-            const float fo = ldexpf(f, run_e - e_new);
+        if (__any(top > run_m + room) || e_new != run_e) {
+            int left = 0;                                  // of a new exponent's bits, what the outputs take: the reference takes the others
+            if (e_new != run_e) {
+                const int more = e_new - run_e, taken = min(more, max(kTiles8Sum - exponent_above(over_blocks<32>(run_l, MaxOp())), 0));
+                run_m -= (float)taken;
+                run_l = ldexpf(run_l, taken);
+                left = taken - more;
+                run_e = e_new;
+            }
+            // The exponent of the row's largest weight relative to its largest score.  In a first half whose scales are alike, theirs: sixteen more
+            // exponentials there, where nothing else is under way, cost short walks 0.2 us of 25.
+            int w_exp = kTiles8Scale - kTiles8Above;
+            if (!alike) {
+                float w_max = 0.0f;
+#pragma unroll
+                for (int r4 = 0; r4 < 4; ++r4) {
+                    const f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float at = x[4 * r4 + c];
+                        w_max = fmaxf(w_max, __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -top)) * vs[c]);
+                    }
+                }
+                w_exp = exponent_above(over_blocks<32>(w_max, MaxOp()));
+            }
+            alike = false;
+            const float m_new = top > run_m + room ? fmaxf(run_m, top + (float)max(w_exp - kTiles8Set0, -kTiles8Far)) : run_m;
+            const float apart = run_m - m_new;
+            const int far = apart < -64.0f ? 64 : 0;       // (2^-126 is the least that exp2 gives; sums may be of 2^100)
+            const float f = m_new == run_m ? 1.0f : __builtin_amdgcn_exp2f(apart + (float)far);
+            const float fo = ldexpf(f, left - far);
 #pragma unroll
             for (int t = 0; t < D32; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[t][r] *= fo;
-            run_l *= f;
+            run_l = ldexpf(run_l * f, -far);
             run_m = m_new;
-            run_e = e_new;
         }
         const float base = END && run_m == -INFINITY ? 0.0f : run_m;
         if constexpr (D32 > 2) __builtin_amdgcn_s_setprio(1);   // until the products are out
@@ -279,23 +322,20 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
             const f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
-            float w[4];
+            float pj[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const float at = x[4 * r4 + c];
-                const float pj = __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -base));
-                sum += pj;
-                w[c] = pj * vs[c];
+                pj[c] = __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -base));
+                sum += pj[c];
             }
 #pragma unroll
-            for (int c = 0; c < 4; c += 2) {
-                const f16x2 hi = __builtin_convertvector((f32x2{w[c], w[c + 1]}), f16x2);
-                const uint32_t both = __builtin_bit_cast(uint32_t, hi);
-                float rest[2];                             // what the first parts leave: w - hi (exact)
-                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rest[0]) : "v"(both), "v"(w[c]));
-                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(rest[1]) : "v"(both), "v"(w[c + 1]));
-                const f16x2 lo = __builtin_convertvector((f32x2{rest[0], rest[1]}), f16x2);
-                w_hi[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = both;
+            for (int c = 0; c < 4; c += 2) {               // a product's f16 number, and what it leaves
+                f16x2 hi = {(_Float16)fmaf(pj[c], vs[c], 0.0f), (_Float16)fmaf(pj[c + 1], vs[c + 1], 0.0f)};
+                asm("" : "+v"(hi));                        // (one register from here on: else the second number is formed twice)
+                const f32x2 rest = {fmaf(pj[c], vs[c], -(float)hi[0]), fmaf(pj[c + 1], vs[c + 1], -(float)hi[1])};
+                const f16x2 lo = __builtin_convertvector(rest, f16x2);
+                w_hi[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, hi);
                 w_lo[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, lo);
             }
         }
@@ -329,7 +369,9 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
     if (mine > 0) {
+        const float v_min = over_lanes<64>(g == 0 ? INFINITY : half_of(0) * kTiles8Keys + l32 >= keys ? 0.0f : scale, MinOp());
         scales_in(0);
+        alike = exponent_above(__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v_min)))) > next_e - kTiles8Above - 4;
         scores_low_high();
         scores_middle();
         __builtin_amdgcn_sched_barrier(0);
@@ -340,9 +382,12 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     if (mine > 1) walk(mine - 2, yes, no, yes);
     if (mine > 0) walk(mine - 1, no, no, yes);
 
-    // ---- the waves meet: maxima and sums first, then the outputs, each scaled by its own factor
+    // ---- the waves meet: references and sums first -- the references moved so that a sum is one of 0.5 to 1: by how much a wave has of a row --
+    // then the outputs, each scaled by its own factor
     run_l = over_blocks<32>(run_l, AddOp());
-    if (g == 0) shared.ml[wave][l32] = make_float2(run_m, run_l);
+    const int l_e = exponent_above(run_l);
+    run_m += (float)l_e;
+    if (g == 0) shared.ml[wave][l32] = make_float2(run_m, ldexpf(run_l, -l_e));
     __syncthreads();
     const auto figure = [&](int at_tile, int r) {
         float m = -INFINITY, l = 0.0f;
@@ -354,7 +399,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         return make_float2(m, l);
     };
     const float2 all = figure(tile, l32);
-    float f = ldexpf(__builtin_amdgcn_exp2f(run_m - (all.x == -INFINITY ? 0.0f : all.x)), run_e - kTiles8Scale);
+    float f = ldexpf(__builtin_amdgcn_exp2f(run_m - (all.x == -INFINITY ? 0.0f : all.x)), run_e - kTiles8Scale - l_e);
     if (SETS < 4) f = rows > 0 ? f / all.y : 0.0f;         // (one split: nobody else has figures)
     float* meet = reinterpret_cast<float*>(lds);   // (the barrier above: every wave has its queries)
 #pragma unroll

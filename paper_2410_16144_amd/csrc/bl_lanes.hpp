@@ -39,6 +39,7 @@ struct AddOp { __device__ __forceinline__ float operator()(float a, float b) con
 struct MaxBitsOp {
     __device__ __forceinline__ float operator()(float a, float b) const { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }
 };
+struct MinOp { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
 struct MaxOp { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
 }  // namespace bl
