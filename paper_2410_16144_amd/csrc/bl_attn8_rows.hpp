@@ -272,7 +272,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                     x[u] = rows8_joined(s[n][u]) * ks[u] * unit[n];
                     if (masked && first + 4 * j + u >= limit[n]) x[u] = -INFINITY;
                 }
-                const float m_c = over_lanes<16>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), MaxOp());
+                float m_c = over_lanes<16>(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), MaxOp());
                 const float base = m_c == -INFINITY ? 0.0f : m_c;      // (a row that sees nothing of this chunk: no weights)
                 float w[4], sum = 0.0f;
 #pragma unroll
@@ -283,7 +283,15 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                 }
                 // the weights' unit: a power of two with which the chunk's largest one has 23 bits (22 where 23 would not fit three bytes)
                 const float w_max = over_lanes<16>(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), MaxOp());
-                const int exponent = max(__builtin_amdgcn_frexp_expf(w_max) - (__builtin_amdgcn_frexp_mantf(w_max) < kWeightMost ? 23 : 22), -120);
+                int exponent = __builtin_amdgcn_frexp_expf(w_max) - (__builtin_amdgcn_frexp_mantf(w_max) < kWeightMost ? 23 : 22);
+                if (__any(exponent < -100)) {              // (values of 1e-22 and less: relative to a score lower by 64 their unit is a normal number)
+                    const int up = exponent < -100 ? 64 : 0;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) w[u] = ldexpf(w[u], up);
+                    sum = ldexpf(sum, up);
+                    m_c -= (float)up;
+                    exponent += up;
+                }
                 const float per = ldexpf(1.0f, -exponent);
                 uint32_t bits[4];
 #pragma unroll

@@ -144,7 +144,7 @@ def test_a_large_value_that_loses_its_weight(dev, mods, form, factor):
 
 
 @pytest.mark.parametrize("form", [f for f in FORMS if FORMS[f][3] > 0])
-@pytest.mark.parametrize("values", [(-60, 60), (60, -60), (0, 0), (80, 80), (30, 20)])
+@pytest.mark.parametrize("values", [(-60, 60), (60, -60), (0, 0), (80, 80), (-100, -100), (30, 20)])
 @pytest.mark.parametrize("scores", [(0.0, 0.0), (-40.0, 60.0), (60.0, -40.0)])
 def test_values_and_scores_that_rise_and_fall_along_the_walk(dev, mods, form, values, scores):
     """Values from 2^a to 2^b, scores from c to d, evenly along the shared positions; the rows' own as the last of them."""
