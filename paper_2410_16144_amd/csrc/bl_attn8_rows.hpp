@@ -281,8 +281,15 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                     sum += p_j;
                     w[u] = p_j * vs[u];
                 }
+                if (masked && p.prompt) {                  // uniform; a later token's row may be anything, NaN and infinities included
+                    asm volatile("");                      // (a branch: else every chunk pays for it)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (first + 4 * j + u >= limit[n]) w[u] = 0.0f;
+                }
                 // the weights' unit: a power of two with which the chunk's largest one has 23 bits (22 where 23 would not fit three bytes)
-                const float w_max = over_lanes<16>(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), MaxOp());
+                const MaxBitsOp larger;                    // (of numbers without a sign, NaN above all)
+                const float w_max = over_lanes<16>(larger(larger(w[0], w[1]), larger(w[2], w[3])), larger);
                 int exponent = __builtin_amdgcn_frexp_expf(w_max) - (__builtin_amdgcn_frexp_mantf(w_max) < kWeightMost ? 23 : 22);
                 if (__any(exponent < -100)) {              // (values of 1e-22 and less: relative to a score lower by 64 their unit is a normal number)
                     const int up = exponent < -100 ? 64 : 0;
@@ -301,7 +308,7 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                 take[n] = __builtin_amdgcn_exp2f(m_c - ref);
                 run_m[n] = m_new;
                 run_l[n] = run_l[n] * keep[n] + sum * take[n];
-                take[n] = ldexpf(take[n], exponent);
+                take[n] = fmaf(w_max, 0.0f, ldexpf(take[n], exponent));   // (a weight that is not finite: NaN)
                 // byte k of the four words, side by side
                 const uint32_t low01 = __builtin_amdgcn_perm(bits[1], bits[0], 0x05010400u), low23 = __builtin_amdgcn_perm(bits[3], bits[2], 0x05010400u);
                 const uint32_t top01 = __builtin_amdgcn_perm(bits[1], bits[0], 0x0c0c0602u), top23 = __builtin_amdgcn_perm(bits[3], bits[2], 0x0c0c0602u);

@@ -321,12 +321,14 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         float sum = 0.0f;
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-            const f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
+            f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
             float pj[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const float at = x[4 * r4 + c];
-                pj[c] = __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -base));
+                const bool unseen = END && at == -INFINITY;   // (its scale may be anything, NaN included)
+                pj[c] = __builtin_amdgcn_exp2f(unseen ? at : fmaf(at, unit, -base));
+                if (unseen) vs[c] = 0.0f;
                 sum += pj[c];
             }
 #pragma unroll

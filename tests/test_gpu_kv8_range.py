@@ -38,6 +38,11 @@ class Case:
         self.kp, self.vp, self.k, self.v = (r.standard_normal((m, n, dim)).astype(np.float32) for m in (P, P, M, M))
         self.kp[..., 0] = self.k[..., 0] = 0
 
+    def copy(self):
+        other = Case.__new__(Case)
+        other.__dict__.update({k: v.copy() if isinstance(v, np.ndarray) else v for k, v in self.__dict__.items()})
+        return other
+
     def run(self, dec, dev):
         n, dim, P, M = self.n, self.dim, self.P, self.M
         flat = lambda x: _t(x.reshape(x.shape[0], -1), dev)  # noqa: E731
@@ -54,8 +59,9 @@ class Case:
             out = dec.Attention8(self.heads, own, flat(self.q), flat(self.k), flat(self.v), pos, table, prefix=past if P else None, prefix_len=P).launch()
         return out.cpu().numpy().astype(np.float64).reshape(M, self.heads, dim)
 
-    def check(self, dec, dev, rows=None):
-        got = self.run(dec, dev)
+    def check(self, dec, dev, rows=None, got=None, groups=None):
+        """Every row, or those of `rows`; got: outputs of a run with other rows that they do not see.  groups: key heads, or all."""
+        got = self.run(dec, dev) if got is None else got
         stored = []
         for past, new in ((self.kp, self.k), (self.vp, self.v)):
             x = np.concatenate([past, new])
@@ -67,6 +73,8 @@ class Case:
             see = list(range(self.P)) + ([self.P + m] if self.batch else list(range(self.P, self.P + m + 1)))
             for h in range(self.heads) if self.heads <= 16 else (0, 1, self.heads // 2 + 1, self.heads - 1):
                 g = h // (self.heads // self.n)
+                if groups is not None and g not in groups:
+                    continue
                 q, kk, vv, root = self.q[m, h].astype(np.float64), k[see, g], v[see, g], math.sqrt(self.dim)
                 s = kk @ q / root
                 p = np.exp(s - s.max())
@@ -183,3 +191,40 @@ def test_heads_of_zeros(dev, mods, form):
     c.check(mods[1], dev, _some(c))
     c.v[-1] = 0
     c.check(mods[1], dev, _some(c))
+
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if FORMS[f][4] > 1])
+@pytest.mark.parametrize("which,what", [("v", INF), ("v", -INF), ("v", NAN), ("k", INF), ("k", NAN), ("kv", NAN)])
+def test_rows_that_are_not_finite_and_not_seen(dev, mods, form, which, what):
+    """An element of the last token's row (of a batch: of the last sequence's): every other token's output is as it was."""
+    c = _make(form, 38000)
+    clean = c.copy()
+    for name in which:
+        getattr(c, name)[-1, :, 5] = what
+    last = c.M - 1
+    clean.check(mods[1], dev, [m for m in (_some(c) or range(c.M)) if m != last], got=c.run(mods[1], dev))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("which,what", [("v", INF), ("v", -INF)])
+def test_rows_that_are_not_finite_and_seen(dev, mods, form, which, what):
+    """An element of a key head's row: the output of every query that sees it is NaN, whatever weight it has; all others are as they were."""
+    c, dec = _make(form, 39000), mods[1]
+    for at, bias in ((0, 0.0), (c.P // 2, -300.0), (c.P - 1, 10.0), (c.P + c.M // 2, 0.0)):
+        if at < 0:
+            continue
+        own = at - c.P
+        row = lambda case, name: getattr(case, name + "p")[at] if own < 0 else getattr(case, name)[own]  # noqa: B023, E731
+        if bias:
+            row(c, "k")[:, 0] = _bias(c.dim, bias)
+        bad = c.copy()
+        for name in which:
+            row(bad, name)[0, 5] = what
+        got = bad.run(dec, dev)
+        sees = [m for m in (_some(c) or range(c.M)) if 0 <= m < c.M and (own < 0 or (m == own if c.batch else m >= own))]
+        assert np.isnan(got[sees][:, :c.heads // c.n]).all()
+        c.check(dec, dev, [m for m in (_some(c) or range(c.M)) if m not in sees], got=got)
+        c.check(dec, dev, sees, got=got, groups=range(1, c.n))
