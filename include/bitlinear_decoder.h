@@ -266,8 +266,8 @@ bl_status bl_attn_prefill(const bl_attn_prefill_args *args, void *stream);
 /*
  * The 8-bit key/value cache.  A position's key and value are stored per key head as head_dim int8 codes and one fp32 scale, quantized as
  * bl_quant_act quantizes a row: amax = max|x|, inv = 127 / amax, code = clip(round_half_even(x * inv)), scale = amax / 127; a head
- * whose inv is not finite: codes 0, scale 0.  Half of the bf16 cache's bytes, several sequences per call, and key heads that several query
- * heads share.
+ * whose inv is infinite: codes 0, scale 0; a head with a NaN or an infinity: codes 0, scale NaN, and NaN is what reads as its row and what comes of
+ * every query that sees it.  Half of the bf16 cache's bytes, several sequences per call, and key heads that several query heads share.
  *   n_heads      key heads; head_dim a multiple of 4 (4 .. BL_ATTN_MAX_HEAD_DIM)
  *   k_codes_dev, v_codes_dev   sequences * bl_kv8_code_bytes(n_heads, head_dim, max_pos) bytes each, 16-byte aligned
  *   k_scale_dev, v_scale_dev   sequences * bl_kv8_scale_count(n_heads, max_pos) floats each, 16-byte aligned

@@ -169,8 +169,8 @@ __device__ __forceinline__ void rows8_walk(const Attn8Args& p, const Attn8Walk& 
                 for (int m = 0; m < kPairs; ++m) {
                     const int i = lane + 64 * m;
                     if (i < half) {
-                        dst[i] = (uint8_t)kv8_code(lo[n][m], inv);
-                        dst[i + half] = (uint8_t)kv8_code(hi[n][m], inv);
+                        dst[i] = kv8_finite(amax) ? (uint8_t)kv8_code(lo[n][m], inv) : 0;
+                        dst[i + half] = kv8_finite(amax) ? (uint8_t)kv8_code(hi[n][m], inv) : 0;
                     }
                 }
                 for (int e = d + lane; e < kDims; e += kWave) dst[e] = 0;

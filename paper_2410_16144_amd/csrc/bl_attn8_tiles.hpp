@@ -216,15 +216,15 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     // A half's scales go through LDS, lanes 0-31 the keys', lanes 32-63 the values', when its keys have arrived.
     const auto scales_in = [&](int i) {
         const int first = half_of(i) * kTiles8Keys;
-        const float own = first + l32 >= keys ? 0.0f : scale;   // (what lies behind the last row may be anything)
-        const float v_max = wave_max(g ? own : 0.0f);
+        // (what lies behind the last row may be anything, a row's scale a NaN)
+        const float v_max = wave_max(g && first + l32 < keys && scale < INFINITY ? scale : 0.0f);
         next_room = kTiles8Far;
-        if (v_max > 0.0f) {
-            const int e = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(v_max));
+        if (__float_as_uint(v_max) != 0) {      // uniform
+            const int e = exponent_above(v_max);
             if (e > next_e) next_e = e + kTiles8Above;
             next_room = min(kTiles8Top - kTiles8Scale + next_e - e, kTiles8Far);
         }
-        shared.scale[wave][i & 1][lane] = g ? ldexpf(own, kTiles8Scale - next_e) : own;
+        shared.scale[wave][i & 1][lane] = g ? ldexpf(scale, kTiles8Scale - next_e) : scale;
         __builtin_amdgcn_wave_barrier();        // (a wave's LDS operations are performed in order)
     };
     const auto scores_low_high = [&] {

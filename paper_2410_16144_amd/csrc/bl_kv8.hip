@@ -90,9 +90,13 @@ __global__ __launch_bounds__(kWriteThreads<L>) void kv8_write_kernel(const Write
                     u[i] = f * c - g * s;
                     w[i] = f * s + g * c;
                 }
-                if (mine) amax = fmaxf(amax, fmaxf(fabsf(u[i]), fabsf(w[i])));
+                if (mine) amax = MaxBitsOp()(amax, MaxBitsOp()(fabsf(u[i]), fabsf(w[i])));
             }
-            amax = over_lanes<L>(amax, MaxOp());
+            amax = over_lanes<L>(amax, MaxBitsOp());
+            if (!kv8_finite(amax)) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) u[i] = w[i] = 0.0f;
+            }
             float inv, scale;
             kv8_scales(amax, inv, scale);
             if (l == 0 && row >= lo && row < hi) (value ? p.cache.v_scale : p.cache.k_scale)[head * p.cache.head_scales + row] = scale;

@@ -49,13 +49,16 @@ inline Kv8 kv8_of(const ::bl_kv8_cache& c, int64_t sequence) {
     return r;
 }
 
-// The quantizer's scalars of a row (bl_quant_act's: one division each; a row whose inv is not finite is a row of zeros).
+// The quantizer's scalars of a row (bl_quant_act's: one division each; a row whose inv is infinite is a row of zeros).  amax with MaxBitsOp:
+// of a row with a NaN or an infinity it is not finite; the row is one of zeros then, too, and its scale a NaN, so that whoever reads it sees that.
+__device__ __forceinline__ bool kv8_finite(float amax) { return amax < INFINITY; }
 __device__ __forceinline__ void kv8_scales(float amax, float& inv, float& scale) {
     inv = 127.0f / amax;
     scale = amax / 127.0f;
-    if (!(fabsf(inv) < INFINITY)) {
+    if (!(inv < INFINITY)) inv = scale = 0.0f;
+    if (!kv8_finite(amax)) {
         inv = 0.0f;
-        scale = 0.0f;
+        scale = __builtin_nanf("");
     }
 }
 __device__ __forceinline__ int kv8_code(float x, float inv) { return (int)fminf(fmaxf(rintf(x * inv), -128.0f), 127.0f); }

@@ -209,7 +209,7 @@ def test_rows_that_are_not_finite_and_not_seen(dev, mods, form, which, what):
 
 
 @pytest.mark.parametrize("form", list(FORMS))
-@pytest.mark.parametrize("which,what", [("v", INF), ("v", -INF)])
+@pytest.mark.parametrize("which,what", [("v", INF), ("v", -INF), ("v", NAN), ("k", INF), ("k", -INF), ("k", NAN)])
 def test_rows_that_are_not_finite_and_seen(dev, mods, form, which, what):
     """An element of a key head's row: the output of every query that sees it is NaN, whatever weight it has; all others are as they were."""
     c, dec = _make(form, 39000), mods[1]
@@ -228,3 +228,51 @@ def test_rows_that_are_not_finite_and_seen(dev, mods, form, which, what):
         assert np.isnan(got[sees][:, :c.heads // c.n]).all()
         c.check(dec, dev, [m for m in (_some(c) or range(c.M)) if m not in sees], got=got)
         c.check(dec, dev, sees, got=got, groups=range(1, c.n))
+
+
+@pytest.mark.parametrize("dim", [64, 96, 100, 252])
+@pytest.mark.parametrize("what", [INF, -INF, NAN])
+def test_every_writer_stores_a_row_that_is_not_finite_alike(dev, mods, dim, what):
+    """Codes 0 and a scale of NaN, through write (fp32 and bf16), a prompt of few rows and of many, and a token; all other heads and rows
+    as without it.  Read back, the row is NaN."""
+    B, dec, ops = mods
+    n, M, at = 2, 41, 17
+    r = _rng(40000 + dim)
+    k, v = (r.standard_normal((M, n, dim)).astype(np.float32) for _ in range(2))
+    k, v = (torch.from_numpy(x).bfloat16().float().numpy() for x in (k, v))
+    flat = lambda x: _t(x.reshape(len(x), -1), dev)  # noqa: E731
+    table = torch.rand((M, dim // 2, 2), device=dev, generator=torch.Generator(device=dev).manual_seed(1)) + 0.5
+    for e in (0, dim // 2 - 1, dim - 1):
+        bad_k, bad_v = k.copy(), v.copy()
+        bad_k[at, 0, e] = bad_v[at, 1, e] = what
+        caches = [dec.KvCache8(n, dim, M, dev) for _ in range(5)]
+        clean = dec.KvCache8(n, dim, M, dev)
+        clean.write(flat(k), flat(v), 0, table)
+        caches[0].write(flat(bad_k), flat(bad_v), 0, table)
+        caches[1].write(flat(bad_k).bfloat16(), flat(bad_v).bfloat16(), 0, table)
+        dec.attn_prefill8(flat(bad_k), flat(bad_k), flat(bad_v), caches[2], table, 0)
+        for first in range(0, M, 6):
+            rows = slice(first, min(first + 6, M))
+            dec.attn_prefill8(flat(bad_k[rows]), flat(bad_k[rows]), flat(bad_v[rows]), caches[3], table, first)
+        for m in range(M):
+            x, y = flat(bad_k[m:m + 1]), flat(bad_v[m:m + 1])
+            dec.Attention8(n, caches[4], x, x, y, torch.tensor([m], dtype=torch.int32, device=dev), table).launch()
+        for c in caches:
+            for name, head in (("k", 0), ("v", 1)):
+                scale, base = getattr(c, name + "_scale")[0], getattr(clean, name + "_scale")[0]
+                assert bool(torch.isnan(scale[head, at])) and int(torch.isnan(scale).sum()) == 1
+                keep = torch.ones_like(scale, dtype=torch.bool)
+                keep[head, at] = False
+                assert torch.equal(scale[keep], base[keep])
+                assert torch.equal(getattr(c, name + "_codes"), getattr(caches[0], name + "_codes"))
+            for dtype in (torch.float32, torch.bfloat16):
+                for got, base, head in zip(c.read(0, M, dtype), clean.read(0, M, dtype), (0, 1)):
+                    got, base = got.view(M, n, dim), base.view(M, n, dim).clone()
+                    assert bool(torch.isnan(got[at, head]).all())
+                    base[at, head] = got[at, head] = 0
+                    assert torch.equal(got, base)
+        places = caches[0].k_codes[0, 0].view(-1)
+        S = (dim + 15) // 16 * 16
+        e_all = np.arange(S)
+        key_at = 4096 * (e_all // 64) + (16 * (at % 4) + at // 4) * np.minimum(64, S - 64 * (e_all // 64)) + e_all % 64
+        assert not places[torch.from_numpy(key_at).to(dev)].any() and not caches[0].v_codes[0, 1].view(-1)[torch.from_numpy(64 * e_all + at).to(dev)].any()
