@@ -646,10 +646,20 @@ bl_status bl_attn8_decode(const bl_attn8_args* a, void* stream) {
         if (s != BL_OK) return s;
         if (a->prefix.n_heads != a->cache.n_heads || a->prefix.head_dim != a->cache.head_dim || a->prefix_len > a->prefix.max_pos) return BL_ERR_SHAPE;
         // the sequences write their caches while others still read the prefix
-        const int64_t own = (int64_t)bl_kv8_code_bytes(a->cache.n_heads, a->cache.head_dim, a->cache.max_pos) * a->cache.sequences;
-        const int64_t shared = (int64_t)bl_kv8_code_bytes(a->prefix.n_heads, a->prefix.head_dim, a->prefix.max_pos);
-        const auto meet = [&](const int8_t* x, const int8_t* y) { return x < y + shared && y < x + own; };
-        if (meet(a->cache.k_codes_dev, a->prefix.k_codes_dev) || meet(a->cache.v_codes_dev, a->prefix.v_codes_dev)) return BL_ERR_SHAPE;
+        struct Range { uintptr_t at; uint64_t bytes; };
+        const auto ranges = [](const bl_kv8_cache& c, uint64_t sequences, Range (&r)[4]) {
+            const uint64_t codes = bl_kv8_code_bytes(c.n_heads, c.head_dim, c.max_pos) * sequences, scales = bl_kv8_scale_count(c.n_heads, c.max_pos) * 4 * sequences;
+            r[0] = {reinterpret_cast<uintptr_t>(c.k_codes_dev), codes};
+            r[1] = {reinterpret_cast<uintptr_t>(c.v_codes_dev), codes};
+            r[2] = {reinterpret_cast<uintptr_t>(c.k_scale_dev), scales};
+            r[3] = {reinterpret_cast<uintptr_t>(c.v_scale_dev), scales};
+        };
+        Range own[4], shared[4];
+        ranges(a->cache, a->cache.sequences, own);
+        ranges(a->prefix, 1, shared);
+        for (const Range& x : own)
+            for (const Range& y : shared)
+                if (x.at < y.at + y.bytes && y.at < x.at + x.bytes) return BL_ERR_SHAPE;
     }
     if (!aligned(a->q_lin_dev, 4) || !aligned(a->k_lin_dev, 4) || !aligned(a->v_lin_dev, 4) || !aligned(a->pos_dev, 4) ||
         !aligned(a->rope_table_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))

@@ -90,6 +90,24 @@ def test_refusals_of_the_token_attention():
     assert call(prefix=_cache(v_scale_dev=P + 4), prefix_len=5) == B.BL_ERR_ALIGN
 
 
+def test_a_prefix_has_memory_of_its_own():
+    """None of its codes and scales may lie in any of the sequences' buffers, of whatever kind: they are written while it is read."""
+    own, far = _cache(k_codes_dev=1 << 32, v_codes_dev=2 << 32, k_scale_dev=3 << 32, v_scale_dev=4 << 32), [(i + 5) << 32 for i in range(4)]
+    names = [f[0] for f in B.Kv8Cache._fields_[:4]]
+    codes, scales = B.bl_kv8_code_bytes(4, 64, 100), 4 * B.bl_kv8_scale_count(4, 100)
+
+    def call(prefix, q=P):
+        return _st(B.bl_attn8_decode, B.make_attn8_args(q, P, P, P, P, P, P, own, 8, prefix, 5))
+    assert call(_cache(**dict(zip(names, far))), q=P + 2) == B.BL_ERR_ALIGN          # (nothing wrong with this one)
+    for i, name in enumerate(names):
+        for j in range(4):
+            mine, theirs = (scales if i >= 2 else codes), 2 * (scales if j >= 2 else codes)
+            for at in (0, theirs - 16, 16 - mine):
+                assert call(_cache(**dict(zip(names, far), **{name: ((j + 1) << 32) + at}))) == B.BL_ERR_SHAPE, (name, j, at)
+            for at in (theirs, -mine):
+                assert call(_cache(**dict(zip(names, far), **{name: ((j + 1) << 32) + at})), q=P + 2) == B.BL_ERR_ALIGN, (name, j, at)
+
+
 def test_refusals_of_the_prompt_attention():
     def call(cache=None, n_q=8, sequence=0, pos0=10, M=20, **kw):
         a = dict(q=P, k=P, v=P, table=P, out=P, scratch=P)
