@@ -352,8 +352,9 @@ bl_status bl_kv8_read(const bl_kv8_read_args *args, void *stream);
  * Arithmetic: the queries enter as 24-bit fixed-point numbers (relative to their row's largest value), the codes as they are, with exact integer
  * sums.  A softmax weight times its value's scale enters as a 23-bit fixed-point number relative to its row's largest one in a chunk of 64 positions
  * (exact sums again), or, where more than eight rows share a prefix, as the sum of two f16 numbers (22 bits, and no finer than 2^-28 of the row's
- * largest).  Values that a row does not see, or gives no weight, have no part in either.  Everything else is fp32.  A query with a NaN or an infinity
- * makes its own row NaN.
+ * largest).  Values that a row does not see, or gives no weight, have no part in either.  Everything else is fp32.  Queries, keys and values may be
+ * as large as 1e28 and as small as 1e-28 (a query whose largest value is below 2.5e-32 counts as zero; beyond 1e30 sums may overflow).  A query with a
+ * NaN or an infinity makes its own row NaN.
  * Up to three launches: up to eight rows (sequence, query head) of a key head take one, in which the workgroups of a row leave their figures in
  * scratch_dev and the last one adds them up; more rows behind a prefix take the prefix in tiles of 32, many sequences' own rows in a launch of
  * their own, and a last one adds the figures up.  Nobody waits for anybody, and figures are added in a fixed order: a call repeated gives the same bits.

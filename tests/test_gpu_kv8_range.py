@@ -193,6 +193,16 @@ def test_heads_of_zeros(dev, mods, form):
     c.check(mods[1], dev, _some(c))
 
 
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("q,k,v", [(-92, 92, 0), (92, -92, 0), (0, 0, 93), (-40, 40, -93), (-95, 90, 90)])
+def test_queries_keys_and_values_of_extreme_sizes(dev, mods, form, q, k, v):
+    """All of them by powers of two that leave the scores as they are, or small: the outputs are the same but for the values' power."""
+    c = _make(form, 41000)
+    c.q, c.k, c.v = c.q * np.float32(2.0 ** q), c.k * np.float32(2.0 ** k), c.v * np.float32(2.0 ** v)
+    c.kp, c.vp = c.kp * np.float32(2.0 ** k), c.vp * np.float32(2.0 ** v)
+    c.check(mods[1], dev, _some(c))
+
+
 NAN, INF = float("nan"), float("inf")
 
 
