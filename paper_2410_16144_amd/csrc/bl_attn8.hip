@@ -35,6 +35,8 @@ hipError_t launch_form(const Attn8Args& p, int wgs, hipStream_t s) {
 template <int KB>
 hipError_t launch_block(const Attn8Args& p, const Attn8Plan& plan, bool stream, int wgs, hipStream_t s) {
     static_assert(kRows8Waves == 8 && kRows8ManyWaves == 2 && kRows8FewWaves == 4, "waves as planned");
+    // Rows in eights and sixteens always by streaming loads: half the kernels.  Ordinary and streaming, us: 64 heads on 8 at 300 positions 7.8 and 8.1, at
+    // 8000 (16 MB) 12.7 and 13.5, at 30 000 (61 MB) 21.7 and 20.5; 64 on 4 at 20 000 (20 MB) 22.1 and 22.9.
     if (plan.block == 8) return plan.waves == 8 ? launch_form<KB, 2, 8, true>(p, wgs, s) : launch_form<KB, 2, 4, true>(p, wgs, s);
     if (plan.block == 16) {
         if constexpr (KB <= 2) {
@@ -48,7 +50,7 @@ hipError_t launch_block(const Attn8Args& p, const Attn8Plan& plan, bool stream, 
 
 hipError_t launch_rows(const Attn8Args& p, const Attn8Plan& plan, int wgs, hipStream_t s) {
     // Caches of 32 MiB and more (the dies' L2s together) by streaming loads.  32 heads of 128, ordinary and streaming, us: 500 positions 6.9 and 7.8, 4000
-    // (33 MB) 12.7 and 12.9, 8000 19.2 and 17.6, 30 000 52.2 and 46.7.
+    // (33 MB) 12.7 and 12.9, 8000 19.2 and 17.6, 30 000 52.2 and 46.7.  (By the caches' size, which the host knows, not by the positions.)
     const int64_t positions = p.shared_wgs > 0 ? (p.prompt ? p.pos0 + p.tokens : p.shared_len) : 0;
     const bool stream = 2 * (positions + (int64_t)p.tokens * p.max_pos) * p.n_heads * p.size >= 32 << 20;
     static_assert(BL_ATTN_MAX_HEAD_DIM == 256, "head sizes up to four blocks of 64");

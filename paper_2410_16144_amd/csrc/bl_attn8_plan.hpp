@@ -29,7 +29,8 @@ constexpr int kAttn8Waves = 2048;         // that a launch aims at: two on each 
 constexpr int kAttn8SharedWaves = 1024;
 // A short walk that meets nobody else is not split: the meeting (figures performed, tickets, figures read: three trips to memory) takes 3.6 us, a
 // set of 512 positions in one compute unit 1.0 us with a head size of 64 and 1.8 with 128.  One workgroup per head and one per set, us: 32 heads
-// of 128 at 1000 positions 9.3 and 10.5, at 2000 12.9 and 10.9; 12 of 64 at 1000 6.7 and 9.0, at 2000 8.7 and 9.3.
+// of 128 at 1000 positions 9.3 and 10.5, at 2000 12.9 and 10.9; 12 of 64 at 1000 6.7 and 9.0, at 2000 8.7 and 9.3.  (By the cache's size, which the host
+// knows, not by the position: at 1000 of 8192 positions a token's walk is one workgroup per set.)
 constexpr int kRows8Together = 256 << 10;   // bytes of codes
 
 // What splitting a prompt's walk in tiles takes and saves, in tenths of a microsecond (32 heads of 128): a set of 128 positions with one wave on a SIMD and

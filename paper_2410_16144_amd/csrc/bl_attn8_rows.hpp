@@ -13,7 +13,7 @@
 //
 // A wave's next keys are requested when this chunk's scores are formed, its next values when the weighted values are: half a chunk is always
 // on its way.  Memory bounds a long walk (32 heads of 128, rows in fours: every further byte at 6.96 TB/s; 64 heads on 8 at 100 000 positions, in
-// eights: 41.7 us, 4.9 TB/s), waiting a short one: 17 positions of 12 heads of 64 take 5.2 us, a split walk 8 to 9 beside its bytes (start 2.1,
+// eights: 41.7 us, 4.9 TB/s), waiting a short one: 17 positions of 12 heads of 64 take 5.2 us (in a cache of 18 rows and of 8192), a split walk 8 to 9 beside its bytes (start 2.1,
 // position and queries 1.4, figures out 0.9, ticket 1.0, figures in 2.3).  The token's own row is quantized by the workgroup whose walk ends with it
 // and put into the operands from LDS.
 #pragma once

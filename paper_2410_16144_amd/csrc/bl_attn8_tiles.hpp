@@ -15,7 +15,7 @@
 // weight w = p s^v as the sum of two f16 numbers (22 bits) -- relative to the row's own largest weight, see kTiles8Top.  fp32 accumulation
 // throughout.
 //
-// A half is 28 matrix instructions (900 cycles) and some 340 vector instructions (1400): the vector ALU bounds a long walk, at 1.0 us per half and
+// A half is 28 matrix instructions (900 cycles) and some 290 vector instructions (1400): the vector ALU bounds a long walk, at 1.0 us per half and
 // SIMD with two waves there (cycles with a vector instruction 67 %, with a matrix one 43 %).  A half's scores are formed beside the weights and
 // outputs of the half before, so that either pipe has work in one wave's stream; by itself that changed nothing (512 tokens behind 16 000, 32 heads of 128:
 // 285 us, in turn 281), with the wave's priority raised while the products are formed 270: the other wave then has the phase that this one has not.  Head
