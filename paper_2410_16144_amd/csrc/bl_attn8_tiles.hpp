@@ -28,17 +28,19 @@ namespace bl {
 constexpr int kTiles8Keys = 32, kTiles8Waves = 4, kTiles8Threads = 64 * kTiles8Waves;
 static_assert(1 << kTiles8Set == kTiles8Waves * kTiles8Keys, "a half chunk per wave");
 // What keeps a row's weights within f16.  A row has a reference score, p = exp2(score - reference), and a wave an exponent E above those of all
-// value scales that it has met; weights, and with them the outputs, are w = p s^v 2^(60 - E).  The reference is set so that the row's largest weight so far
+// value scales that it has met; weights, and with them the outputs, are w = p s^v 2^(9 - E).  The reference is set so that the row's largest weight so far
 // is between 2^6 and 2^7 (2^3 at least, see alike): weights down to 2^-3 then have 22 bits, smaller ones are rounded to 2^-25, 2^-28 of the largest.
 // By the largest score alone, a value that a row does not see, or gives no weight, would take the bits of those that it does: E is all rows'.  The
 // reference is looked at again where score and scales of a half would allow a weight of 2^15, and rises if a weight of the row's own is above 2^7
 // by then: nearly every half has a new maximum for one of 32 queries, and the 64 products that rescale the outputs are a sixth of a half's
-// instructions.  It is never further than 2^96 below a half's largest score, so that 4 million sums of p stay below 2^119: a row that weighs values
-// 2^-140 times as large as what others see has all bits of them.  Nor is it more than 2^53 above one: p down to 2^-73 are in the sums.
-constexpr int kTiles8Top = 15, kTiles8Set0 = 7, kTiles8Far = 96;
-constexpr int kTiles8Scale = 60;           // 2^60: between what the sums' range leaves for large p and for small ones
+// instructions.  It is at most 118 below a half's largest score (a half's sum of p stays below 2^122, and the sums of 4 million positions, in units of
+// 2^24, below 2^116): a row that weighs values 2^-120 times as large as what others see has all bits of them.  Where the scales are alike it is the
+// largest score itself, and the exponents of what weighs much are small numbers (with 9 + 51 for the 9, their rounding alone gave 5e-7 of the output).
+constexpr int kTiles8Top = 15, kTiles8Set0 = 7, kTiles8Far = 118;
 constexpr int kTiles8Above = 2;            // E is set so far above a scale's exponent: the next, slightly larger ones leave it (2048 tokens 108.8 and 106.7 us)
-constexpr int kTiles8Sum = 100;            // a sum of p above 2^100 is not scaled up any more
+constexpr int kTiles8Scale = kTiles8Set0 + kTiles8Above;
+constexpr int kTiles8Unit = 24;            // sums of p are in units of 2^24
+constexpr int kTiles8Sum = 100;            // ... and above 2^100 of them not scaled up any more
 constexpr int kTiles8NoScale = -140;       // below every scale's exponent
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -300,7 +302,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
             alike = false;
             const float m_new = top > run_m + room ? fmaxf(run_m, top + (float)max(w_exp - kTiles8Set0, -kTiles8Far)) : run_m;
             const float apart = run_m - m_new;
-            const int far = apart < -64.0f ? 64 : 0;       // (2^-126 is the least that exp2 gives; sums may be of 2^100)
+            const int far = apart < -64.0f ? 64 : 0;       // (2^-126 is the least that exp2 gives; sums may be as large)
             const float f = m_new == run_m ? 1.0f : __builtin_amdgcn_exp2f(apart + (float)far);
             const float fo = ldexpf(f, left - far);
 #pragma unroll
@@ -341,7 +343,7 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
                 w_lo[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, lo);
             }
         }
-        run_l += sum;
+        run_l = fmaf(sum, 1.0f / (1 << kTiles8Unit), run_l);
         if constexpr (NEXT) {
             __builtin_amdgcn_sched_barrier(0);
             scores_middle();
@@ -387,9 +389,9 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     // ---- the waves meet: references and sums first -- the references moved so that a sum is one of 0.5 to 1: by how much a wave has of a row --
     // then the outputs, each scaled by its own factor
     run_l = over_blocks<32>(run_l, AddOp());
-    const int l_e = exponent_above(run_l);
+    const int l_own = exponent_above(run_l), l_e = l_own + kTiles8Unit;
     run_m += (float)l_e;
-    if (g == 0) shared.ml[wave][l32] = make_float2(run_m, ldexpf(run_l, -l_e));
+    if (g == 0) shared.ml[wave][l32] = make_float2(run_m, ldexpf(run_l, -l_own));
     __syncthreads();
     const auto figure = [&](int at_tile, int r) {
         float m = -INFINITY, l = 0.0f;
