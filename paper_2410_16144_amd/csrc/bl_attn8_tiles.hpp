@@ -218,15 +218,20 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
     // A half's scales go through LDS, lanes 0-31 the keys', lanes 32-63 the values', when its keys have arrived.
     const auto scales_in = [&](int i) {
         const int first = half_of(i) * kTiles8Keys;
-        // (what lies behind the last row may be anything, a row's scale a NaN)
-        const float v_max = wave_max(g && first + l32 < keys && scale < INFINITY ? scale : 0.0f);
+        // What lies behind the last row may be anything.  A value's scale that is not finite becomes its key's NaN: that makes NaN of the queries that
+        // see the row, and of no others, whose weight times it would be.
+        const bool there = first + l32 < keys, finite = scale < INFINITY;
+        const float own = g && there && finite ? scale : 0.0f, v_max = wave_max(own);
+        const uint32_t bad = (uint32_t)(__ballot(there && !finite) >> 32);   // uniform
         next_room = kTiles8Far;
         if (__float_as_uint(v_max) != 0) {      // uniform
             const int e = exponent_above(v_max);
             if (e > next_e) next_e = e + kTiles8Above;
             next_room = min(kTiles8Top - kTiles8Scale + next_e - e, kTiles8Far);
         }
-        shared.scale[wave][i & 1][lane] = g ? ldexpf(scale, kTiles8Scale - next_e) : scale;
+        float k_scale = scale;
+        if (bad != 0 && (bad >> l32 & 1)) k_scale = __builtin_nanf("");
+        shared.scale[wave][i & 1][lane] = g ? ldexpf(own, kTiles8Scale - next_e) : k_scale;
         __builtin_amdgcn_wave_barrier();        // (a wave's LDS operations are performed in order)
     };
     const auto scores_low_high = [&] {
@@ -323,23 +328,24 @@ __device__ __forceinline__ void tiles8_walk(const Attn8Args& p, const Attn8Walk&
         float sum = 0.0f;
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-            f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
-            float pj[4];
+            const f32x4 vs = *reinterpret_cast<const f32x4*>(scales_of + kTiles8Keys + 16 * g + 4 * r4);
+            float w[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const float at = x[4 * r4 + c];
-                const bool unseen = END && at == -INFINITY;   // (its scale may be anything, NaN included)
-                pj[c] = __builtin_amdgcn_exp2f(unseen ? at : fmaf(at, unit, -base));
-                if (unseen) vs[c] = 0.0f;
-                sum += pj[c];
+                const float pj = __builtin_amdgcn_exp2f(END && at == -INFINITY ? at : fmaf(at, unit, -base));
+                sum += pj;
+                w[c] = pj * vs[c];
             }
 #pragma unroll
-            for (int c = 0; c < 4; c += 2) {               // a product's f16 number, and what it leaves
-                f16x2 hi = {(_Float16)fmaf(pj[c], vs[c], 0.0f), (_Float16)fmaf(pj[c + 1], vs[c + 1], 0.0f)};
-                asm("" : "+v"(hi));                        // (one register from here on: else the second number is formed twice)
-                const f32x2 rest = {fmaf(pj[c], vs[c], -(float)hi[0]), fmaf(pj[c + 1], vs[c + 1], -(float)hi[1])};
+            for (int c = 0; c < 4; c += 2) {
+                const f16x2 hi = __builtin_convertvector((f32x2{w[c], w[c + 1]}), f16x2);
+                const uint32_t both = __builtin_bit_cast(uint32_t, hi);
+                f32x2 rest;                                // what the first parts leave: w - hi (exact)
+                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(rest[0]) : "v"(both), "v"(w[c]));
+                asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(rest[1]) : "v"(both), "v"(w[c + 1]));
                 const f16x2 lo = __builtin_convertvector(rest, f16x2);
-                w_hi[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, hi);
+                w_hi[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = both;
                 w_lo[r4 >> 1][2 * (r4 & 1) + (c >> 1)] = __builtin_bit_cast(uint32_t, lo);
             }
         }
