@@ -358,7 +358,8 @@ bl_status bl_kv8_read(const bl_kv8_read_args *args, void *stream);
  * Up to three launches: up to eight rows (sequence, query head) of a key head take one, in which the workgroups of a row leave their figures in
  * scratch_dev and the last one adds them up; more rows behind a prefix take the prefix in tiles of 32, many sequences' own rows in a launch of
  * their own, and a last one adds the figures up.  Nobody waits for anybody, and figures are added in a fixed order: a call repeated gives the same bits.
- * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache.n_heads, a prefix of another shape or in the sequences' memory),
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache.n_heads, a prefix of another shape or in the sequences' memory, a
+ *         batch that needs 2^32 threads),
  *         BL_ERR_ALIGN, BL_ERR_HIP.
  */
 typedef struct bl_attn8_args {
@@ -389,7 +390,7 @@ bl_status bl_attn8_decode(const bl_attn8_args *args, void *stream);
  *   out_dev      [M, n_q_heads * head_dim] fp32
  *   scratch_dev  bl_attn8_prefill_scratch_bytes(...) bytes, 16-byte aligned, contents free
  * 0 <= pos0, pos0 + M <= max_pos, 1 <= M <= 65535.
- * Errors: BL_ERR_NULL, BL_ERR_SHAPE, BL_ERR_ALIGN, BL_ERR_HIP.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also a prompt that needs 2^32 threads), BL_ERR_ALIGN, BL_ERR_HIP.
  */
 typedef struct bl_attn8_prefill_args {
     const float        *q_lin_dev;

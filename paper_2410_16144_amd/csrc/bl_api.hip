@@ -622,6 +622,9 @@ bl_status bl_kv8_read(const bl_kv8_read_args* a, void* stream) {
     return hip_status(bl::launch_kv8_read(*a, static_cast<hipStream_t>(stream)));
 }
 
+// (a batch or prompt too large for a launch: seen ahead of the first one)
+static bl_status attn8_status(hipError_t e) { return e == hipErrorInvalidConfiguration ? BL_ERR_SHAPE : hip_status(e); }
+
 static bool attn8_heads_ok(int32_t n_q_heads, int32_t n_heads) {
     return n_heads >= 1 && n_q_heads >= 1 && n_q_heads <= 65535 && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_ATTN8_MAX_GROUP;
 }
@@ -665,7 +668,7 @@ bl_status bl_attn8_decode(const bl_attn8_args* a, void* stream) {
         !aligned(a->rope_table_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
         return BL_ERR_ALIGN;
     drop_stale_hip_error();
-    return hip_status(bl::launch_attn8_decode(*a, static_cast<hipStream_t>(stream)));
+    return attn8_status(bl::launch_attn8_decode(*a, static_cast<hipStream_t>(stream)));
 }
 
 static bool attn8_prefill_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M) {
@@ -688,7 +691,7 @@ bl_status bl_attn8_prefill(const bl_attn8_prefill_args* a, void* stream) {
         !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
         return BL_ERR_ALIGN;
     drop_stale_hip_error();
-    return hip_status(bl::launch_attn8_prefill(*a, static_cast<hipStream_t>(stream)));
+    return attn8_status(bl::launch_attn8_prefill(*a, static_cast<hipStream_t>(stream)));
 }
 
 bl_status bl_pos_advance(int32_t* pos_dev, void* stream) {

@@ -72,7 +72,6 @@ hipError_t launch(Attn8Args& p, const Attn8Plan& plan, void* scratch, hipStream_
     p.shared_set = plan.shared_set; p.own_set = plan.own_set;
     p.shared_splits = plan.shared_splits; p.shared_blocks = plan.shared_blocks; p.shared_units = (int32_t)plan.shared_units; p.strips = plan.strips;
     p.own_splits = plan.own_splits; p.own_blocks = plan.own_blocks;
-    if (plan.shared_wgs + plan.own_wgs > INT32_MAX) return hipErrorInvalidValue;
     p.shared_wgs = (int32_t)plan.shared_wgs;
     const int wgs = (int)(plan.shared_wgs + plan.own_wgs);
     p.by_heads = divider(p.n_heads); p.by_group = divider(p.group); p.by_half = divider(p.head_dim / 2); p.by_tokens = divider(p.tokens);
@@ -111,7 +110,8 @@ hipError_t launch_attn8_decode(const ::bl_attn8_args& a, hipStream_t s) {
     p.tokens = a.cache.sequences; p.shared_len = a.prefix_len; p.max_pos = a.cache.max_pos;
     p.own_codes = p.own.head_bytes * p.n_heads;
     p.own_scales = p.own.head_scales * p.n_heads;
-    return launch(p, attn8_plan(p.n_heads, p.group, p.tokens, p.shared_len, p.max_pos, kv8_size(p.head_dim)), a.scratch_dev, s);
+    const Attn8Plan plan = attn8_plan(p.n_heads, p.group, p.tokens, p.shared_len, p.max_pos, kv8_size(p.head_dim));
+    return plan.launchable() ? launch(p, plan, a.scratch_dev, s) : hipErrorInvalidConfiguration;
 }
 
 int64_t attn8_prefill_scratch_bytes(int n_heads, int group, int head_dim, int pos0, int M) {
@@ -127,6 +127,7 @@ hipError_t launch_attn8_prefill(const ::bl_attn8_prefill_args& a, hipStream_t s)
     p.n_heads = a.cache.n_heads; p.group = a.n_q_heads / a.cache.n_heads; p.head_dim = a.cache.head_dim;
     p.tokens = a.M; p.prompt = 1; p.pos0 = a.pos0;
     const Attn8Plan plan = prompt_plan(p.n_heads, p.group, p.head_dim, a.pos0, a.M);
+    if (!plan.launchable()) return hipErrorInvalidConfiguration;
     const int64_t counters = plan.meets() ? attn8_counters(p.n_heads, (int64_t)a.M * p.group) : 0;
     const ::bl_kv8_write_args w{&a.cache, a.k_lin_dev, a.v_lin_dev, a.rope_table_dev, (int64_t)p.n_heads * p.head_dim, BL_F32, a.sequence, a.pos0, a.M};
     const hipError_t e = launch_kv8_write(w, static_cast<uint32_t*>(a.scratch_dev), counters, s);

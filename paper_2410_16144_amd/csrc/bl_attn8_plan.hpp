@@ -73,6 +73,10 @@ struct Attn8Plan {
     int64_t shared_wgs, own_wgs;
     int     slots() const { return shared_splits + own_splits; }   // figures that a row's workgroups leave
     bool    meets() const { return !tiles && slots() > 1; }        // the workgroups of a row meet by counters (else: one, or a merging launch)
+    bool    launchable() const {                                   // fewer than 2^32 threads in each launch
+        const int64_t rows_threads = 64 * waves, tiles_threads = tiles ? 64 * kRows8FewWaves : rows_threads;
+        return (apart ? shared_wgs : shared_wgs + own_wgs) * tiles_threads < 1ll << 32 && own_wgs * rows_threads < 1ll << 32;
+    }
 };
 
 // shared_len: positions of the shared walk, own_len: of each token's own (0: none).  size: bytes of a row of codes.
@@ -148,10 +152,12 @@ inline Attn8Plan attn8_plan(int n_heads, int group, int tokens, int shared_len, 
     return p;
 }
 
-// The scratch memory: a counter per (key head, row), a head's in lines of their own, then the figures (none where a row has one workgroup).
+// The scratch memory: a counter per (key head, row), a head's in lines of their own, then the figures (none where a row has one workgroup).  0: a batch or prompt too large
+// for a launch.
 constexpr int64_t attn8_padded(int64_t rows) { return (rows + 31) / 32 * 32; }
 inline int64_t attn8_counters(int n_heads, int64_t rows) { return n_heads * attn8_padded(rows); }
 inline int64_t attn8_scratch(const Attn8Plan& p, int n_heads, int64_t rows, int head_dim) {
+    if (!p.launchable()) return 0;
     return attn8_counters(n_heads, rows) * 4 + (p.slots() > 1 ? n_heads * rows * p.slots() * (head_dim / 2 + 1) * 8 : 0);
 }
 

@@ -130,6 +130,19 @@ def test_scratch_sizes():
     assert B.bl_attn8_prefill_scratch_bytes(8, 4, 64, 0, 5) > 0
 
 
+def test_batches_and_prompts_too_large_for_a_launch():
+    """A launch has less than 2^32 threads: what needs more is refused ahead of every launch, a prompt's write included."""
+    assert B.bl_attn8_scratch_bytes(65535, 65535, 4, 1, 64, 0) > 0 and B.bl_attn8_scratch_bytes(65535, 65535, 4, 1, 1024, 0) == 0
+    assert B.bl_attn8_scratch_bytes(32000, 32000, 4, 1, 1024, 5) > 0 and B.bl_attn8_scratch_bytes(65535, 65535, 4, 1, 1024, 5) == 0
+    assert B.bl_attn8_prefill_scratch_bytes(65535, 65535, 4, 0, 60000) > 0 and B.bl_attn8_prefill_scratch_bytes(65535, 65535, 4, 0, 65535) == 0
+    far = dict(k_codes_dev=1 << 44, v_codes_dev=2 << 44, k_scale_dev=3 << 44, v_scale_dev=4 << 44)
+    for prefix_len in (0, 5):
+        prefix = _cache(n_heads=65535, head_dim=4, max_pos=5, sequences=1) if prefix_len else None
+        args = B.make_attn8_args(P, P, P, P, P, P, P, _cache(n_heads=65535, head_dim=4, max_pos=1, sequences=1024, **far), 65535, prefix, prefix_len)
+        assert _st(B.bl_attn8_decode, args) == B.BL_ERR_SHAPE
+    assert _st(B.bl_attn8_prefill, P, P, P, P, P, P, _cache(n_heads=65535, head_dim=4, max_pos=65535), 65535, 0, 0, 65535) == B.BL_ERR_SHAPE
+
+
 def _program(tmp_path, name, text):
     src = tmp_path / (name + ".cpp")
     src.write_text(text)
