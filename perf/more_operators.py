@@ -1,0 +1,301 @@
+"""A paged key/value cache and the attention over it: what is timed, in plain form and as the framework's calls.
+
+A pool of pages holds `page` positions each of every key head, bf16; a sequence's positions lie in the pages that its line of a table names. A
+call's rows are packed: sequence b has rows start[b] .. start[b + 1] - 1, at positions pos[b], pos[b] + 1, ... The operators: queries and keys
+normed per head and rotated, keys and values into their pages ("append"); attention of one token of every sequence ("decode"); attention of
+packed sequences of any number of tokens, each seeing its own sequence up to itself ("prompt").
+
+Both forms work on the same pools, k and v [pages, key heads, page, width]: width is the head size rounded up to a size that the framework stores.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda"
+THETA = 10000.0
+EPS = 1e-5
+
+# (query heads, key heads, head size) of the framework's models (125M to 100B), and shared key heads and sizes that fill no sixteen
+SHAPES = [(12, 12, 64), (16, 16, 96), (32, 32, 64), (32, 32, 48), (20, 20, 128), (32, 32, 120), (32, 32, 128), (40, 40, 128), (64, 64, 128),
+          (32, 8, 128), (64, 8, 128), (28, 4, 128), (12, 4, 100), (16, 1, 64), (16, 2, 256), (10, 5, 36)]
+WIDTHS = [32, 48, 64, 96, 128, 192, 256]
+
+
+def _several(n, lo, hi, seed):
+    """n lengths, spread over their logarithm, as a text."""
+    r = random.Random(seed)
+    return ",".join(str(_log_int(r, lo, hi)) for _ in range(n))
+
+
+def listed():
+    f, b = "float32", "bfloat16"
+    return [
+        # one token of a small model: the smallest call, latency
+        dict(name="append_1_small", kind="append", heads=12, keys=12, dim=64, page=16, new="1", before="17", dtype=f, out=f),
+        # a served batch's step: one token of 48 sequences, shared key heads, fp32 projections and bf16 queries
+        dict(name="append_48_served", kind="append", heads=64, keys=8, dim=128, page=64, new=",".join(["1"] * 48), before=_several(48, 10, 4000, 1), dtype=f, out=b),
+        # three prompts of a 7B model at once, bf16 projections: a stream
+        dict(name="append_2000_7b", kind="append", heads=32, keys=32, dim=128, page=64, new="1200,37,763", before="0,512,3", dtype=b, out=b),
+        # the first words of an answer, a small model
+        dict(name="decode_17_small", kind="decode", heads=12, keys=12, dim=64, page=16, before="17", dtype=f),
+        # eight conversations of different length on the 7B shape
+        dict(name="decode_8_7b", kind="decode", heads=32, keys=32, dim=128, page=64, before="8000,4100,6533,7999,1023,2890,5007,64", dtype=b),
+        # a token behind a book, query heads in groups that share a key head
+        dict(name="decode_100k_grouped", kind="decode", heads=64, keys=8, dim=128, page=128, before="100003", dtype=b),
+        # a served batch with shared key heads, in the framework's own fp32, small pages
+        dict(name="decode_64_served", kind="decode", heads=32, keys=8, dim=128, page=16, before=_several(64, 60, 4000, 2), dtype=f),
+        # five drafted tokens of four sequences looked at together behind long caches
+        dict(name="prompt_5_drafts", kind="prompt", heads=32, keys=8, dim=128, page=64, new="5,5,5,5", before="8000,1200,3333,5950", dtype=b),
+        # rows that fill no tile, one of them behind a cache that ends inside a page, head size 120, fp32
+        dict(name="prompt_77_ragged", kind="prompt", heads=32, keys=32, dim=120, page=16, new="77,1,30", before="1001,0,64", dtype=f),
+        # a prompt's second piece on the 7B shape
+        dict(name="prompt_512_7b", kind="prompt", heads=32, keys=32, dim=128, page=64, new="512", before="512", dtype=b),
+        # six requests' prompts packed behind each other
+        dict(name="prompt_6_packed", kind="prompt", heads=32, keys=8, dim=128, page=32, new="1300,250,611,17,990,1", before="0,0,700,0,0,400", dtype=b),
+        # a long prompt at once: the largest contraction
+        dict(name="prompt_4096", kind="prompt", heads=32, keys=8, dim=128, page=64, new="4096", before="0", dtype=b),
+    ]
+
+
+# ---- drawing ---------------------------------------------------------------------------------------------------------
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    heads, keys, dim = rng.choice(SHAPES)
+    kind = rng.choice(["append", "append", "decode", "decode", "decode", "prompt", "prompt", "prompt"])
+    c = dict(kind=kind, heads=heads, keys=keys, dim=dim, page=rng.choice([16, 32, 64, 128, 256]), dtype=rng.choice(["float32", "bfloat16", "bfloat16"]))
+    while True:
+        B = _log_int(rng, 1, 64)
+        before = [rng.choice([0, _log_int(rng, 1, 6000), _log_int(rng, 1, 6000)]) for _ in range(B)]
+        new = [1 if kind == "decode" or rng.random() < 0.3 else _log_int(rng, 1, 2048) for _ in range(B)]
+        if kind == "decode" and rng.random() < 0.3:
+            before, new = [_log_int(rng, 1, 100003)], [1]
+        c.update(new=",".join(map(str, new)), before=",".join(map(str, before)))
+        c["out"] = rng.choice([c["dtype"], "bfloat16"]) if kind == "append" else c["dtype"]
+        longest, reach, rows = max(new), max(n + p for n, p in zip(new, before)), sum(new)
+        # (the plain form pads all sequences to the longest one)
+        if kind == "append" and rows * (heads + 2 * keys) * dim <= 2000 * 96 * 128 and sum(before) * keys * dim <= 60000 * 1024:
+            return c
+        if kind != "append" and len(new) * longest * reach * heads <= 32 * 4096 * 4096 and work(c)["flops"] <= 32 * 128 * 4096 * 4096 and \
+                len(new) * reach * keys * dim <= 64 * 4000 * 1024 and rows * heads * dim <= 4096 * 4096 and work(c)["bytes"] <= 420e6:
+            return c
+
+
+# ---- inputs, from the seed alone ----------------------------------------------------------------------------------------
+
+def _gen(seed, what):
+    return torch.Generator(device=DEV).manual_seed(seed * 1009 + what)
+
+
+def _normal(seed, what, *shape):
+    return torch.randn(shape, device=DEV, generator=_gen(seed, what))
+
+
+def _rows(seed, what, M, heads, dim):
+    """Projections of M tokens: normal values, some channels of a head larger than others, tokens of different size."""
+    channel = torch.exp(0.5 * _normal(seed, what + 500, heads, dim))
+    token = torch.exp(0.3 * _normal(seed, what + 501, M, 1, 1))
+    return (_normal(seed, what, M, heads, dim) * channel * token).reshape(M, heads * dim)
+
+
+def _table(dim, positions):
+    """[positions, dim / 2, 2]: cosine and sine, angles in 64 bits, kept in 32."""
+    i = torch.arange(dim // 2, device=DEV, dtype=torch.float64)
+    a = torch.arange(positions, device=DEV, dtype=torch.float64)[:, None] * THETA ** (-2.0 * i / dim)
+    return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def _lengths(case):
+    """(rows of each sequence in this call, positions before it)."""
+    before = [int(x) for x in case["before"].split(",")]
+    return [int(x) for x in case["new"].split(",")] if case["kind"] != "decode" else [1] * len(before), before
+
+
+def _pool(case, seed):
+    """The pools, with rows of earlier calls (and whatever else) in all pages, and the sequences' lines of the table: pages in any order, some in
+    nobody's hands."""
+    new, before = _lengths(case)
+    page, keys, dim = case["page"], case["keys"], case["dim"]
+    need = [-(-(n + p) // page) for n, p in zip(new, before)]
+    pages, width = sum(need) + 3, next(w for w in WIDTHS if w >= dim)
+    order = torch.randperm(pages, device=DEV, generator=_gen(seed, 7)).to(torch.int32)
+    lines = torch.full((len(new), max(need)), -1, dtype=torch.int32, device=DEV)
+    at = 0
+    for i, n in enumerate(need):
+        lines[i, :n] = order[at:at + n]
+        at += n
+    k, v = (torch.zeros((pages, keys, page, width), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    channel = torch.exp(0.4 * _normal(seed, 8, keys, 1, dim))
+    for i in range(0, pages, 64):
+        n = min(64, pages - i)
+        k[i:i + n, ..., :dim] = (_normal(seed, 100 + 2 * i, n, keys, page, dim) * channel).to(torch.bfloat16)
+        v[i:i + n, ..., :dim] = _normal(seed, 101 + 2 * i, n, keys, page, dim).to(torch.bfloat16)
+    return k, v, lines
+
+
+def prepare(case, seed):
+    kind, heads, keys, dim = case["kind"], case["heads"], case["keys"], case["dim"]
+    new, before = _lengths(case)
+    T, dtype = sum(new), getattr(torch, case["dtype"])
+    st = dict(kind=kind, heads=heads, keys=keys, dim=dim, page=case["page"])
+    st["k_pool"], st["v_pool"], st["lines"] = _pool(case, seed)
+    st["pos"] = torch.tensor(before, dtype=torch.int32, device=DEV)
+    starts = [0]
+    for n in new:
+        starts.append(starts[-1] + n)
+    st["start"] = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    st["longest"], st["reach"] = max(new), max(n + p for n, p in zip(new, before))
+    st["q"] = _rows(seed, 1, T, heads, dim).to(dtype)
+    if kind == "append":
+        st["k"], st["v"] = _rows(seed, 2, T, keys, dim).to(dtype), _rows(seed, 3, T, keys, dim).to(dtype)
+        st["g_q"], st["g_k"] = (torch.rand(dim, device=DEV, generator=_gen(seed, n)) + 0.5 for n in (4, 5))
+        st["angles"] = _table(dim, st["reach"])
+        st["out"] = getattr(torch, case["out"])
+    if own:
+        _handles(st, case)
+    return st
+
+
+def _handles(st, case):
+    """The framework's cache around the same pools, the rows' description, and what a serving loop keeps between its steps."""
+    from paper_2410_16144_amd import decoder
+    st["cache"] = decoder.PagedCache(case["keys"], case["dim"], case["page"], st["k_pool"].shape[0], torch.device(DEV), k=st["k_pool"], v=st["v_pool"])
+    st["rows"] = decoder.PagedRows(st["lines"], st["pos"], st["reach"], start=None if case["kind"] == "decode" else st["start"], rows=st["q"].shape[0])
+    if case["kind"] == "decode":
+        st["attention"] = decoder.AttentionPaged(case["heads"], st["cache"], st["rows"], st["q"])
+    if case["kind"] == "prompt":
+        st["scratch"] = decoder.paged_scratch(case["heads"], st["cache"], st["rows"], st["q"].dtype)
+
+
+# ---- one pass -----------------------------------------------------------------------------------------------------------
+
+def run(st):
+    if own:
+        from paper_2410_16144_amd import decoder
+        if st["kind"] == "append":
+            q = st["cache"].append(st["q"], st["k"], st["v"], st["rows"], st["angles"], g_q=st["g_q"], g_k=st["g_k"], eps=EPS, q_dtype=st["out"])
+            return {"q": q, "k_pool": st["k_pool"], "v_pool": st["v_pool"]}
+        if st["kind"] == "decode":
+            return {"out": st["attention"].launch()}
+        return {"out": decoder.attn_paged(st["q"], st["cache"], st["rows"], scratch=st["scratch"])}
+    return _plain_append(st) if st["kind"] == "append" else _plain_attention(st)
+
+
+def _owners(st):
+    """Each row's sequence, and its number in it."""
+    row = torch.arange(st["q"].shape[0], device=DEV)
+    sequence = torch.searchsorted(st["start"][1:].contiguous(), row, right=True)
+    return sequence, row - st["start"][sequence]
+
+
+def _normed(x, gamma, angles):
+    """x [rows, heads, dim] in fp32: rmsnorm of every head's vector, then its pairs (i, i + dim / 2) rotated."""
+    y = x * gamma * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS)
+    a, b = y.chunk(2, -1)
+    c, s = angles[:, None, :, 0], angles[:, None, :, 1]
+    return torch.cat([a * c - b * s, a * s + b * c], -1)
+
+
+def _plain_append(st):
+    dim, rows = st["dim"], st["q"].shape[0]
+    sequence, i = _owners(st)
+    at = st["pos"][sequence] + i
+    page, slot = st["lines"][sequence, at // st["page"]].long(), at % st["page"]
+    angles = st["angles"][at]
+    q, k = (_normed(st[n].float().view(rows, -1, dim), st["g_" + n], angles) for n in "qk")
+    st["k_pool"][page, :, slot, :dim] = k.to(torch.bfloat16)
+    st["v_pool"][page, :, slot, :dim] = st["v"].float().view(rows, -1, dim).to(torch.bfloat16)
+    return {"q": q.reshape(rows, -1).to(st["out"]), "k_pool": st["k_pool"], "v_pool": st["v_pool"]}
+
+
+def _plain_attention(st):
+    """All sequences side by side, padded to the longest."""
+    heads, keys, dim, page, N, L = (st[n] for n in ("heads", "keys", "dim", "page", "longest", "reach"))
+    sequence, i = _owners(st)
+    B = st["pos"].shape[0]
+    q = torch.zeros((B, N, heads, dim), device=DEV)
+    q[sequence, i] = st["q"].float().view(-1, heads, dim)
+    q = q.view(B, N, keys, heads // keys, dim).permute(0, 2, 1, 3, 4).reshape(B, keys, -1, dim) / math.sqrt(dim)
+    at = torch.arange(L, device=DEV)
+    seen = at < (st["pos"] + st["start"][1:] - st["start"][:-1])[:, None]                      # the sequence's own positions
+    pages = torch.where(seen, st["lines"][:, at // page], 0).long()
+    k, v = (torch.where(seen[..., None, None], p[pages, :, at % page, :dim].float(), 0.0).permute(0, 2, 1, 3).contiguous() for p in (st["k_pool"], st["v_pool"]))
+    s = torch.matmul(q, k.transpose(2, 3).contiguous()).view(B, keys, N, -1, L)
+    beyond = at > st["pos"][:, None, None] + torch.arange(N, device=DEV)[:, None]              # [B, N, L]
+    s = s.masked_fill(beyond[:, None, :, None], -math.inf)
+    w = torch.exp(s - s.amax(-1, keepdim=True))
+    w = (w / w.sum(-1, keepdim=True)).view(B, keys, -1, L)
+    out = torch.matmul(w, v).view(B, keys, N, -1, dim).permute(0, 2, 1, 3, 4).reshape(B, N, heads * dim)
+    return {"out": out[sequence, i].to(st["q"].dtype)}
+
+
+# ---- what a pass cannot do without ----------------------------------------------------------------------------------------
+
+def work(case):
+    heads, keys, dim = case["heads"], case["keys"], case["dim"]
+    new, before = _lengths(case)
+    rows, e = sum(new), 4 if case["dtype"] == "float32" else 2
+    if case["kind"] == "append":
+        o = 4 if case["out"] == "float32" else 2
+        return {"bytes": rows * dim * ((heads + 2 * keys) * e + heads * o + 2 * keys * 2 + 4), "flops": rows * dim * (heads + keys) * 7}
+    seen = sum(n * p + n * (n + 1) / 2 for n, p in zip(new, before))
+    return {"bytes": 2 * rows * heads * dim * e + sum(n + p for n, p in zip(new, before)) * keys * dim * 4, "flops": 4 * heads * dim * seen}
+
+
+# ---- the same in 64 bits ---------------------------------------------------------------------------------------------------
+
+def _exact_head(x, gamma, angles):
+    """x [heads, dim] of one row, in 64 bits."""
+    half = x.shape[1] // 2
+    r = torch.sqrt(x.pow(2).sum(1, keepdim=True) / x.shape[1] + EPS)
+    y = x / r * gamma
+    z = torch.complex(y[:, :half], y[:, half:]) * torch.complex(angles[:, 0], angles[:, 1])
+    return torch.cat([z.real, z.imag], 1)
+
+
+def _exact_append(case, seed):
+    heads, keys, dim, page = case["heads"], case["keys"], case["dim"], case["page"]
+    new, before = _lengths(case)
+    dtype, T = getattr(torch, case["dtype"]), sum(new)
+    q, k, v = (_rows(seed, n, T, h, dim).to(dtype).double().view(T, h, dim) for n, h in ((1, heads), (2, keys), (3, keys)))
+    g_q, g_k = (torch.rand(dim, device=DEV, generator=_gen(seed, n)).add(0.5).double() for n in (4, 5))
+    angles = _table(dim, max(n + p for n, p in zip(new, before))).double()
+    k_pool, v_pool, lines = _pool(case, seed)
+    k_pool, v_pool, lines = k_pool.double(), v_pool.double(), lines.tolist()
+    out, t = torch.empty_like(q), 0
+    for b, (n, p) in enumerate(zip(new, before)):
+        for at in range(p, p + n):
+            where, slot = lines[b][at // page], at % page
+            out[t] = _exact_head(q[t], g_q, angles[at])
+            k_pool[where, :, slot, :dim] = _exact_head(k[t], g_k, angles[at])
+            v_pool[where, :, slot, :dim] = v[t]
+            t += 1
+    return {"q": out.view(T, -1), "k_pool": k_pool, "v_pool": v_pool}
+
+
+def exact(case, seed):
+    if case["kind"] == "append":
+        return _exact_append(case, seed)
+    heads, keys, dim, page = case["heads"], case["keys"], case["dim"], case["page"]
+    new, before = _lengths(case)
+    T, group = sum(new), heads // keys
+    q = _rows(seed, 1, T, heads, dim).to(getattr(torch, case["dtype"])).double().view(T, heads, dim)
+    k_pool, v_pool, lines = _pool(case, seed)
+    out, t = torch.empty_like(q), 0
+    for b, (n, p) in enumerate(zip(new, before)):
+        line = lines[b, :-(-(n + p) // page)].long()
+        k, v = (x[line].transpose(0, 1).reshape(keys, -1, x.shape[-1])[:, :n + p, :dim].double() for x in (k_pool, v_pool))
+        last = torch.arange(p, p + n, device=DEV)[:, None]
+        for h in range(heads):
+            s = q[t:t + n, h] @ k[h // group].t() / math.sqrt(dim)
+            s[torch.arange(n + p, device=DEV)[None] > last] = -math.inf
+            w = torch.softmax(s, 1)
+            out[t:t + n, h] = w @ v[h // group]
+        t += n
+    return {"out": out.view(T, -1)}
