@@ -170,7 +170,7 @@ def _handles(st, case):
     if case["kind"] == "decode":
         st["attention"] = decoder.AttentionPaged(case["heads"], st["cache"], st["rows"], st["q"])
     if case["kind"] == "prompt":
-        st["scratch"] = decoder.paged_scratch(case["heads"], st["cache"], st["rows"], st["q"].dtype)
+        st["scratch"] = decoder.paged_scratch(case["heads"], st["cache"], st["rows"])
 
 
 # ---- one pass -----------------------------------------------------------------------------------------------------------
