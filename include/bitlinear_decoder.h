@@ -19,7 +19,8 @@
  * Conventions as in bitlinear.h: device pointers end in _dev, no entry point allocates, frees or
  * synchronizes, `stream` is a hipStream_t (NULL = default stream), errors are bl_status codes and
  * nothing is launched when one is returned.  All floating-point data here is fp32 except the
- * key/value cache (bf16 bit patterns, or int8 codes with fp32 scales: bl_kv8_cache).
+ * key/value cache (bf16 bit patterns, or int8 codes with fp32 scales: bl_kv8_cache) and what the paged cache's calls
+ * name a bl_dtype for.
  */
 #ifndef BITLINEAR_DECODER_H
 #define BITLINEAR_DECODER_H
@@ -410,6 +411,117 @@ typedef struct bl_attn8_prefill_args {
 uint64_t bl_attn8_prefill_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M);
 
 bl_status bl_attn8_prefill(const bl_attn8_prefill_args *args, void *stream);
+
+/*
+ * The paged key/value cache: one pool of pages for the sequences of a server, of any lengths.  A page holds page_size positions of every key
+ * head, as bf16; which pages a sequence has, in which order, a table on the device says.
+ *   n_heads      key heads; head_dim a multiple of 4 (4 .. BL_ATTN_MAX_HEAD_DIM)
+ *   page_size    positions of a page, a power of two, BL_PAGE_MIN .. BL_PAGE_MAX
+ *   k_pages_dev, v_pages_dev   [pages][n_heads][page_size][bl_paged_width(head_dim)] bf16 bit patterns, 16-byte aligned
+ * The elements behind head_dim of a row are written as zero with their row; rows that were never written may hold anything.
+ */
+#define BL_PAGE_MIN 16
+#define BL_PAGE_MAX 4096
+#define BL_PAGED_MAX_GROUP 64        /* query heads per key head */
+#define BL_PAGED_MAX_SEQUENCES 1024  /* of one call */
+
+typedef struct bl_paged_cache {
+    uint16_t *k_pages_dev;
+    uint16_t *v_pages_dev;
+    int32_t   n_heads;
+    int32_t   head_dim;
+    int32_t   page_size;
+    int32_t   pages;
+} bl_paged_cache;
+
+/* Elements of a stored row: head_dim rounded up to 32, 48, 64, 96, 128, 192 or 256; 0 if it is out of range. */
+int32_t bl_paged_width(int32_t head_dim);
+
+/*
+ * The rows of a call, and whose they are.  Row start_dev[b] + i is sequence b's token at position pos_dev[b] + i, up to row start_dev[b + 1] - 1 (no
+ * row at all is allowed); without start_dev every sequence has one, row b.  Position p of sequence b lies in row p % page_size of page
+ * table_dev[b * table_width + p / page_size].
+ *   table_dev   [sequences, table_width] int32; only entries up to the call's last position of a sequence are read
+ *   pos_dev     [sequences] int32
+ *   start_dev   [sequences + 1] int32, rising; may be NULL: then rows == sequences
+ *   max_pos     no position of the call is max_pos or beyond; 1 <= max_pos <= table_width * page_size
+ * All four are read on the device, so a captured launch serves other lengths, pages and numbers of rows up to `rows`.  What they say is looked at
+ * before it is used: a sequence with a negative position, with positions from max_pos on, or with rows outside 0 .. rows - 1 takes no part, its
+ * rows of the outputs stay as they are, like rows that no sequence has.  Two sequences may share pages that nobody writes in the call.
+ */
+typedef struct bl_paged_rows {
+    const int32_t *table_dev;
+    const int32_t *pos_dev;
+    const int32_t *start_dev;
+    int32_t        table_width;
+    int32_t        sequences;
+    int32_t        rows;
+    int32_t        max_pos;
+} bl_paged_rows;
+
+/*
+ * What stands between the projections and the attention, in one launch: every query and key head's vector is normalised and rotated, queries go to
+ * q_out_dev, keys and values (as they are), rounded to bf16, into their pages.
+ *   y[e] = (x[e] * gamma[e]) * r,   r = 1 / sqrt(mean_e(x^2) + eps)   over the head's elements (fp32; without gamma: y = x)
+ *   (y[i], y[i + head_dim/2]) rotated by the table's row of the token's position, as bl_attn_decode rotates (without a table: as they are)
+ *   q_dev        [rows, ld_q >= n_q_heads * head_dim], k_dev [rows, ld_k], v_dev [rows, ld_v >= n_heads * head_dim], fp32 or bf16 (dt), aligned
+ *                to the element
+ *   q_out_dev    [rows, n_q_heads * head_dim] fp32 or bf16 (q_out_dt), 16-byte aligned; must not overlap the inputs
+ *   gamma_q_dev, gamma_k_dev   [head_dim] fp32, either may be NULL
+ *   rope_table_dev   the table of bl_rope_table, max_pos rows or more; may be NULL
+ * A position whose page number is outside 0 .. pages - 1 is not stored.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN, BL_ERR_HIP.
+ */
+typedef struct bl_paged_append_args {
+    const bl_paged_cache *cache;    /* host */
+    const bl_paged_rows  *rows;     /* host */
+    const void  *q_dev;
+    const void  *k_dev;
+    const void  *v_dev;
+    void        *q_out_dev;
+    const float *gamma_q_dev;
+    const float *gamma_k_dev;
+    const float *rope_table_dev;
+    int64_t      ld_q;
+    int64_t      ld_k;
+    int64_t      ld_v;
+    int32_t      dt;                /* bl_dtype of q, k and v */
+    int32_t      q_out_dt;          /* bl_dtype of q_out */
+    int32_t      n_q_heads;
+    float        eps;
+} bl_paged_append_args;
+
+bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
+
+/*
+ * Attention over the pages: the row of position p attends to positions 0 .. p of its sequence, which are in the cache already (bl_paged_append),
+ * scores scaled by 1 / sqrt(head_dim).  Query head i reads key head i / (n_q_heads / cache->n_heads).  One call serves single tokens, prompts,
+ * pieces of prompts and any mixture; without start_dev it is made for single tokens.
+ *   q_dev, out_dev  [rows, n_q_heads * head_dim] fp32 or bf16 (dt, both the same), 8-byte aligned; must not overlap
+ *   scratch_dev     bl_attn_paged_scratch_bytes(...) bytes, 256-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
+ *                   any other call with as many key heads and no greater need.  Calls that may overlap in time must not share it.
+ * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with
+ * weights rounded to bf16; everything else is fp32.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
+ * that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
+ * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
+ * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,
+ *         BL_ERR_HIP.
+ */
+typedef struct bl_attn_paged_args {
+    const bl_paged_cache *cache;    /* host */
+    const bl_paged_rows  *rows;     /* host */
+    const void *q_dev;
+    void       *out_dev;
+    void       *scratch_dev;
+    int32_t     n_q_heads;
+    int32_t     dt;                 /* bl_dtype of q and out */
+} bl_attn_paged_args;
+
+/* Bytes of bl_attn_paged_args.scratch_dev; 0 if a shape is out of range.  single: whether the call has no start_dev. */
+uint64_t bl_attn_paged_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t sequences, int32_t rows, int32_t max_pos,
+                                     int32_t single);
+
+bl_status bl_attn_paged(const bl_attn_paged_args *args, void *stream);
 
 /*
  * A model's last norm, y = rmsnorm(h + delta, gamma) without a quantizer (bl_norm_quant's arithmetic in mode

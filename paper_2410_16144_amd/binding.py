@@ -38,6 +38,7 @@ DECLARED_SYMBOLS = (
     "bl_norm_quant", "bl_final_norm", "bl_rope_table", "bl_attn_scratch_bytes", "bl_attn_decode", "bl_pos_advance", "bl_decode_norm_batch", "bl_pack_gate_up", "bl_attn_prefill", "bl_attn_prefill_scratch_bytes",
     "bl_kv8_code_bytes", "bl_kv8_scale_count", "bl_kv8_write", "bl_kv8_read", "bl_attn8_scratch_bytes", "bl_attn8_decode",
     "bl_attn8_prefill_scratch_bytes", "bl_attn8_prefill",
+    "bl_paged_width", "bl_paged_append", "bl_attn_paged_scratch_bytes", "bl_attn_paged",
 )
 
 BL_NORM_MAX_K = 49152
@@ -48,6 +49,9 @@ BL_ATTN_BLOCK_MAX_HEAD_DIM = 128
 BL_KV8_CHUNK = 64
 BL_ATTN8_MAX_GROUP = 64
 BL_ATTN8_MAX_BATCH = 1024
+BL_PAGE_MIN, BL_PAGE_MAX = 16, 4096
+BL_PAGED_MAX_GROUP = 64
+BL_PAGED_MAX_SEQUENCES = 1024
 BL_NORM_PLAIN, BL_NORM_RESIDUAL, BL_NORM_GATED, BL_NORM_PREMULTIPLIED = 0, 1, 2, 3
 BL_DECODE_NORM_MAX_K = 16384
 
@@ -168,6 +172,32 @@ class Attn8PrefillArgs(ctypes.Structure):
                 ("M", ctypes.c_int32)]
 
 
+class PagedCache(ctypes.Structure):
+    """Mirror of bl_paged_cache."""
+    _fields_ = [("k_pages_dev", ctypes.c_void_p), ("v_pages_dev", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("pages", ctypes.c_int32)]
+
+
+class PagedRows(ctypes.Structure):
+    """Mirror of bl_paged_rows."""
+    _fields_ = [("table_dev", ctypes.c_void_p), ("pos_dev", ctypes.c_void_p), ("start_dev", ctypes.c_void_p), ("table_width", ctypes.c_int32),
+                ("sequences", ctypes.c_int32), ("rows", ctypes.c_int32), ("max_pos", ctypes.c_int32)]
+
+
+class PagedAppendArgs(ctypes.Structure):
+    """Mirror of bl_paged_append_args."""
+    _fields_ = [("cache", ctypes.POINTER(PagedCache)), ("rows", ctypes.POINTER(PagedRows)), ("q_dev", ctypes.c_void_p), ("k_dev", ctypes.c_void_p),
+                ("v_dev", ctypes.c_void_p), ("q_out_dev", ctypes.c_void_p), ("gamma_q_dev", ctypes.c_void_p), ("gamma_k_dev", ctypes.c_void_p),
+                ("rope_table_dev", ctypes.c_void_p), ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64),
+                ("dt", ctypes.c_int32), ("q_out_dt", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class AttnPagedArgs(ctypes.Structure):
+    """Mirror of bl_attn_paged_args."""
+    _fields_ = [("cache", ctypes.POINTER(PagedCache)), ("rows", ctypes.POINTER(PagedRows)), ("q_dev", ctypes.c_void_p), ("out_dev", ctypes.c_void_p),
+                ("scratch_dev", ctypes.c_void_p), ("n_q_heads", ctypes.c_int32), ("dt", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -230,6 +260,11 @@ def lib():
     l.bl_kv8_read.argtypes = [ctypes.POINTER(Kv8ReadArgs), vp]
     l.bl_attn8_decode.argtypes = [ctypes.POINTER(Attn8Args), vp]
     l.bl_attn8_prefill.argtypes = [ctypes.POINTER(Attn8PrefillArgs), vp]
+    l.bl_paged_width.argtypes = [i32]
+    l.bl_paged_append.argtypes = [ctypes.POINTER(PagedAppendArgs), vp]
+    l.bl_attn_paged_scratch_bytes.argtypes = [i32] * 7
+    l.bl_attn_paged_scratch_bytes.restype = ctypes.c_uint64
+    l.bl_attn_paged.argtypes = [ctypes.POINTER(AttnPagedArgs), vp]
     l.bl_set_tuning.argtypes = [ctypes.c_char_p, i32]
     l.bl_get_stat.argtypes = [ctypes.c_char_p]
     l.bl_get_stat.restype = i64
@@ -242,7 +277,7 @@ def lib():
                  "bl_gemv_batch", "bl_decode_batch", "bl_gemm", "bl_set_tuning", "bl_tl2_desc_init", "bl_tl2_pack",
                  "bl_tl2_unpack", "bl_tl2_gemv", "bl_tl2_gemv_batch", "bl_norm_quant", "bl_final_norm", "bl_rope_table", "bl_attn_decode",
                  "bl_pos_advance", "bl_decode_norm_batch", "bl_attn_prefill", "bl_gemm_batch", "bl_gemv_batch_static", "bl_pack_gate_up",
-                 "bl_kv8_write", "bl_kv8_read", "bl_attn8_decode", "bl_attn8_prefill"):
+                 "bl_kv8_write", "bl_kv8_read", "bl_attn8_decode", "bl_attn8_prefill", "bl_paged_append", "bl_attn_paged"):
         getattr(l, name).restype = ctypes.c_int
     _lib = l
     return l
@@ -250,7 +285,7 @@ def lib():
 
 _calls = None
 # bl_calls.cpp: the `which` of calls().launch
-LAUNCH_GEMV_BATCH, LAUNCH_DECODE_BATCH, LAUNCH_QUANT_BATCH, LAUNCH_DECODE_NORM_BATCH, LAUNCH_TL2_BATCH, LAUNCH_ATTN_DECODE, LAUNCH_ATTN8_DECODE = range(7)
+LAUNCH_GEMV_BATCH, LAUNCH_DECODE_BATCH, LAUNCH_QUANT_BATCH, LAUNCH_DECODE_NORM_BATCH, LAUNCH_TL2_BATCH, LAUNCH_ATTN_DECODE, LAUNCH_ATTN8_DECODE, LAUNCH_ATTN_PAGED = range(8)
 
 
 def calls():
@@ -283,12 +318,12 @@ def current_stream() -> int:
 
 def launch(which: int, items, M: int, workspace_dev: int = 0):
     """One prepared launch on the current stream: items is the ctypes array of make_*_items (for LAUNCH_ATTN_DECODE the AttnArgs,
-    for LAUNCH_ATTN8_DECODE the Attn8Args).
+    for LAUNCH_ATTN8_DECODE the Attn8Args, for LAUNCH_ATTN_PAGED the AttnPagedArgs).
     Anything else goes to the ctypes binding, which takes or refuses it as it always did.  Raises BitLinearError like the
     calls below."""
     of, call, where = _LAUNCHES[which]
     c = calls()
-    if c and (isinstance(items, ctypes.Array) and items._type_ is of or type(items) is of and of in (AttnArgs, Attn8Args)):
+    if c and (isinstance(items, ctypes.Array) and items._type_ is of or type(items) is of and of in (AttnArgs, Attn8Args, AttnPagedArgs)):
         status = c.launch(which, items, M, workspace_dev or 0)
         if status is not None:
             return _check(status, where)
@@ -541,6 +576,35 @@ def bl_attn8_prefill(q_lin_dev: int, k_lin_dev: int, v_lin_dev: int, rope_table_
     _check(lib().bl_attn8_prefill(ctypes.byref(args), stream or None), "bl_attn8_prefill")
 
 
+def bl_paged_width(head_dim: int) -> int:
+    return int(lib().bl_paged_width(head_dim))
+
+
+def _at(struct):
+    return ctypes.pointer(struct) if struct is not None else None
+
+
+def bl_paged_append(cache: PagedCache, rows: PagedRows, q_dev: int, k_dev: int, v_dev: int, q_out_dev: int, ld_q: int, ld_k: int, ld_v: int, dtype: int,
+                    q_out_dtype: int, n_q_heads: int, gamma_q_dev: int = 0, gamma_k_dev: int = 0, eps: float = 0.0, rope_table_dev: int = 0,
+                    stream: int = 0):
+    args = PagedAppendArgs(_at(cache), _at(rows), q_dev or None, k_dev or None, v_dev or None, q_out_dev or None, gamma_q_dev or None,
+                           gamma_k_dev or None, rope_table_dev or None, ld_q, ld_k, ld_v, dtype, q_out_dtype, n_q_heads, eps)
+    _check(lib().bl_paged_append(ctypes.byref(args), stream or None), "bl_paged_append")
+
+
+def bl_attn_paged_scratch_bytes(n_q_heads: int, n_heads: int, head_dim: int, sequences: int, rows: int, max_pos: int, single: bool) -> int:
+    return int(lib().bl_attn_paged_scratch_bytes(n_q_heads, n_heads, head_dim, sequences, rows, max_pos, int(single)))
+
+
+def make_attn_paged_args(cache: PagedCache, rows: PagedRows, q_dev: int, out_dev: int, scratch_dev: int, n_q_heads: int, dtype: int) -> AttnPagedArgs:
+    """The structures are read at every launch: cache and rows have to stay."""
+    return AttnPagedArgs(_at(cache), _at(rows), q_dev or None, out_dev or None, scratch_dev or None, n_q_heads, dtype)
+
+
+def bl_attn_paged(args: AttnPagedArgs, stream: int = 0):
+    _check(lib().bl_attn_paged(ctypes.byref(args), stream or None), "bl_attn_paged")
+
+
 def bl_pos_advance(pos_dev: int, stream: int = 0):
     _check(lib().bl_pos_advance(pos_dev, stream), "bl_pos_advance")
 
@@ -585,4 +649,5 @@ _LAUNCHES = (
     (GemvItem, lambda items, M, ws: bl_tl2_gemv_batch(items, ws, current_stream()), "bl_tl2_gemv_batch"),
     (AttnArgs, lambda items, M, ws: bl_attn_decode(items, current_stream()), "bl_attn_decode"),
     (Attn8Args, lambda items, M, ws: bl_attn8_decode(items, current_stream()), "bl_attn8_decode"),
+    (AttnPagedArgs, lambda items, M, ws: bl_attn_paged(items, current_stream()), "bl_attn_paged"),
 )

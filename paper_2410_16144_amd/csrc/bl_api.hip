@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include "bl_kv8.hpp"
+#include "bl_paged.hpp"
 
 namespace {
 
@@ -623,7 +624,7 @@ bl_status bl_kv8_read(const bl_kv8_read_args* a, void* stream) {
 }
 
 // (a batch or prompt too large for a launch: seen ahead of the first one)
-static bl_status attn8_status(hipError_t e) { return e == hipErrorInvalidConfiguration ? BL_ERR_SHAPE : hip_status(e); }
+static bl_status shape_status(hipError_t e) { return e == hipErrorInvalidConfiguration ? BL_ERR_SHAPE : hip_status(e); }
 
 static bool attn8_heads_ok(int32_t n_q_heads, int32_t n_heads) {
     return n_heads >= 1 && n_q_heads >= 1 && n_q_heads <= 65535 && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_ATTN8_MAX_GROUP;
@@ -668,7 +669,7 @@ bl_status bl_attn8_decode(const bl_attn8_args* a, void* stream) {
         !aligned(a->rope_table_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
         return BL_ERR_ALIGN;
     drop_stale_hip_error();
-    return attn8_status(bl::launch_attn8_decode(*a, static_cast<hipStream_t>(stream)));
+    return shape_status(bl::launch_attn8_decode(*a, static_cast<hipStream_t>(stream)));
 }
 
 static bool attn8_prefill_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t pos0, int32_t M) {
@@ -691,7 +692,67 @@ bl_status bl_attn8_prefill(const bl_attn8_prefill_args* a, void* stream) {
         !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 16))
         return BL_ERR_ALIGN;
     drop_stale_hip_error();
-    return attn8_status(bl::launch_attn8_prefill(*a, static_cast<hipStream_t>(stream)));
+    return shape_status(bl::launch_attn8_prefill(*a, static_cast<hipStream_t>(stream)));
+}
+
+int32_t bl_paged_width(int32_t head_dim) {
+    return head_dim >= 4 && head_dim <= BL_ATTN_MAX_HEAD_DIM && head_dim % 4 == 0 ? bl::paged_width(head_dim) : 0;
+}
+
+static bool paged_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t sequences, int32_t rows, int32_t max_pos) {
+    return n_heads >= 1 && n_heads <= 65535 && n_q_heads >= n_heads && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_PAGED_MAX_GROUP &&
+           bl_paged_width(head_dim) > 0 && sequences >= 1 && sequences <= BL_PAGED_MAX_SEQUENCES && rows >= 1 && rows <= (1 << 24) && max_pos >= 1;
+}
+
+static bl_status check_paged(const bl_paged_cache* c, const bl_paged_rows* r, int32_t n_q_heads) {
+    if (!c || !r || !c->k_pages_dev || !c->v_pages_dev || !r->table_dev || !r->pos_dev) return BL_ERR_NULL;
+    if (!paged_shape_ok(n_q_heads, c->n_heads, c->head_dim, r->sequences, r->rows, r->max_pos)) return BL_ERR_SHAPE;
+    if (c->page_size < BL_PAGE_MIN || c->page_size > BL_PAGE_MAX || (c->page_size & (c->page_size - 1)) || c->pages < 1) return BL_ERR_SHAPE;
+    if (r->table_width < 1 || r->max_pos > (int64_t)r->table_width * c->page_size) return BL_ERR_SHAPE;
+    if (!r->start_dev && r->rows != r->sequences) return BL_ERR_SHAPE;
+    if (!aligned(c->k_pages_dev, 16) || !aligned(c->v_pages_dev, 16) || !aligned(r->table_dev, 4) || !aligned(r->pos_dev, 4) || !aligned(r->start_dev, 4))
+        return BL_ERR_ALIGN;
+    return BL_OK;
+}
+
+static bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+bl_status bl_paged_append(const bl_paged_append_args* a, void* stream) {
+    if (!a || !a->q_dev || !a->k_dev || !a->v_dev || !a->q_out_dev) return BL_ERR_NULL;
+    const bl_status s = check_paged(a->cache, a->rows, a->n_q_heads);
+    if (s != BL_OK) return s;
+    if ((a->dt != BL_F32 && a->dt != BL_BF16) || (a->q_out_dt != BL_F32 && a->q_out_dt != BL_BF16)) return BL_ERR_DTYPE;
+    const int64_t d = a->cache->head_dim, T = a->rows->rows, heads[3] = {a->n_q_heads, a->cache->n_heads, a->cache->n_heads}, ld[3] = {a->ld_q, a->ld_k, a->ld_v};
+    const void* x[3] = {a->q_dev, a->k_dev, a->v_dev};
+    const uint64_t e = a->dt == BL_BF16 ? 2 : 4, out_bytes = (uint64_t)(T * heads[0] * d) * (a->q_out_dt == BL_BF16 ? 2 : 4);
+    for (int i = 0; i < 3; ++i) {
+        if (ld[i] < heads[i] * d || ld[i] > INT64_MAX / 4 / T) return BL_ERR_SHAPE;
+        if (overlap(x[i], (uint64_t)((T - 1) * ld[i] + heads[i] * d) * e, a->q_out_dev, out_bytes)) return BL_ERR_SHAPE;
+        if (!aligned(x[i], e)) return BL_ERR_ALIGN;
+    }
+    if (!aligned(a->q_out_dev, 16) || !aligned(a->gamma_q_dev, 4) || !aligned(a->gamma_k_dev, 4) || !aligned(a->rope_table_dev, 8)) return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return shape_status(bl::launch_paged_append(*a, static_cast<hipStream_t>(stream)));
+}
+
+uint64_t bl_attn_paged_scratch_bytes(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t sequences, int32_t rows, int32_t max_pos, int32_t single) {
+    if (!paged_shape_ok(n_q_heads, n_heads, head_dim, sequences, rows, max_pos) || (single && rows != sequences)) return 0;
+    return (uint64_t)bl::paged_scratch_bytes(n_heads, n_q_heads / n_heads, head_dim, sequences, rows, max_pos, single != 0);
+}
+
+bl_status bl_attn_paged(const bl_attn_paged_args* a, void* stream) {
+    if (!a || !a->q_dev || !a->out_dev || !a->scratch_dev) return BL_ERR_NULL;
+    const bl_status s = check_paged(a->cache, a->rows, a->n_q_heads);
+    if (s != BL_OK) return s;
+    if (a->dt != BL_F32 && a->dt != BL_BF16) return BL_ERR_DTYPE;
+    const uint64_t bytes = (uint64_t)a->rows->rows * a->n_q_heads * a->cache->head_dim * (a->dt == BL_BF16 ? 2 : 4);
+    if (overlap(a->q_dev, bytes, a->out_dev, bytes)) return BL_ERR_SHAPE;
+    if (!aligned(a->q_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 256)) return BL_ERR_ALIGN;
+    drop_stale_hip_error();
+    return shape_status(bl::launch_attn_paged(*a, static_cast<hipStream_t>(stream)));
 }
 
 bl_status bl_pos_advance(int32_t* pos_dev, void* stream) {

@@ -404,9 +404,106 @@ PyObject* attn_prefill8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// The paged cache: `cache` and `rows` are the bl_paged_cache and bl_paged_rows, `pages` and `lines` a tensor of each.
+struct CachePaged {
+    Memory cache_memory, rows_memory;
+    const at::Tensor *pages, *lines;
+    void* stream = nullptr;
+    bool ok = false;
+    CachePaged(PyObject* cache, PyObject* tensor, PyObject* rows, PyObject* line)
+        : cache_memory(cache, sizeof(bl_paged_cache)), rows_memory(rows, sizeof(bl_paged_rows)), pages(plain(tensor)), lines(plain(line)) {
+        if (!cache_memory.ok || !rows_memory.ok || !pages || !lines) return;
+        const c10::hip::HIPStream now = c10::hip::getCurrentHIPStream();
+        stream = now.stream();
+        ok = pages->get_device() == now.device_index() && lines->get_device() == now.device_index();
+    }
+    const bl_paged_cache& c() const { return *cache_memory.as<const bl_paged_cache>(); }
+    const bl_paged_rows& r() const { return *rows_memory.as<const bl_paged_rows>(); }
+    bool here(const at::Tensor* t) const { return t && t->get_device() == pages->get_device(); }
+    static bool typed(const at::Tensor* t) { return t->scalar_type() == at::kFloat || t->scalar_type() == at::kBFloat16; }
+    static int32_t code(at::ScalarType t) { return t == at::kFloat ? BL_F32 : BL_BF16; }
+    // projections of the call's rows: [rows, heads * head_dim] with the rows anywhere; where a row is the next one's begins
+    bool takes(const at::Tensor* t, int64_t& ld) const {
+        if (!here(t) || !typed(t) || t->dim() != 2 || t->size(0) != r().rows || t->size(1) < 1 || t->size(1) % c().head_dim != 0 || t->stride(1) != 1) return false;
+        ld = t->size(0) > 1 ? t->stride(0) : t->size(1);
+        return ld >= t->size(1);
+    }
+};
+
+// paged_append(cache, pages, rows, lines, q, k, v, g_q or None, g_k or None, eps, rotary table or None, out or None, bf16) -> q_out
+PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    BL_NEEDS(13)
+    const double eps = PyFloat_AsDouble(args[9]);
+    if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+    const CachePaged cache(args[0], args[1], args[2], args[3]);
+    if (!cache.ok) Py_RETURN_NONE;
+    const at::Tensor *x[3] = {plain(args[4]), plain(args[5]), plain(args[6])}, *gamma[2] = {nullptr, nullptr}, *table = nullptr;
+    const int64_t d = cache.c().head_dim;
+    int64_t ld[3];
+    for (int i = 0; i < 3; ++i)
+        if (!cache.takes(x[i], ld[i]) || x[i]->scalar_type() != x[0]->scalar_type() || (i && x[i]->size(1) != cache.c().n_heads * d)) Py_RETURN_NONE;
+    for (int i = 0; i < 2; ++i)
+        if (args[7 + i] != Py_None && (!(gamma[i] = plain(args[7 + i], at::kFloat)) || !cache.here(gamma[i]) || gamma[i]->dim() != 1 || gamma[i]->size(0) != d))
+            Py_RETURN_NONE;
+    if (args[10] != Py_None && (!(table = plain(args[10], at::kFloat)) || !cache.here(table) || table->dim() != 3 || table->size(0) < cache.r().max_pos ||
+                                table->size(1) != d / 2 || table->size(2) != 2))
+        Py_RETURN_NONE;
+    at::Tensor out;
+    if (args[11] == Py_None) {
+        out = fresh({x[0]->size(0), x[0]->size(1)}, args[12] == Py_True ? at::kBFloat16 : at::kFloat, *x[0]);
+    } else {
+        const at::Tensor* given = plain(args[11]);
+        if (!cache.here(given) || !CachePaged::typed(given) || !given->is_contiguous() || given->sizes() != x[0]->sizes()) Py_RETURN_NONE;
+        out = *given;
+    }
+    const auto floats = [](const at::Tensor* t) { return t ? static_cast<const float*>(t->data_ptr()) : nullptr; };
+    const bl_paged_append_args p{&cache.c(), &cache.r(), x[0]->data_ptr(), x[1]->data_ptr(), x[2]->data_ptr(), out.data_ptr(), floats(gamma[0]),
+                                 floats(gamma[1]), floats(table), ld[0], ld[1], ld[2], CachePaged::code(x[0]->scalar_type()),
+                                 CachePaged::code(out.scalar_type()), (int32_t)(x[0]->size(1) / d), (float)eps};
+    bl_status status;
+    {
+        WithoutGil release;
+        status = bl_paged_append(&p, cache.stream);
+    }
+    return status == BL_OK ? THPVariable_Wrap(out) : PyLong_FromLong(status);
+    END_HANDLE_TH_ERRORS
+}
+
+// attn_paged(cache, pages, rows, lines, q, scratch, out or None) -> out
+PyObject* attn_paged(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    BL_NEEDS(7)
+    const CachePaged cache(args[0], args[1], args[2], args[3]);
+    if (!cache.ok) Py_RETURN_NONE;
+    const at::Tensor *q = plain(args[4]), *scratch = plain(args[5], at::kByte);
+    int64_t ld;
+    if (!cache.takes(q, ld) || !q->is_contiguous() || !cache.here(scratch)) Py_RETURN_NONE;
+    const int32_t n_heads = (int32_t)(q->size(1) / cache.c().head_dim);
+    const uint64_t bytes = bl_attn_paged_scratch_bytes(n_heads, cache.c().n_heads, cache.c().head_dim, cache.r().sequences, cache.r().rows, cache.r().max_pos,
+                                                       cache.r().start_dev == nullptr);
+    if (bytes == 0 || (uint64_t)scratch->numel() < bytes) Py_RETURN_NONE;
+    at::Tensor out;
+    if (args[6] == Py_None) {
+        out = fresh({q->size(0), q->size(1)}, q->scalar_type(), *q);
+    } else {
+        const at::Tensor* given = plain(args[6], q->scalar_type());
+        if (!cache.here(given) || given->sizes() != q->sizes()) Py_RETURN_NONE;
+        out = *given;
+    }
+    const bl_attn_paged_args p{&cache.c(), &cache.r(), q->data_ptr(), out.data_ptr(), scratch->data_ptr(), n_heads, CachePaged::code(q->scalar_type())};
+    bl_status status;
+    {
+        WithoutGil release;
+        status = bl_attn_paged(&p, cache.stream);
+    }
+    return status == BL_OK ? THPVariable_Wrap(out) : PyLong_FromLong(status);
+    END_HANDLE_TH_ERRORS
+}
+
 // The prepared launches: launch(which, items, M, workspace) -> bl_status, on the current stream; None if `items`, a ctypes array (for
-// the last two the argument struct), does not hold whole ones of that launch's.
-enum { kGemvBatch, kDecodeBatch, kQuantBatch, kDecodeNormBatch, kTl2Batch, kAttnDecode, kAttn8Decode, kLaunches };
+// the last three the argument struct), does not hold whole ones of that launch's.
+enum { kGemvBatch, kDecodeBatch, kQuantBatch, kDecodeNormBatch, kTl2Batch, kAttnDecode, kAttn8Decode, kAttnPaged, kLaunches };
 
 PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
@@ -415,7 +512,7 @@ PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     void* workspace = PyLong_AsVoidPtr(args[3]);
     if (PyErr_Occurred()) return nullptr;
     constexpr size_t kSizes[kLaunches] = {sizeof(bl_gemv_item), sizeof(bl_decode_item), sizeof(bl_quant_item),
-                                          sizeof(bl_decode_norm_item), sizeof(bl_gemv_item), sizeof(bl_attn_args), sizeof(bl_attn8_args)};
+                                          sizeof(bl_decode_norm_item), sizeof(bl_gemv_item), sizeof(bl_attn_args), sizeof(bl_attn8_args), sizeof(bl_attn_paged_args)};
     if (which < 0 || which >= kLaunches) Py_RETURN_NONE;
     Memory items(args[1], kSizes[which]);
     if (!items.ok || items.view.len % kSizes[which] != 0 || items.view.len / kSizes[which] > INT32_MAX) Py_RETURN_NONE;
@@ -431,6 +528,7 @@ PyObject* launch(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             case kDecodeNormBatch: status = bl_decode_norm_batch(items.as<const bl_decode_norm_item>(), n, workspace, stream); break;
             case kTl2Batch: status = bl_tl2_gemv_batch(items.as<const bl_gemv_item>(), n, workspace, stream); break;
             case kAttnDecode: status = bl_attn_decode(items.as<const bl_attn_args>(), stream); break;
+            case kAttnPaged: status = bl_attn_paged(items.as<const bl_attn_paged_args>(), stream); break;
             case kAttn8Decode: status = bl_attn8_decode(items.as<const bl_attn8_args>(), stream); break;
         }
     }
@@ -446,7 +544,7 @@ PyObject* stream(PyObject*, PyObject*) {
 
 #define BL_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {BL_FAST(quant_act), BL_FAST(product), BL_FAST(gemm_batch), BL_FAST(norm_quant), BL_FAST(final_norm), BL_FAST(kv8_write), BL_FAST(kv8_read),
-                         BL_FAST(attn_prefill8), BL_FAST(launch),
+                         BL_FAST(attn_prefill8), BL_FAST(paged_append), BL_FAST(attn_paged), BL_FAST(launch),
                          {"stream", stream, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -298,6 +298,10 @@ int64_t attn8_scratch_bytes(int n_heads, int group, int head_dim, int max_pos, i
 hipError_t launch_attn8_decode(const ::bl_attn8_args& a, hipStream_t s);
 int64_t attn8_prefill_scratch_bytes(int n_heads, int group, int head_dim, int pos0, int M);
 hipError_t launch_attn8_prefill(const ::bl_attn8_prefill_args& a, hipStream_t s);
+// The paged cache (bl_paged_append.hip) and the attention over it (bl_paged.hip).
+hipError_t launch_paged_append(const ::bl_paged_append_args& a, hipStream_t s);
+int64_t paged_scratch_bytes(int n_heads, int group, int head_dim, int sequences, int rows, int max_pos, bool single);
+hipError_t launch_attn_paged(const ::bl_attn_paged_args& a, hipStream_t s);
 
 // The calling thread's most recent product launch: kernel template instance and grid, for tools that label what they
 // time (bl_last_kernel).  Only the pieces are stored at launch time; the text is formatted on request.

@@ -1,0 +1,308 @@
+// The paged key/value cache (bl_paged_cache): its layout, the rows of a call, and how 32 positions get into LDS.
+//
+// A pool of pages; a page holds page_size positions of every key head, [page][key head][position][element], bf16, rows of paged_width(head_dim)
+// elements.  Positions 16 n .. 16 n + 15 of a sequence lie behind each other whatever the page size (a power of two, 16 at least), so
+// everything here goes by sixteens: one entry of the sequence's line of the table, one address.
+#pragma once
+#include "bl_internal.hpp"
+#include "bl_lanes.hpp"
+
+namespace bl {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Elements of a stored row: whole sixteens that the matrix instructions take without a remainder worth speaking of.
+constexpr int paged_width(int head_dim) {
+    return head_dim <= 32 ? 32 : head_dim <= 48 ? 48 : head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : head_dim <= 128 ? 128 : head_dim <= 192 ? 192 : 256;
+}
+
+// The cache and a call's rows as the kernels see them.
+struct Paged {
+    uint16_t*      k;
+    uint16_t*      v;
+    const int32_t* table;      // [sequences][table_width]
+    const int32_t* pos;        // [sequences]
+    const int32_t* start;      // [sequences + 1]; null: row b is sequence b's only one
+    int32_t        n_heads, head_dim, page_shift, pages, table_width, sequences, rows, max_pos;
+};
+
+inline Paged paged_of(const ::bl_paged_cache& c, const ::bl_paged_rows& r) {
+    Paged p;
+    p.k = c.k_pages_dev; p.v = c.v_pages_dev;
+    p.table = r.table_dev; p.pos = r.pos_dev; p.start = r.start_dev;
+    p.n_heads = c.n_heads; p.head_dim = c.head_dim; p.page_shift = 0;
+    while ((1 << p.page_shift) < c.page_size) ++p.page_shift;
+    p.pages = c.pages; p.table_width = r.table_width; p.sequences = r.sequences; p.rows = r.rows; p.max_pos = r.max_pos;
+    return p;
+}
+
+// Numbers that nothing in a launch writes, by scalar loads (the index is uniform).
+__device__ __forceinline__ int32_t scalar_word(const int32_t* at, int64_t i) {
+    return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)at)[i];
+}
+
+struct PagedSequence {
+    int first, rows, pos;      // its rows of the call (0: it takes no part), and the position of the first
+};
+// What the device's words say is looked at before anything is addressed with it.
+__device__ __forceinline__ PagedSequence paged_sequence(const Paged& p, int first, int end, int pos) {
+    const bool takes_part = first >= 0 && end >= first && end <= p.rows && pos >= 0 && end - first <= p.max_pos && pos <= p.max_pos - (end - first);
+    return takes_part ? PagedSequence{first, end - first, pos} : PagedSequence{0, 0, 0};
+}
+__device__ __forceinline__ PagedSequence paged_sequence(const Paged& p, int b) {   // any lane's own
+    return p.start ? paged_sequence(p, p.start[b], p.start[b + 1], p.pos[b]) : paged_sequence(p, b, b + 1, p.pos[b]);
+}
+__device__ __forceinline__ PagedSequence paged_sequence_uniform(const Paged& p, int b) {
+    const int pos = scalar_word(p.pos, b);
+    return p.start ? paged_sequence(p, scalar_word(p.start, b), scalar_word(p.start, b + 1), pos) : paged_sequence(p, b, b + 1, pos);
+}
+
+__device__ __forceinline__ int wave_inclusive_sum(int v, int lane) {
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+        const int other = __shfl_up(v, step);
+        if (lane >= step) v += other;
+    }
+    return v;
+}
+
+// The sequences, in order, have count(sequence) items of work each: whose is item `item`, and which of its items is it?  Also how many there are
+// before the sequence's first.  By every wave for itself, a lane for every (sequences / 64) of them.  False: there are fewer.
+template <typename Count>
+__device__ __forceinline__ bool paged_find(const Paged& p, int lane, int item, const Count& count, int& b, int& index, int& before, PagedSequence& s) {
+    if (p.sequences == 1) {
+        b = before = 0;
+        index = item;
+        s = paged_sequence_uniform(p, 0);
+        return item < count(s);
+    }
+    const int each = (p.sequences + 63) >> 6;
+    int sum = 0;
+    for (int i = 0; i < each; ++i)
+        if (lane * each + i < p.sequences) sum += count(paged_sequence(p, lane * each + i));
+    const int upto = wave_inclusive_sum(sum, lane);
+    const unsigned long long later = __ballot(item < upto);
+    if (later == 0) return false;
+    const int which = __builtin_ctzll(later);
+    before = __builtin_amdgcn_readlane(upto - sum, which);
+    b = which * each;
+    for (;; ++b) {          // (the item is one of this lane's sequences')
+        s = paged_sequence_uniform(p, b);
+        const int n = count(s);
+        if (item - before < n) break;
+        before += n;
+    }
+    index = item - before;
+    return true;
+}
+
+// ---- 32 positions of one key head in LDS: rows of 32 KS bytes, their 16-byte pieces moved about so that the reads of the products meet
+// all banks: keys by one piece of 16 or 32 rows, values by 32 bytes of four.  Every pattern repeats after 16 rows.
+template <int KS>
+__device__ __forceinline__ int paged_k_place(int row, int c) {
+    return KS == 8 || KS == 16 ? c ^ (row & 15) : KS == 4 || KS == 12 ? c ^ ((row >> 1) & 7) : KS == 2 || KS == 6 ? c ^ ((row >> 2) & 3) : c;
+}
+template <int KS>
+__device__ __forceinline__ int paged_v_place(int row, int c) {
+    return KS == 8 || KS == 16 ? c ^ ((row & 3) << 2) : KS == 4 || KS == 12 ? c ^ (((row >> 1) & 1) << 2) : c;
+}
+
+// Addresses of the two sixteens of 32 positions of one key head, in the keys' pool or the values' (offsets in bytes).
+struct PagedBase {
+    int64_t at[2];
+    bool    bad;     // the table names a page that is not there
+};
+// line: the sequence's line of the table; last: its last position.  Sixteens behind it are not looked up.
+template <int KS>
+__device__ __forceinline__ PagedBase paged_base(const Paged& p, const int32_t* line, int head, int j0, int last) {
+    PagedBase r;
+    r.bad = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int j = min(j0 + 16 * h, last);
+        int page = __builtin_amdgcn_readfirstlane(scalar_word(line, j >> p.page_shift));
+        if ((uint32_t)page >= (uint32_t)p.pages) {
+            page = 0;
+            r.bad = true;
+        }
+        const int inside = j & ((1 << p.page_shift) - 1) & ~15;
+        r.at[h] = ((((int64_t)page * p.n_heads + head) << p.page_shift) + inside) * (32 * KS);
+    }
+    return r;
+}
+
+template <int KS>
+struct PagedTile {
+    static constexpr int kRow = 32 * KS;
+    static constexpr int kBytes = 32 * kRow;                      // KS pieces of 1 KiB
+    static constexpr bool kWhole = KS % 2 == 0;                   // a piece lies in one sixteen
+    static constexpr int kKept = kWhole ? KS / 2 : KS;            // offsets of a lane
+};
+
+// A lane's place in piece s: row and byte offset in the row's memory.
+template <int KS, bool VALUE>
+__device__ __forceinline__ void paged_piece(int s, int lane, int& row, int& byte) {
+    const int at = s * 64 + lane;
+    row = at / (2 * KS);
+    const int place = at % (2 * KS);
+    byte = (VALUE ? paged_v_place<KS>(row, place) : paged_k_place<KS>(row, place)) * 16;
+}
+
+template <int KS>
+struct PagedRequest {
+    uint32_t off[PagedTile<KS>::kKept];   // in a sixteen (or, odd KS, in 32 rows)
+    template <bool VALUE>
+    __device__ __forceinline__ void prepare(int lane) {
+#pragma unroll
+        for (int s = 0; s < PagedTile<KS>::kKept; ++s) {
+            int row, byte;
+            paged_piece<KS, VALUE>(s, lane, row, byte);
+            off[s] = (uint32_t)(row * PagedTile<KS>::kRow + byte);
+        }
+    }
+    // KS pieces on their way to LDS address dst.  limit: the last of the 32 rows that the sequence has (rows behind it repeat that one).
+    template <bool VALUE>
+    __device__ __forceinline__ void send(const uint16_t* pool, const PagedBase& base, uint32_t dst, int limit, int lane) const {
+        const uint8_t* from[2] = {reinterpret_cast<const uint8_t*>(pool) + base.at[0], reinterpret_cast<const uint8_t*>(pool) + base.at[1]};
+        constexpr int kRow = PagedTile<KS>::kRow;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+        if (PagedTile<KS>::kWhole && limit >= 31) {   // uniform
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const uint8_t* src = uniform_ptr(from[2 * s / KS]);
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                             ::"s"(dst + 1024 * s), "v"(off[s % PagedTile<KS>::kKept]), "s"(src) : "memory", "m0");
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                int row, byte;
+                paged_piece<KS, VALUE>(s, lane, row, byte);
+                row = min(row, limit);
+                const uint8_t* src = (row < 16 ? from[0] : from[1]) + (row & 15) * kRow + byte;
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + 1024 * s), "v"(src) : "memory", "m0");
+            }
+        }
+#pragma clang diagnostic pop
+    }
+};
+
+__device__ __forceinline__ uint32_t lds_address(const void* at) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)at; }
+
+// ---- operands
+
+__device__ __forceinline__ uint32_t paged_bf16_pair(float a, float b) {   // rounded to nearest even, the first in the low half
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// Two numbers as PIECES bf16 numbers each, the first one's in the low halves: one, rounded, or three by cutting off 8 bits at a time, whose sum
+// is the number itself (24 bits; nothing rounds up to an infinity).
+template <int PIECES>
+__device__ __forceinline__ void paged_split(float a, float b, uint32_t (&out)[PIECES]) {
+    if constexpr (PIECES == 1) {
+        out[0] = paged_bf16_pair(a, b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+            out[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            a -= __uint_as_float(x & 0xffff0000u);
+            b -= __uint_as_float(y & 0xffff0000u);
+        }
+    }
+}
+
+// Eight elements e .. e + 7 of a row's query (zeros from head_dim on; head_dim is a multiple of four, e of eight) as operand pieces.
+template <int PIECES>
+__device__ __forceinline__ void paged_query(const void* q, int64_t row_at, int e, int head_dim, bool there, s16x8 (&out)[PIECES]) {
+    uint32_t parts[PIECES][4];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) parts[i][j] = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (!there || e + 4 * h >= head_dim) continue;
+        if constexpr (PIECES == 1) {
+            typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(2)));
+            const u32x2_u x = *reinterpret_cast<const u32x2_u*>(static_cast<const uint16_t*>(q) + row_at + e + 4 * h);
+            parts[0][2 * h] = x[0];
+            parts[0][2 * h + 1] = x[1];
+        } else {
+            typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+            const f32x4_u x = *reinterpret_cast<const f32x4_u*>(static_cast<const float*>(q) + row_at + e + 4 * h);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t two[PIECES];
+                paged_split<PIECES>(x[2 * j], x[2 * j + 1], two);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) parts[i][2 * h + j] = two[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) out[i] = __builtin_bit_cast(s16x8, (u32x4{parts[i][0], parts[i][1], parts[i][2], parts[i][3]}));
+}
+
+// Whether a bf16 number is an infinity or NaN, of the two in a word: the largest exponents seen, to be told at the end.
+__device__ __forceinline__ uint32_t paged_exponents(uint32_t most, uint32_t word) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const u16x2 a = __builtin_bit_cast(u16x2, most), b = __builtin_bit_cast(u16x2, word & 0x7f807f80u);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, b));
+}
+__device__ __forceinline__ bool paged_not_finite(uint32_t most) { return (most & 0xffffu) == 0x7f80u || most >> 16 == 0x7f80u; }
+
+// Values with infinities and NaN put away: the finite ones, and ones where +infinity (or NaN) and -infinity (or NaN) were.
+__device__ __forceinline__ void paged_put_away(const s16x8& v, s16x8& finite, s16x8& up, s16x8& down) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t x = (uint16_t)v[i], size = x & 0x7fffu;
+        const bool odd = size >= 0x7f80u, nan = size > 0x7f80u;
+        finite[i] = odd ? (short)0 : v[i];
+        up[i] = odd && (nan || x < 0x8000u) ? (short)0x3f80 : (short)0;
+        down[i] = odd && (nan || x >= 0x8000u) ? (short)0x3f80 : (short)0;
+    }
+}
+
+// A row's four outputs.
+template <bool BF16>
+__device__ __forceinline__ void paged_store(void* out, int64_t at, const f32x4& x) {
+    if constexpr (BF16) {
+        typedef uint32_t u32x2_u __attribute__((ext_vector_type(2), aligned(2)));
+        *reinterpret_cast<u32x2_u*>(static_cast<uint16_t*>(out) + at) = u32x2_u{paged_bf16_pair(x[0], x[1]), paged_bf16_pair(x[2], x[3])};
+    } else {
+        typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+        *reinterpret_cast<f32x4_u*>(static_cast<float*>(out) + at) = x;
+    }
+}
+
+// ---- the attention's launches
+
+constexpr int kPagedFew = 16;         // rows of a sequence and key head up to which the rows form takes it
+constexpr int kPagedLeast = 256;      // fewest positions of a workgroup that shares a walk
+constexpr int kPagedMostSplits = 256; // workgroups that share a walk in the rows form
+
+struct PagedArgs {
+    Paged       c;
+    const void* q;
+    void*       out;
+    uint32_t*   counters;      // rows form: [sequence][key head]
+    float*      figures;       // rows form: [workgroup][row][2 + width]; tiles form: [workgroup][row][2 + width]
+    int32_t     group;         // query heads per key head
+    int32_t     few;           // rows up to which the rows form takes a sequence (0: the tiles form takes all)
+    int32_t     slot_rows;     // rows of a slot of the rows form
+    int32_t     splits;        // tiles form: workgroups that may share a walk
+    float       target;        // rows form: 1 / workgroups that the whole walk is meant for
+    float       scale;         // log2(e) / sqrt(head_dim)
+};
+
+}  // namespace bl

@@ -236,6 +236,132 @@ def attn_prefill8(q_lin: torch.Tensor, k_lin: torch.Tensor, v_lin: torch.Tensor,
     return out
 
 
+class PagedCache:
+    """A pool of pages for the keys and values of one layer (bl_paged_cache), shared by any number of sequences: k and v are [pages, n_heads, page_size,
+    width] bf16, width the head size rounded up (bl_paged_width).  Which pages a sequence has is the caller's: see PagedRows."""
+
+    def __init__(self, n_heads: int, head_dim: int, page_size: int, pages: int, device, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+        width = B.bl_paged_width(head_dim)
+        if width == 0 or n_heads < 1 or pages < 1 or not B.BL_PAGE_MIN <= page_size <= B.BL_PAGE_MAX or page_size & (page_size - 1):
+            raise B.BitLinearError(B.BL_ERR_SHAPE, "PagedCache")
+        self.n_heads, self.head_dim, self.page_size, self.pages, self.hidden = n_heads, head_dim, page_size, pages, n_heads * head_dim
+        shape = (pages, n_heads, page_size, width)
+        self.k, self.v = (t if t is not None else torch.zeros(shape, dtype=torch.bfloat16, device=device) for t in (k, v))
+        for t in (self.k, self.v):
+            assert t.dtype == torch.bfloat16 and t.shape == shape and t.is_contiguous() and t.device == self.k.device
+        self.args = B.PagedCache(self.k.data_ptr(), self.v.data_ptr(), n_heads, head_dim, page_size, pages)
+
+    def _here(self, *tensors):
+        """The launch goes to the current device's stream: everything has to be there."""
+        dev = self.k.device
+        assert dev.type == "cuda" and dev.index == torch.cuda.current_device(), "the cache is not on the current device"
+        assert all(t is None or t.device == dev for t in tensors), "tensors and cache on different devices"
+
+    def append(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rows: "PagedRows", table: Optional[torch.Tensor], g_q: Optional[torch.Tensor] = None,
+               g_k: Optional[torch.Tensor] = None, eps: float = EPS, q_dtype: Optional[torch.dtype] = None, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """bl_paged_append: the rows' keys (normed per head by g_k [head_dim], rotated) and values into their pages; returns the queries (normed by g_q,
+        rotated), in q_dtype (default: q's) or in q_out.  q [rows, n_q_heads * head_dim], k, v [rows, n_heads * head_dim], fp32 or bf16, rows anywhere.
+        table: the rotary table, up to rows.max_pos; None: no rotation."""
+        c = B.calls()
+        q_dtype = q.dtype if q_dtype is None else q_dtype
+        r = None
+        if c and q_dtype in (torch.float32, torch.bfloat16):
+            r = c.paged_append(self.args, self.k, rows.args, rows.table, q, k, v, g_q, g_k, eps, table, q_out, q_dtype == torch.bfloat16)
+        if r is not None:
+            if type(r) is int:
+                raise B.BitLinearError(r, "bl_paged_append")
+            return r
+        self._here(q, k, v, rows.table, table, g_q, g_k, q_out)
+        d, T = self.head_dim, rows.rows
+        assert q.shape[0] == T and q.dim() == 2 and q.shape[1] % d == 0 and k.shape == v.shape == (T, self.hidden) and q.dtype == k.dtype == v.dtype
+        assert q.stride(1) == k.stride(1) == v.stride(1) == 1
+        ld = [max(int(t.stride(0)), int(t.shape[1])) if T > 1 else int(t.shape[1]) for t in (q, k, v)]
+        assert all(T <= 1 or t.stride(0) >= t.shape[1] for t in (q, k, v))
+        for g in (g_q, g_k):
+            assert g is None or (g.dtype == torch.float32 and g.shape == (d,) and g.is_contiguous())
+        assert table is None or (table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (d // 2, 2) and table.shape[0] >= rows.max_pos)
+        if q_out is None:
+            q_out = torch.empty((T, int(q.shape[1])), dtype=q_dtype, device=q.device)
+        assert q_out.shape == q.shape and q_out.is_contiguous()
+        ptr = lambda t: t.data_ptr() if t is not None else 0
+        B.bl_paged_append(self.args, rows.args, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), *ld, ops._dtype_code(q), ops._dtype_code(q_out),
+                          int(q.shape[1]) // d, ptr(g_q), ptr(g_k), eps, ptr(table), _stream())
+        return q_out
+
+
+class PagedRows:
+    """The rows of a call over a paged cache (bl_paged_rows).  table [sequences, width] int32: the pages of every sequence, in order; pos [sequences] int32:
+    the position of its first row; start [sequences + 1] int32: its rows are start[b] .. start[b + 1] - 1 of the call's `rows` (without: one row each).
+    No position is max_pos or beyond.  All of it is read on the device at the launch, so the tensors may be changed in place between launches."""
+
+    def __init__(self, table: torch.Tensor, pos: torch.Tensor, max_pos: int, start: Optional[torch.Tensor] = None, rows: Optional[int] = None):
+        n = int(pos.shape[0])
+        assert table.dim() == 2 and table.shape[0] == n and (start is None or start.shape == (n + 1,))
+        for t in (table, pos, start):
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == table.device)
+        if rows is None:
+            if start is not None:
+                raise ValueError("rows: how many rows the call has at most")
+            rows = n
+        self.table, self.pos, self.start, self.max_pos, self.rows, self.sequences = table, pos, start, max_pos, rows, n
+        self.args = B.PagedRows(table.data_ptr(), pos.data_ptr(), start.data_ptr() if start is not None else None, int(table.shape[1]), n, rows, max_pos)
+
+
+def paged_scratch(n_heads: int, cache: PagedCache, rows: PagedRows) -> torch.Tensor:
+    """Scratch memory for attn_paged calls of n_heads query heads with as many sequences and rows (or fewer): zero, and kept usable by every call.  Calls
+    that may overlap in time need one each."""
+    bytes_ = B.bl_attn_paged_scratch_bytes(n_heads, cache.n_heads, cache.head_dim, rows.sequences, rows.rows, rows.max_pos, rows.start is None)
+    if bytes_ == 0:
+        raise B.BitLinearError(B.BL_ERR_SHAPE, "paged_scratch")
+    return torch.zeros(bytes_, dtype=torch.uint8, device=cache.k.device)
+
+
+def _check_paged(q, cache, rows, scratch, out):
+    cache._here(q, rows.table, scratch, out)
+    assert q.dim() == 2 and q.shape[0] == rows.rows and q.shape[1] % cache.head_dim == 0 and q.is_contiguous()
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+    bytes_ = B.bl_attn_paged_scratch_bytes(int(q.shape[1]) // cache.head_dim, cache.n_heads, cache.head_dim, rows.sequences, rows.rows, rows.max_pos, rows.start is None)
+    if bytes_ == 0:
+        raise B.BitLinearError(B.BL_ERR_SHAPE, "bl_attn_paged")
+    assert scratch.dtype == torch.uint8 and scratch.is_contiguous() and scratch.numel() >= bytes_, "scratch: see paged_scratch"
+
+
+def attn_paged(q: torch.Tensor, cache: PagedCache, rows: PagedRows, scratch: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bl_attn_paged: every row of q ([rows, n_heads * head_dim] fp32 or bf16, as PagedCache.append leaves it) against its sequence's positions up to its
+    own.  Rows that no sequence has stay as they are in out."""
+    c = B.calls()
+    r = c.attn_paged(cache.args, cache.k, rows.args, rows.table, q, scratch, out) if c else None
+    if r is not None:
+        if type(r) is int:
+            raise B.BitLinearError(r, "bl_attn_paged")
+        return r
+    out = torch.empty_like(q) if out is None else out
+    _check_paged(q, cache, rows, scratch, out)
+    B.bl_attn_paged(B.make_attn_paged_args(cache.args, rows.args, q.data_ptr(), out.data_ptr(), scratch.data_ptr(), int(q.shape[1]) // cache.head_dim,
+                                           ops._dtype_code(q)), _stream())
+    return out
+
+
+class AttentionPaged:
+    """A prepared bl_attn_paged call on tensors that stay: q and out [rows, n_heads * head_dim] fp32 or bf16.  scratch: shared with other launches of the
+    same stream (paged_scratch), or its own."""
+
+    def __init__(self, n_heads: int, cache: PagedCache, rows: PagedRows, q: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 scratch: Optional[torch.Tensor] = None):
+        assert q.shape[1] == n_heads * cache.head_dim
+        self.n_heads, self.cache, self.rows, self.q = n_heads, cache, rows, q
+        self.scratch = scratch if scratch is not None else paged_scratch(n_heads, cache, rows)
+        self.out = out if out is not None else torch.zeros_like(q)
+        _check_paged(q, cache, rows, self.scratch, self.out)
+        self._device = cache.k.device.index
+        self.args = B.make_attn_paged_args(cache.args, rows.args, q.data_ptr(), self.out.data_ptr(), self.scratch.data_ptr(), n_heads, ops._dtype_code(q))
+
+    def launch(self):
+        assert torch.cuda.current_device() == self._device, "the cache is not on the current device"
+        B.launch(B.LAUNCH_ATTN_PAGED, self.args, 1)
+        return self.out
+
+
 class NormDecodeGroup:
     """A prepared bl_decode_norm_batch launch: RMSNorm (with an optional residual add) folded into the quantizer of
     the products that consume the normalised row.  weights share x / delta / gamma; h_out receives x + delta.
