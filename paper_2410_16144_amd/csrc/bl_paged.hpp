@@ -65,43 +65,17 @@ __device__ __forceinline__ PagedSequence paged_sequence_uniform(const Paged& p, 
     return p.start ? paged_sequence(p, scalar_word(p.start, b), scalar_word(p.start, b + 1), pos) : paged_sequence(p, b, b + 1, pos);
 }
 
-__device__ __forceinline__ int wave_inclusive_sum(int v, int lane) {
-#pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-        const int other = __shfl_up(v, step);
-        if (lane >= step) v += other;
-    }
+// Sum over this lane and those before it, on the vector ALU's lane moves.
+__device__ __forceinline__ int wave_inclusive_sum(int v) {
+#define BL_BEFORE(ctrl, rows) __builtin_amdgcn_update_dpp(0, v, (ctrl), (rows), 0xf, false)
+    v += BL_BEFORE(0x111, 0xf);    // row_shr 1, 2, 4, 8
+    v += BL_BEFORE(0x112, 0xf);
+    v += BL_BEFORE(0x114, 0xf);
+    v += BL_BEFORE(0x118, 0xf);
+    v += BL_BEFORE(0x142, 0xa);    // row 0's and 2's last lane to the row behind it
+    v += BL_BEFORE(0x143, 0xc);    // lane 31 to the upper half
+#undef BL_BEFORE
     return v;
-}
-
-// The sequences, in order, have count(sequence) items of work each: whose is item `item`, and which of its items is it?  Also how many there are
-// before the sequence's first.  By every wave for itself, a lane for every (sequences / 64) of them.  False: there are fewer.
-template <typename Count>
-__device__ __forceinline__ bool paged_find(const Paged& p, int lane, int item, const Count& count, int& b, int& index, int& before, PagedSequence& s) {
-    if (p.sequences == 1) {
-        b = before = 0;
-        index = item;
-        s = paged_sequence_uniform(p, 0);
-        return item < count(s);
-    }
-    const int each = (p.sequences + 63) >> 6;
-    int sum = 0;
-    for (int i = 0; i < each; ++i)
-        if (lane * each + i < p.sequences) sum += count(paged_sequence(p, lane * each + i));
-    const int upto = wave_inclusive_sum(sum, lane);
-    const unsigned long long later = __ballot(item < upto);
-    if (later == 0) return false;
-    const int which = __builtin_ctzll(later);
-    before = __builtin_amdgcn_readlane(upto - sum, which);
-    b = which * each;
-    for (;; ++b) {          // (the item is one of this lane's sequences')
-        s = paged_sequence_uniform(p, b);
-        const int n = count(s);
-        if (item - before < n) break;
-        before += n;
-    }
-    index = item - before;
-    return true;
 }
 
 // ---- 32 positions of one key head in LDS: rows of 32 KS bytes, their 16-byte pieces moved about so that the reads of the products meet
@@ -173,6 +147,7 @@ struct PagedRequest {
     __device__ __forceinline__ void send(const uint16_t* pool, const PagedBase& base, uint32_t dst, int limit, int lane) const {
         const uint8_t* from[2] = {reinterpret_cast<const uint8_t*>(pool) + base.at[0], reinterpret_cast<const uint8_t*>(pool) + base.at[1]};
         constexpr int kRow = PagedTile<KS>::kRow;
+        dst = __builtin_amdgcn_readfirstlane(dst);         // (uniform already, as everything here that is no lane's)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
         if (PagedTile<KS>::kWhole && limit >= 31) {   // uniform
@@ -183,10 +158,12 @@ struct PagedRequest {
                              ::"s"(dst + 1024 * s), "v"(off[s % PagedTile<KS>::kKept]), "s"(src) : "memory", "m0");
             }
         } else {
+            int here = lane;
+            asm volatile("" : "+v"(here));                 // (a walk's last request: its addresses take no registers for the length of the walk)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 int row, byte;
-                paged_piece<KS, VALUE>(s, lane, row, byte);
+                paged_piece<KS, VALUE>(s, here, row, byte);
                 row = min(row, limit);
                 const uint8_t* src = (row < 16 ? from[0] : from[1]) + (row & 15) * kRow + byte;
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + 1024 * s), "v"(src) : "memory", "m0");
@@ -204,8 +181,8 @@ __device__ __forceinline__ uint32_t paged_bf16_pair(float a, float b) {   // rou
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
 
-// Two numbers as PIECES bf16 numbers each, the first one's in the low halves: one, rounded, or three by cutting off 8 bits at a time, whose sum
-// is the number itself (24 bits; nothing rounds up to an infinity).
+// Two numbers as PIECES bf16 numbers each, the first one's in the low halves: one, rounded; two, of which the second is the rounded rest (16 bits);
+// three by cutting off 8 bits at a time, whose sum is the number itself (24 bits; nothing rounds up to an infinity).
 template <int PIECES>
 __device__ __forceinline__ void paged_split(float a, float b, uint32_t (&out)[PIECES]) {
     if constexpr (PIECES == 1) {
@@ -213,6 +190,10 @@ __device__ __forceinline__ void paged_split(float a, float b, uint32_t (&out)[PI
     } else {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
+            if (PIECES == 2 && i == 1) {
+                out[i] = paged_bf16_pair(a, b);
+                break;
+            }
             const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
             out[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
             a -= __uint_as_float(x & 0xffff0000u);
@@ -285,24 +266,167 @@ __device__ __forceinline__ void paged_store(void* out, int64_t at, const f32x4& 
     }
 }
 
-// ---- the attention's launches
+// ---- who does what: the attention's launches
+//
+// A sequence's rows of one key head (tokens x query heads of the group, token by token) go by tiles; a tile's walk over the positions up to its last row's
+// may be shared by several workgroups.  How many follows on the device from all positions that the call walks: each workgroup is meant to have
+// an equal share of them, `least` at least.  The grid is an upper bound; workgroups beyond what there is to do end at once.
 
-constexpr int kPagedFew = 16;         // rows of a sequence and key head up to which the rows form takes it
-constexpr int kPagedLeast = 256;      // fewest positions of a workgroup that shares a walk
-constexpr int kPagedMostSplits = 256; // workgroups that share a walk in the rows form
+constexpr int kPagedFew = 16;         // rows of a sequence and key head up to which the rows form takes them
 
 struct PagedArgs {
     Paged       c;
     const void* q;
     void*       out;
-    uint32_t*   counters;      // rows form: [sequence][key head]
-    float*      figures;       // rows form: [workgroup][row][2 + width]; tiles form: [workgroup][row][2 + width]
+    uint32_t*   counters;      // [slot]: tickets of the walks whose first slot it is
+    float*      figures;       // [slot]: maxima, sums and weighted values of a tile's rows, as each form has them
+    int32_t     slot_bytes;
     int32_t     group;         // query heads per key head
-    int32_t     few;           // rows up to which the rows form takes a sequence (0: the tiles form takes all)
-    int32_t     slot_rows;     // rows of a slot of the rows form
-    int32_t     splits;        // tiles form: workgroups that may share a walk
-    float       target;        // rows form: 1 / workgroups that the whole walk is meant for
+    int32_t     tile_rows;
+    int32_t     most;          // workgroups of a walk
+    int32_t     least;         // positions that are worth one
+    int32_t     rounded;       // whether a walk of a part and a bit is two (else one)
+    int32_t     slots;         // of figures
+    float       target;        // key heads / workgroups that the call is meant for
     float       scale;         // log2(e) / sqrt(head_dim)
 };
+
+struct PagedWork {
+    PagedSequence s;
+    int b, head;
+    int row0, rows;            // the tile's rows, of the sequence's
+    int low, reach;            // the last position that its first row sees; positions that its last row sees
+    int part, parts;           // which of the walk's workgroups this is
+    int slot;                  // of the walk's first part; its others' behind it
+};
+
+__device__ __forceinline__ int paged_tiles(const PagedArgs& p, int rows) { return (int)(((int64_t)rows * p.group + p.tile_rows - 1) / p.tile_rows); }
+// (Rounded up, or, where joining parts is dear, down.)
+__device__ __forceinline__ int paged_parts(const PagedArgs& p, const PagedSequence& s, int per) {
+    const int reach = s.pos + s.rows;
+    return min(max((reach + p.rounded * (per - 1)) / per, 1), p.most);
+}
+
+// Uniform numbers, in scalar registers: divisions leave them in vector ones.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// What the call walks of a sequence, in positions (its tiles' mean).
+__device__ __forceinline__ float paged_cost(const PagedArgs& p, const PagedSequence& s) {
+    return s.rows ? (float)paged_tiles(p, s.rows) * ((float)(s.pos + s.rows) - 0.5f * (float)(s.rows - 1)) : 0.0f;
+}
+
+// By every wave for itself, a lane for every (sequences / 64) of them.  False: nothing to do.
+__device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWork& w) {
+    const Paged& c = p.c;
+    const int item = uniform((int)blockIdx.x / c.n_heads), items = uniform((int)gridDim.x / c.n_heads);
+    w.head = (int)blockIdx.x - item * c.n_heads;
+    const int each = (c.sequences + 63) >> 6;
+    int index = item, first_slot = 0, per;
+    // (a little more than the quotient, so that there are never more parts than the grid has: see paged_plan)
+    const auto share = [&](float cost) { return __builtin_amdgcn_readfirstlane(max(p.least, (int)fminf(cost * p.target * 1.0001f, 2.0e9f) + 1)); };
+    if (c.sequences == 1) {
+        w.b = 0;
+        w.s = paged_sequence_uniform(c, 0);
+        per = share(paged_cost(p, w.s));
+    } else {
+        PagedSequence mine{0, 0, 0};
+        float cost = 0.0f;
+        for (int i = 0; i < each; ++i)
+            if (lane * each + i < c.sequences) {
+                mine = paged_sequence(c, lane * each + i);
+                cost += paged_cost(p, mine);
+            }
+        per = share(over_lanes<64>(cost, AddOp()));
+        int sum = 0, shared = 0;
+        const auto count = [&](const PagedSequence& s, int& n, int& shared_n) {
+            const int parts = s.rows ? paged_parts(p, s, per) : 0;
+            n = parts ? paged_tiles(p, s.rows) * parts : 0;
+            shared_n = parts > 1 ? n : 0;
+        };
+        for (int i = 0; i < each; ++i)
+            if (lane * each + i < c.sequences) {
+                if (each > 1) mine = paged_sequence(c, lane * each + i);
+                int n, shared_n;
+                count(mine, n, shared_n);
+                sum += n;
+                shared += shared_n;
+            }
+        const int upto = wave_inclusive_sum(sum), shared_upto = wave_inclusive_sum(shared);
+        const unsigned long long later = __ballot(item < upto);
+        if (later == 0) return false;
+        const int which = __builtin_ctzll(later);
+        index = item - __builtin_amdgcn_readlane(upto - sum, which);
+        first_slot = __builtin_amdgcn_readlane(shared_upto - shared, which);
+        for (w.b = which * each;; ++w.b) {                 // (the item is one of this lane's sequences')
+            w.s = paged_sequence_uniform(c, w.b);
+            int n, shared_n;
+            count(w.s, n, shared_n);
+            if (index < n) break;
+            index -= n;
+            first_slot += shared_n;
+        }
+    }
+    if (w.s.rows == 0) return false;
+    const int tiles = uniform(paged_tiles(p, w.s.rows)), all = w.s.rows * p.group;
+    w.parts = uniform(paged_parts(p, w.s, per));
+    const int turn = uniform(index / w.parts);
+    w.part = index - turn * w.parts;
+    if (turn >= tiles || item - w.part + w.parts > items) return false;   // (a walk that the grid has no room for, as where sequences overlap: nobody's)
+    w.row0 = (tiles - 1 - turn) * p.tile_rows;             // the longest walk first
+    w.rows = min(p.tile_rows, all - w.row0);
+    w.low = w.s.pos + uniform(w.row0 / p.group);
+    w.reach = w.s.pos + uniform((w.row0 + w.rows - 1) / p.group) + 1;
+    w.slot = (first_slot + turn * w.parts) * c.n_heads + w.head * w.parts;
+    if (w.parts > 1 && w.slot + w.parts > p.slots) {       // (never, see paged_plan)
+        if (w.part) return false;
+        w.parts = 1;
+    }
+    return true;
+}
+
+__device__ __forceinline__ int64_t paged_row_at(const PagedArgs& p, const PagedWork& w, int row) {   // of q and out; row of the tile
+    const int of = w.row0 + row, token = of / p.group;
+    return (((int64_t)(w.s.first + token) * p.c.n_heads + w.head) * p.group + of - token * p.group) * p.c.head_dim;
+}
+
+// ---- the parts of a walk meet
+//
+// Every part's figures travel by device-scope stores of 16 bytes, performed past the dies' caches; every thread waits until its own have been
+// performed, then the workgroup draws a ticket, and the one that draws the last reads all of them, by device-scope loads, and adds them up in the
+// parts' order.  Nobody waits for anybody.
+
+constexpr int kDeviceScope = 16;       // the buffer instructions' sc1
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t paged_resource(float* at) { return __builtin_amdgcn_make_buffer_rsrc(at, 0, -1, 0x00027000); }
+__device__ __forceinline__ float* paged_slot(const PagedArgs& p, int slot) {
+    return reinterpret_cast<float*>(const_cast<uint8_t*>(uniform_ptr(reinterpret_cast<const uint8_t*>(p.figures) + (int64_t)slot * p.slot_bytes)));
+}
+__device__ __forceinline__ void paged_leave(__amdgpu_buffer_rsrc_t slot, int byte, const f32x4& x) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), slot, byte, 0, kDeviceScope);
+}
+__device__ __forceinline__ f32x4 paged_read(__amdgpu_buffer_rsrc_t slot, int byte) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slot, byte, 0, kDeviceScope));
+}
+__device__ __forceinline__ float2 paged_read_pair(__amdgpu_buffer_rsrc_t slot, int byte) {
+    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(slot, byte, 0, kDeviceScope);
+    return make_float2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+
+// Whether this workgroup is the walk's last, all of whose figures are there now.
+__device__ __forceinline__ bool paged_last(const PagedArgs& p, const PagedWork& w, int& last_one) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t* counter = p.counters + w.slot;
+        last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w.parts - 1);
+        if (last_one) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return last_one != 0;
+}
+
+// The sum of a part's, or a wave's, figures relative to `ref`: nothing of what a row has seen nothing of; NaN weights stay NaN.
+__device__ __forceinline__ float paged_factor(float m, float l, float scale, float ref) {
+    return m == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : __builtin_amdgcn_exp2f(fmaf(m, scale, -ref));
+}
 
 }  // namespace bl

@@ -10,12 +10,11 @@
 //   * Scores are formed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16): a lane has eight of the chunk's weights of ONE row, already laid out as
 //     the operand of O^T += V^T P^T, V^T by the transposing LDS read.  The contraction index runs over the positions in the order of the
 //     result registers: slots 0..3 of lane group g are positions 4 g .. 4 g + 3, slots 4..7 positions 16 + 4 g .. 16 + 4 g + 3.
-//   * fp32 queries and weights enter as three bf16 numbers each, their sum (three products; the operator is bound by memory all the same);
-//     bf16 queries as they are, and their weights rounded to bf16: at most 2^-8 of a weight, as much as the output's own rounding.
+//   * fp32 queries and weights enter as three bf16 numbers each, their sum (three products; the operator is bound by memory all the same); bf16
+//     queries as they are, and their weights as two: off by at most 2^-16 of a weight, far below the output's rounding.
 //   * Running maxima and sums are fp32; the parts of a walk meet in scratch memory in their order, and the workgroup that draws a row's last
 //     ticket adds them up.  Nobody waits for anybody.
 #include "bl_paged.hpp"
-#include "bl_figures.hpp"
 
 namespace bl {
 
@@ -23,14 +22,17 @@ namespace {
 
 constexpr int kWaves = 4;
 
+constexpr int kMostParts = 256;
+
 template <int KS>
 struct RowsLds {
     static constexpr int kWidth = 16 * KS;
     static constexpr int kRing = kWaves * 2 * PagedTile<KS>::kBytes;
     static constexpr int kPitch = kWidth + 4;                           // floats of a row where the waves meet
     static constexpr int kMeet = kWaves * kPagedFew * (kPitch * 4 + 8);
-    static constexpr int kFactors = kPagedFew * kPagedMostSplits * 8;   // the parts' factors
-    static constexpr int kBytes = kRing > kMeet ? (kRing > kFactors ? kRing : kFactors) : (kMeet > kFactors ? kMeet : kFactors);
+    static constexpr int kJoin = kPagedFew * kMostParts * 8 + 256 * 16; // the parts' factors, and the teams' sums
+    static constexpr int kMore = kMeet > kJoin ? kMeet : kJoin;
+    static constexpr int kBytes = kRing > kMore ? kRing : kMore;
     static_assert(kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
 };
 
@@ -42,14 +44,82 @@ __device__ __forceinline__ f32x4 mfma16(const s16x8& a, const s16x8 (&b)[PIECES]
     return c;
 }
 
-// The positions of a part of a walk, in chunks of 32: a walk of so many positions has so many parts.
-__device__ __forceinline__ int rows_parts(int walked, int per) { return walked > 0 ? min((walked - 1) / per + 1, kPagedMostSplits) : 0; }
+// A slot's row: (maximum, sum), two words of padding, the weighted values.
+__device__ __forceinline__ int figure_at(int head_dim, int row, int word) { return (row * (4 + head_dim) + word) * 4; }
+
+// After every thread has left its figures.  factor: LDS of rows * parts pairs, sums of 256 quads; store(row, e, x): four outputs.
+template <typename Store>
+__device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& w, float2* factor, f32x4* sums, int& last_one, const Store& store) {
+    constexpr int kThreads = 256, kAhead = 16;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (!paged_last(p, w, last_one)) return;               // uniform
+    const int d = p.c.head_dim, quads = d >> 2, total = w.rows * quads, parts = w.parts;
+    const __amdgpu_buffer_rsrc_t from = paged_resource(paged_slot(p, w.slot));
+    const int teams = max(1, kThreads / total);            // that share an output's parts, where there are few outputs
+    const int team = teams > 1 ? tid / total : 0;
+    f32x4 a[kAhead];
+    const auto read = [&](int i, int n0) {                 // output quad i of parts n0, n0 + teams, ...
+        const int row = i / quads, at = figure_at(d, row, 4 + 4 * (i - row * quads));
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h)
+            a[h] = paged_read(from, min(n0 + h * teams, parts - 1) * p.slot_bytes + at);
+    };
+    const int i0 = teams > 1 ? tid - team * total : tid;
+    read(min(i0, total - 1), min(team, teams - 1));        // (the first of them travel with the maxima and sums)
+    for (int i = tid; i < w.rows * parts; i += kThreads) { // [row][part]
+        const int row = i / parts;
+        factor[i] = paged_read_pair(from, (i - row * parts) * p.slot_bytes + figure_at(d, row, 0));
+    }
+    __syncthreads();
+    for (int row = wave; row < w.rows; row += kThreads / 64) {
+        float2* mine = factor + row * parts;
+        float m = -INFINITY, l = 0.0f;
+        for (int n = lane; n < parts; n += 64) m = fmaxf(m, mine[n].x);
+        m = over_lanes<64>(m, MaxOp());
+        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
+        for (int n = lane; n < parts; n += 64) l += paged_factor(mine[n].x, mine[n].y, p.scale, ref) * mine[n].y;
+        l = over_lanes<64>(l, AddOp());
+        for (int n = lane; n < parts; n += 64) mine[n].x = paged_factor(mine[n].x, mine[n].y, p.scale, ref) / l;
+    }
+    __syncthreads();
+    for (int i = i0; i < total; i += kThreads) {
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int row = i / quads;
+        if (team < teams)
+            for (int n0 = team; n0 < parts; n0 += kAhead * teams) {
+                if (n0 != team || i != i0) read(i, n0);
+#pragma unroll
+                for (int h = 0; h < kAhead; ++h) {
+                    const int n = n0 + h * teams;
+                    if (n >= parts) continue;
+                    const float2 f = factor[row * parts + n];
+                    if (f.y == 0.0f && f.x == f.x) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
+                    sum += f.x * a[h];
+                }
+            }
+        if (teams > 1) {                                   // (all outputs in one turn)
+            if (team < teams) sums[tid] = sum;
+            break;
+        }
+        store(row, 4 * (i - row * quads), sum);
+    }
+    if (teams > 1) {                                       // uniform
+        __syncthreads();
+        if (tid < total) {
+            f32x4 sum = sums[tid];
+            for (int t = 1; t < teams; ++t) sum += sums[t * total + tid];
+            const int row = tid / quads;
+            store(row, 4 * (tid - row * quads), sum);
+        }
+    }
+}
 
 template <int KS, int PIECES>
 __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs p) {
     using L = RowsLds<KS>;
     using T = PagedTile<KS>;
     constexpr bool kBf16 = PIECES == 1;
+    constexpr int kWeight = kBf16 ? 2 : 3;                 // pieces of a weight
     constexpr int kSteps = (KS + 1) / 2;                   // of 32 elements
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int last_one;
@@ -57,27 +127,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     const int i16 = lane & 15, g = lane >> 4;
     const Paged& c = p.c;
 
-    // ---- whose part of which walk
-    const int each = (int)blockIdx.x / c.n_heads, head = (int)blockIdx.x - each * c.n_heads;
-    const auto walked = [&](const PagedSequence& s) { return s.rows > 0 && s.rows * (int64_t)p.group <= p.few ? s.pos + s.rows : 0; };
-    float total = 0.0f;
-    if (c.sequences == 1) {
-        total = (float)walked(paged_sequence_uniform(c, 0));
-    } else {
-        const int lanes = (c.sequences + 63) >> 6;
-        for (int i = 0; i < lanes; ++i)
-            if (lane * lanes + i < c.sequences) total += (float)walked(paged_sequence(c, lane * lanes + i));
-        total = over_lanes<64>(total, AddOp());
-    }
-    // (a little more than the quotient, so that the parts are never more than the grid: see paged_rows_grid)
-    const int per = max(kPagedLeast, (int)fminf(total * p.target * 1.0001f, 2.0e9f) + 1);
-    int b, part, before;
-    PagedSequence s;
-    if (!paged_find(c, lane, each, [&](const PagedSequence& q) { return rows_parts(walked(q), per); }, b, part, before, s)) return;
-    const int reach = s.pos + s.rows, parts = rows_parts(reach, per), chunks = (reach + 31) >> 5;
-    const int c0 = (int)((int64_t)chunks * part / parts), c1 = (int)((int64_t)chunks * (part + 1) / parts);
-    const int rows = s.rows * p.group;
-    const int32_t* line = c.table + (int64_t)b * c.table_width;
+    PagedWork w;
+    if (!paged_work(p, lane, w)) return;
+    const PagedSequence& s = w.s;
+    const int reach = w.reach, chunks = (reach + 31) >> 5, head = w.head, rows = w.rows;
+    const int c0 = uniform((int)((int64_t)chunks * w.part / w.parts)), c1 = uniform((int)((int64_t)chunks * (w.part + 1) / w.parts));
+    const int32_t* line = c.table + (int64_t)w.b * c.table_width;
 
     // ---- requests
     uint8_t* tile = lds + wave * 2 * T::kBytes;
@@ -96,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     // ---- the rows: operand column i16
     const int token = i16 / p.group;
     const bool there = i16 < rows;
-    const int64_t row_at = ((int64_t)(s.first + token) * c.n_heads + head) * p.group * c.head_dim + (int64_t)(i16 - token * p.group) * c.head_dim;
+    const int64_t row_at = there ? paged_row_at(p, w, i16) : 0;
     const int limit = s.pos + token;                       // the last position that the row sees
     s16x8 q[kSteps][PIECES];
 #pragma unroll
@@ -147,7 +202,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         const float keep = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
         run_m = m_new;
         run_l *= keep;
-        uint32_t w[PIECES][4];
+        uint32_t words[kWeight][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -155,14 +210,14 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
                 const float u = __builtin_amdgcn_exp2f(fmaf(x[h][r], p.scale, -ref)), v = __builtin_amdgcn_exp2f(fmaf(x[h][r + 1], p.scale, -ref));
                 run_l += u;
                 run_l += v;
-                uint32_t two[PIECES];
-                paged_split<PIECES>(u, v, two);
+                uint32_t two[kWeight];
+                paged_split<kWeight>(u, v, two);
 #pragma unroll
-                for (int i = 0; i < PIECES; ++i) w[i][2 * h + (r >> 1)] = two[i];
+                for (int i = 0; i < kWeight; ++i) words[i][2 * h + (r >> 1)] = two[i];
             }
-        s16x8 weights[PIECES];
+        s16x8 weights[kWeight];
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) weights[i] = __builtin_bit_cast(s16x8, (u32x4{w[i][0], w[i][1], w[i][2], w[i][3]}));
+        for (int i = 0; i < kWeight; ++i) weights[i] = __builtin_bit_cast(s16x8, (u32x4{words[i][0], words[i][1], words[i][2], words[i][3]}));
 
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const uint8_t* values = tile + T::kBytes;
@@ -175,7 +230,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         };
         if (!masked) {
 #pragma unroll
-            for (int t = 0; t < KS; ++t) o[t] = mfma16<PIECES>(read_v(t), weights, o[t] * keep);
+            for (int t = 0; t < KS; ++t) o[t] = mfma16<kWeight>(read_v(t), weights, o[t] * keep);
         } else {
             // The end of the walk.  What lies behind the sequence's last row is nobody's (zero here); among several tokens' rows a weight of
             // zero may stand before a value that the row does not see: infinities and NaN are counted apart, by whom they weigh with.
@@ -187,12 +242,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
                 const s16x8 v = read_v(t) & mine;
                 s16x8 finite, up, down;
                 paged_put_away(v, finite, up, down);
-                f32x4 x_t = mfma16<PIECES>(finite, weights, o[t] * keep);
+                f32x4 x_t = mfma16<kWeight>(finite, weights, o[t] * keep);
                 const s16x8 either = up | down;
                 const u32x4 any = __builtin_bit_cast(u32x4, either);
                 if (__any((any[0] | any[1] | any[2] | any[3]) != 0)) {
                     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const f32x4 n_up = mfma16<PIECES>(up, weights, zero), n_down = mfma16<PIECES>(down, weights, zero);
+                    const f32x4 n_up = mfma16<kWeight>(up, weights, zero), n_down = mfma16<kWeight>(down, weights, zero);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         if (n_up[r] > 0.0f) x_t[r] += INFINITY;
@@ -216,112 +271,36 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     for (int t = 0; t < KS; ++t) *reinterpret_cast<f32x4*>(meet + (wave * kPagedFew + i16) * L::kPitch + 16 * t + 4 * g) = o[t];
     __syncthreads();
     const int quads = c.head_dim >> 2;
-    const auto out_at = [&](int r, int e) {
-        const int of = r / p.group;
-        return ((int64_t)(s.first + of) * c.n_heads + head) * p.group * c.head_dim + (int64_t)(r - of * p.group) * c.head_dim + e;
-    };
-    const int stride = 1 + c.head_dim / 2;                 // pairs of a row's figures: (maximum, sum), then the values
-    const auto figures_of = [&](int n, int r) {            // part n of this walk
-        return reinterpret_cast<float2*>(p.figures) + (((int64_t)(before + n) * c.n_heads + head) * p.slot_rows + r) * stride;
-    };
+    const __amdgpu_buffer_rsrc_t slot = paged_resource(paged_slot(p, w.slot + w.part));
+    const auto store = [&](int r, int e, const f32x4& x) { paged_store<kBf16>(p.out, paged_row_at(p, w, r) + e, x); };
     for (int i = tid; i < rows * quads; i += 64 * kWaves) {
         const int r = i / quads, e = 4 * (i - r * quads);
         float2 ml[kWaves];
         float m = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            ml[w] = meet_ml[w * kPagedFew + r];
-            m = fmaxf(m, ml[w].x);
+        for (int n = 0; n < kWaves; ++n) {
+            ml[n] = meet_ml[n * kPagedFew + r];
+            m = fmaxf(m, ml[n].x);
         }
         const float ref = m == -INFINITY ? 0.0f : m * p.scale;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = ml[w].x == -INFINITY ? (ml[w].y == 0.0f ? 0.0f : NAN) : __builtin_amdgcn_exp2f(fmaf(ml[w].x, p.scale, -ref));
-            if (ml[w].y == 0.0f) continue;                 // (a wave that had no chunk, or none that the row sees)
-            l += f * ml[w].y;
-            sum += f * *reinterpret_cast<const f32x4*>(meet + (w * kPagedFew + r) * L::kPitch + e);
+        for (int n = 0; n < kWaves; ++n) {
+            if (ml[n].y == 0.0f) continue;                 // (a wave that had no chunk, or none that the row sees)
+            const float f = paged_factor(ml[n].x, ml[n].y, p.scale, ref);
+            l += f * ml[n].y;
+            sum += f * *reinterpret_cast<const f32x4*>(meet + (n * kPagedFew + r) * L::kPitch + e);
         }
-        if (parts == 1) {
-            paged_store<kBf16>(p.out, out_at(r, e), sum / l);
+        if (w.parts == 1) {
+            store(r, e, sum / l);
         } else {
-            float2* dst = figures_of(part, r);
-            leave_figure(dst + 1 + (e >> 1), sum[0], sum[1]);
-            leave_figure(dst + 2 + (e >> 1), sum[2], sum[3]);
-            if (e == 0) leave_figure(dst, m, l);
+            paged_leave(slot, figure_at(c.head_dim, r, 4 + e), sum);
+            if (e == 0) paged_leave(slot, figure_at(c.head_dim, r, 0), f32x4{m, l, 0.0f, 0.0f});
         }
     }
-    if (parts == 1) return;                                // uniform
-
-    // ---- the walk's parts meet: figures travel by device-scope stores, every thread waits until its own have been performed, then the ticket
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    uint32_t* counter = p.counters + (int64_t)b * c.n_heads + head;
-    if (tid == 0) last_one = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
-    __syncthreads();
-    if (!last_one) return;                                 // uniform
-    float2* factor = reinterpret_cast<float2*>(lds);       // [row][part]: (maximum, sum), then (factor, -)
-    for (int i = tid; i < rows * parts; i += 64 * kWaves) {
-        const int r = i / parts;
-        factor[i] = read_figure(figures_of(i - r * parts, r));
-    }
-    __syncthreads();
-    for (int r = wave; r < rows; r += kWaves) {
-        float2* mine = factor + r * parts;
-        float m = -INFINITY, l = 0.0f;
-        for (int n = lane; n < parts; n += 64) m = fmaxf(m, mine[n].x);
-        m = over_lanes<64>(m, MaxOp());
-        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
-        const auto factor_of = [&](const float2& f) {      // (a part that the row sees nothing of: nothing)
-            return f.x == -INFINITY ? (f.y == 0.0f ? 0.0f : NAN) : __builtin_amdgcn_exp2f(fmaf(f.x, p.scale, -ref));
-        };
-        for (int n = lane; n < parts; n += 64) l += factor_of(mine[n]) * mine[n].y;
-        l = over_lanes<64>(l, AddOp());
-        for (int n = lane; n < parts; n += 64) mine[n].x = factor_of(mine[n]) / l;
-    }
-    __syncthreads();
-    const int halves = c.head_dim >> 1, pairs = rows * halves;
-    // threads in teams, a team's share of the parts each, where there are fewer outputs than threads
-    const int teams = max(1, 64 * kWaves / pairs);
-    float2* sums = factor + kPagedFew * kPagedMostSplits - 64 * kWaves;   // (teams > 1: few rows, whose factors end far ahead)
-    for (int i0 = 0; i0 < pairs; i0 += 64 * kWaves) {
-        const int team = teams > 1 ? tid / pairs : 0, i = teams > 1 ? tid - team * pairs : i0 + tid;
-        const int r = min(i, pairs - 1) / halves, e = min(i, pairs - 1) - r * halves;
-        float2 sum = make_float2(0.0f, 0.0f);
-        if (team < teams && i < pairs) {
-            constexpr int kAhead = 8;
-            for (int n0 = team; n0 < parts; n0 += kAhead * teams) {
-                float2 a[kAhead];
-#pragma unroll
-                for (int h = 0; h < kAhead; ++h) a[h] = read_figure(figures_of(min(n0 + h * teams, parts - 1), r) + 1 + e);
-#pragma unroll
-                for (int h = 0; h < kAhead; ++h) {
-                    const int n = n0 + h * teams;
-                    if (n >= parts) continue;
-                    const float2 f = factor[r * parts + n];
-                    if (f.y == 0.0f && f.x == f.x) continue;   // (a part that the row sees nothing of)
-                    sum.x += f.x * a[h].x;
-                    sum.y += f.x * a[h].y;
-                }
-            }
-        }
-        if (teams > 1) {
-            __syncthreads();
-            sums[tid] = sum;
-            __syncthreads();
-            if (tid >= pairs) break;
-            sum = make_float2(0.0f, 0.0f);
-            for (int t = 0; t < teams; ++t) {
-                sum.x += sums[t * pairs + tid].x;
-                sum.y += sums[t * pairs + tid].y;
-            }
-        }
-        if (i < pairs && team == 0) {
-            if constexpr (kBf16) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + out_at(r, 2 * e)) = paged_bf16_pair(sum.x, sum.y);
-            else *reinterpret_cast<float2*>(static_cast<float*>(p.out) + out_at(r, 2 * e)) = sum;
-        }
-    }
-    if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (w.parts == 1) return;                              // uniform
+    float2* factor = reinterpret_cast<float2*>(lds);
+    join_parts(p, w, factor, reinterpret_cast<f32x4*>(factor + kPagedFew * kMostParts), last_one, store);
 }
 
 template <int KS, int PIECES>

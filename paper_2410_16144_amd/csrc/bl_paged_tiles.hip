@@ -3,8 +3,8 @@
 
 namespace bl {
 
-hipError_t launch_paged_tiles_bf16(const PagedArgs& p, int64_t tiles, int tile_rows, hipStream_t s) {
-    return tile_rows == 128 ? launch_paged_tiles_width<1, 4>(p, tiles, s) : launch_paged_tiles_width<1, 2>(p, tiles, s);
+hipError_t launch_paged_tiles_bf16(const PagedArgs& p, int64_t wgs, hipStream_t s) {
+    return p.tile_rows == 128 ? launch_paged_tiles_width<1, 4>(p, wgs, s) : launch_paged_tiles_width<1, 2>(p, wgs, s);
 }
 
 }  // namespace bl

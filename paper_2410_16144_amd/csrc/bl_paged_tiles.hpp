@@ -11,7 +11,7 @@
 // weights as three bf16 numbers each, their sum, in three products.  Maxima, sums and outputs are fp32.  The running maximum is moved only when a
 // score exceeds it by 2^8 or more: weights are then at most 2^8, and what they are relative to cancels in the division.
 //
-// Long walks of few tiles are shared by up to `splits` workgroups, which leave their sums in memory for a launch of their own that adds them.
+// Long walks of few tiles are shared by several workgroups, the last of which adds up their sums (paged_last).
 #pragma once
 #include "bl_paged.hpp"
 
@@ -27,37 +27,16 @@ __device__ __forceinline__ f32x16 paged_mfma32(const s16x8& a, const s16x8 (&b)[
     return c;
 }
 
-// A tile: rows row0 .. row0 + rows - 1 of sequence b's rows of one key head.
-struct PagedTileOf {
-    PagedSequence s;
-    int b, row0, rows, low, reach;   // low: the last position that its first row sees; reach: positions that its last row sees
-    int slot;                        // number of the tile among all
+constexpr int kPagedTileParts = 32;    // workgroups that share a tile's walk
+
+template <int KS, int RW>
+struct PagedTilesLds {
+    static constexpr int DT = (KS + 1) / 2;
+    static constexpr int kRing = 8 * PagedTile<KS>::kBytes;                             // [chunk % 2][keys, values][32 positions]
+    static constexpr int kMeet = RW == 4 ? 0 : RW * 64 * (16 * DT * 4 + 8);             // half of the waves' sums
+    static constexpr int kBytes = kRing > kMeet ? kRing : kMeet;
+    static_assert(kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
 };
-__device__ __forceinline__ int paged_tiles_of(const PagedArgs& p, const PagedSequence& s, int tile_rows) {
-    const int64_t rows = (int64_t)s.rows * p.group;
-    return rows > p.few ? (int)((rows + tile_rows - 1) / tile_rows) : 0;
-}
-__device__ __forceinline__ bool paged_tile(const PagedArgs& p, int lane, int item, int tile_rows, PagedTileOf& t) {
-    int index, before;
-    if (!paged_find(p.c, lane, item, [&](const PagedSequence& s) { return paged_tiles_of(p, s, tile_rows); }, t.b, index, before, t.s)) return false;
-    t.slot = item;
-    const int rows = t.s.rows * p.group;
-    t.row0 = (paged_tiles_of(p, t.s, tile_rows) - 1 - index) * tile_rows;      // the longest walk first
-    t.rows = min(tile_rows, rows - t.row0);
-    t.low = t.s.pos + t.row0 / p.group;
-    t.reach = t.s.pos + (t.row0 + t.rows - 1) / p.group + 1;
-    return true;
-}
-// Workgroups that share the tile's walk.
-__device__ __forceinline__ int paged_tile_parts(const PagedArgs& p, const PagedTileOf& t) { return min(p.splits, (t.reach + kPagedLeast - 1) / kPagedLeast); }
-__device__ __forceinline__ int64_t paged_row_at(const PagedArgs& p, const PagedTileOf& t, int head, int row) {   // of q and out
-    const int token = row / p.group;
-    return (((int64_t)(t.s.first + token) * p.c.n_heads + head) * p.group + row - token * p.group) * p.c.head_dim;
-}
-// A part's figures of a tile's row: (maximum, sum), two words of padding, then the values.
-__device__ __forceinline__ float* paged_figures(const PagedArgs& p, const PagedTileOf& t, int head, int part, int row, int tile_rows) {
-    return p.figures + ((((int64_t)t.slot * p.splits + part) * p.c.n_heads + head) * tile_rows + row) * (4 + p.c.head_dim);
-}
 
 template <int KS, int PIECES, int RW>
 __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const PagedArgs p) {
@@ -68,20 +47,16 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
     constexpr int kTurns = 2 / KW / NB;
     static_assert(RW == 4 || RW == 2, "forms");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ int odd_chunk, bad_page;
+    __shared__ int odd_chunk, bad_page, last_one;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
     const int rw = wave % RW, kw = wave / RW;
     const Paged& c = p.c;
 
-    const int item = (int)blockIdx.x / c.n_heads, head = (int)blockIdx.x - item * c.n_heads;
-    PagedTileOf t;
-    const int which = item / p.splits, part = item - which * p.splits;
-    if (!paged_tile(p, lane, which, kTileRows, t)) return;
-    const int parts = paged_tile_parts(p, t);
-    if (part >= parts) return;
-    const int chunks = (t.reach + kPagedChunk - 1) / kPagedChunk;
-    const int c0 = (int)((int64_t)chunks * part / parts), c1 = (int)((int64_t)chunks * (part + 1) / parts);
+    PagedWork t;
+    if (!paged_work(p, lane, t)) return;
+    const int head = t.head, chunks = (t.reach + kPagedChunk - 1) / kPagedChunk;
+    const int c0 = uniform((int)((int64_t)chunks * t.part / t.parts)), c1 = uniform((int)((int64_t)chunks * (t.part + 1) / t.parts));
     const int32_t* line = c.table + (int64_t)t.b * c.table_width;
     if (tid == 0) odd_chunk = bad_page = 0;
     __syncthreads();
@@ -107,11 +82,11 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
     const int row = rw * 32 + l32;                         // of the tile
     const bool there = row < t.rows;
     const int limit = t.s.pos + (t.row0 + row) / p.group;  // the last position that the row sees
-    const int wave_low = t.s.pos + (t.row0 + rw * 32) / p.group;
-    const int wave_high = rw * 32 < t.rows ? t.s.pos + (t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group : -1;
+    const int wave_low = t.s.pos + uniform((t.row0 + rw * 32) / p.group);
+    const int wave_high = rw * 32 < t.rows ? t.s.pos + uniform((t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group) : -1;
     s16x8 q[KS][PIECES];
     {
-        const int64_t row_at = there ? paged_row_at(p, t, head, t.row0 + row) : 0;
+        const int64_t row_at = there ? paged_row_at(p, t, row) : 0;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) paged_query<PIECES>(p.q, row_at, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
     }
@@ -161,22 +136,41 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
             const uint8_t* keys = ring + block * T::kBytes;
             const uint8_t* values = ring + (2 + block) * T::kBytes;
             f32x16 x[NB];
+            // (four key operands are on their way from LDS at any time)
+            constexpr int kReads = KS * NB, kAhead = kReads < 4 ? kReads : 4;
+            s16x8 k[kAhead];
+            const auto read_k = [&](int i) {               // block i % NB, elements 16 (i / NB) ..
+                return *reinterpret_cast<const s16x8*>(keys + i % NB * T::kBytes + l32 * T::kRow + paged_k_place<KS>(l32, 2 * (i / NB) + g) * 16);
+            };
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int i = 0; i < kAhead; ++i) k[i] = read_k(i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x[n][r] = 0.0f;
+            for (int i = 0; i < kReads; ++i) {
+                const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                x[i % NB] = paged_mfma32<PIECES>(k[i % kAhead], q[i / NB], i < NB ? zero : x[i % NB]);
+                if (i + kAhead < kReads) k[i % kAhead] = read_k(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // the first sixteen keys' value operands travel under the softmax
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const auto read_v = [&](int n, int d) {        // 16 keys, 32 elements
+                const uint8_t* at = values + v_at[d] + n * 16 * T::kRow;
+                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * T::kRow));
+                return s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            };
+            s16x8 v[DT];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-                    x[n] = paged_mfma32<PIECES>(*reinterpret_cast<const s16x8*>(keys + n * T::kBytes + l32 * T::kRow + paged_k_place<KS>(l32, 2 * ks + g) * 16),
-                                                q[ks], x[n]);
+            for (int d = 0; d < DT; ++d) v[d] = read_v(0, d);
+            __builtin_amdgcn_sched_barrier(0);
             if (j1 + 32 * NB - 1 > wave_low) {
+                const int seen = limit - j1 - 4 * g;
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (j1 + 32 * n + 8 * (r >> 2) + 4 * g + (r & 3) > limit) x[n][r] = -INFINITY;
+                        if (32 * n + 8 * (r >> 2) + (r & 3) > seen) x[n][r] = -INFINITY;
             }
             float most = x[0][0];
 #pragma unroll
@@ -196,56 +190,63 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
                 run_m = m_new;
             }
             const float ref = run_m == -INFINITY ? 0.0f : run_m * p.scale;   // (a row that has seen nothing yet)
-            s16x8 w[2 * NB][PIECES];                       // of 16 keys each
-#pragma unroll
-            for (int n = 0; n < 2 * NB; ++n) {
-                uint32_t parts_of[PIECES][4];
+            const auto weights = [&](int n, s16x8 (&w)[PIECES]) {   // of 16 keys
+                uint32_t words[PIECES][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float a = __builtin_amdgcn_exp2f(fmaf(x[n >> 1][8 * (n & 1) + 2 * j], p.scale, -ref));
                     const float b = __builtin_amdgcn_exp2f(fmaf(x[n >> 1][8 * (n & 1) + 2 * j + 1], p.scale, -ref));
-                    run_l += a;
-                    run_l += b;
                     uint32_t two[PIECES];
                     paged_split<PIECES>(a, b, two);
+                    // (a sum of the weights that the values are multiplied by: where one weight outweighs the others, its rounding cancels)
+                    if constexpr (kBf16) {
+                        run_l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two[0]), __builtin_bit_cast(bf16x2, 0x3f803f80u), run_l, false);
+                    } else {
+                        run_l += a;
+                        run_l += b;
+                    }
 #pragma unroll
-                    for (int i = 0; i < PIECES; ++i) parts_of[i][j] = two[i];
+                    for (int i = 0; i < PIECES; ++i) words[i][j] = two[i];
                 }
 #pragma unroll
-                for (int i = 0; i < PIECES; ++i)
-                    w[n][i] = __builtin_bit_cast(s16x8, (u32x4{parts_of[i][0], parts_of[i][1], parts_of[i][2], parts_of[i][3]}));
-            }
-            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const auto read_v = [&](int n, int d) {        // 16 keys, 32 elements
-                const uint8_t* at = values + v_at[d] + n * 16 * T::kRow;
-                const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-                const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * T::kRow));
-                return s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                for (int i = 0; i < PIECES; ++i) w[i] = __builtin_bit_cast(s16x8, (u32x4{words[i][0], words[i][1], words[i][2], words[i][3]}));
             };
+            s16x8 w[2][PIECES];
+            weights(0, w[0]);
             if (!careful) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int n = 0; n < 2 * NB; ++n)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[d] = paged_mfma32<PIECES>(read_v(n, d), w[n], o[d]);
-            } else {
-#pragma unroll
-                for (int n = 0; n < 2 * NB; ++n)
+                for (int n = 0; n < 2 * NB; ++n) {         // sixteen keys' products beside the next sixteen's weights
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
+                        o[d] = paged_mfma32<PIECES>(v[d], w[n & 1], o[d]);
+                        if (n + 1 < 2 * NB) v[d] = read_v(n + 1, d);
+                    }
+                    if (n + 1 < 2 * NB) weights(n + 1, w[(n + 1) & 1]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 2 * NB; ++n) {
+                    if (n) weights(n, w[0]);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        __builtin_amdgcn_sched_barrier(0);
                         s16x8 finite, up, down;
                         paged_put_away(read_v(n, d), finite, up, down);
-                        o[d] = paged_mfma32<PIECES>(finite, w[n], o[d]);
-                        f32x16 n_up, n_down;
+                        const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                        o[d] = paged_mfma32<PIECES>(finite, w[0], o[d]);
+                        f32x16 weighed = paged_mfma32<PIECES>(up, w[0], zero);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) n_up[r] = n_down[r] = 0.0f;
-                        n_up = paged_mfma32<PIECES>(up, w[n], n_up);
-                        n_down = paged_mfma32<PIECES>(down, w[n], n_down);
+                        for (int r = 0; r < 16; ++r)
+                            if (weighed[r] > 0.0f) o[d][r] += INFINITY;
+                        weighed = paged_mfma32<PIECES>(down, w[0], zero);
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            if (n_up[r] > 0.0f) o[d][r] += INFINITY;
-                            if (n_down[r] > 0.0f) o[d][r] -= INFINITY;
-                        }
+                        for (int r = 0; r < 16; ++r)
+                            if (weighed[r] > 0.0f) o[d][r] -= INFINITY;
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                }
             }
         }
     }
@@ -264,21 +265,22 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
             meet_ml[lane] = make_float2(run_m, run_l);
         }
         __syncthreads();
-        if (kw == 1) return;
-        const float2 other = meet_ml[lane];
-        const float m = fmaxf(run_m, other.x), ref = m == -INFINITY ? 0.0f : m * p.scale;
-        const float f0 = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
-        const float f1 = other.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(other.x, p.scale, -ref));
-        run_l = run_l * f0 + other.y * f1;
-        run_m = m;
+        if (kw == 0) {
+            const float2 other = meet_ml[lane];
+            const float m = fmaxf(run_m, other.x), ref = m == -INFINITY ? 0.0f : m * p.scale;
+            const float f0 = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
+            const float f1 = other.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(other.x, p.scale, -ref));
+            run_l = run_l * f0 + other.y * f1;
+            run_m = m;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * f0 + meet[(d * 16 + r) * 64 + lane] * f1;
+                for (int r = 0; r < 16; ++r) o[d][r] = o[d][r] * f0 + meet[(d * 16 + r) * 64 + lane] * f1;
+        }
     }
-    if (!there) return;
-    if (parts == 1) {
-        const int64_t at = paged_row_at(p, t, head, t.row0 + row);
+    if (t.parts == 1) {
+        if (kw || !there) return;
+        const int64_t at = paged_row_at(p, t, row);
         const float inv = 1.0f / run_l;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -287,41 +289,85 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
                 const int e = 32 * d + 8 * r + 4 * g;
                 if (e < c.head_dim) paged_store<kBf16>(p.out, at + e, f32x4{o[d][4 * r] * inv, o[d][4 * r + 1] * inv, o[d][4 * r + 2] * inv, o[d][4 * r + 3] * inv});
             }
-    } else {
-        float* at = paged_figures(p, t, head, part, row, kTileRows);
-        if (g == 0) *reinterpret_cast<float2*>(at) = make_float2(run_m, run_l);
+        return;
+    }
+    // Figures as the lanes have them, a KiB side by side; (maximum, sum) of the rows behind them.
+    const int mine = (rw * DT * 256 + lane) * 16, pair = RW * DT * 4096 + row * 8;
+    const bool used = rw * 32 < t.rows;                    // uniform
+    if (kw == 0 && used) {
+        const __amdgpu_buffer_rsrc_t slot = paged_resource(paged_slot(p, t.slot + t.part));
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int e = 32 * d + 8 * r + 4 * g;
-                if (e < c.head_dim) *reinterpret_cast<f32x4*>(at + 4 + e) = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
-            }
+            for (int r = 0; r < 4; ++r) paged_leave(slot, mine + (d * 4 + r) * 1024, f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]});
+        if (g == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(run_m), __float_as_uint(run_l)}, slot, pair, 0, kDeviceScope);
     }
+    if (!paged_last(p, t, last_one) || !used) return;      // uniform
+    const __amdgpu_buffer_rsrc_t from = paged_resource(paged_slot(p, t.slot));
+    float m = -INFINITY, l = 0.0f;
+    constexpr int kSome = 8;
+    for (int n0 = 0; n0 < t.parts; n0 += kSome) {
+        float2 ml[kSome];
+#pragma unroll
+        for (int n = 0; n < kSome; ++n) ml[n] = paged_read_pair(from, min(n0 + n, t.parts - 1) * p.slot_bytes + pair);
+#pragma unroll
+        for (int n = 0; n < kSome; ++n) m = fmaxf(m, ml[n].x);
+    }
+    const float ref = m == -INFINITY ? 0.0f : m * p.scale;
+    // the waves of the same rows have every KW-th 32 elements each
+    constexpr int kPieces = (DT + KW - 1) / KW;
+    f32x4 sum[kPieces][4];
+#pragma unroll
+    for (int d = 0; d < kPieces; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[d][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < t.parts; ++n) {
+        const float2 ml = paged_read_pair(from, n * p.slot_bytes + pair);
+        f32x4 x[kPieces][4];
+#pragma unroll
+        for (int d = 0; d < kPieces; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[d][r] = paged_read(from, n * p.slot_bytes + mine + (min(d * KW + kw, DT - 1) * 4 + r) * 1024);
+        if (ml.y == 0.0f) continue;                        // (a part that the row sees nothing of has no share, whatever it holds)
+        const float f = paged_factor(ml.x, ml.y, p.scale, ref);
+        l += f * ml.y;
+#pragma unroll
+        for (int d = 0; d < kPieces; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[d][r] += f * x[d][r];
+    }
+    if (!there) return;
+    const int64_t at = paged_row_at(p, t, row);
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < kPieces; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int e = 32 * (d * KW + kw) + 8 * r + 4 * g;
+            if (e < c.head_dim) paged_store<kBf16>(p.out, at + e, sum[d][r] * inv);
+        }
 }
 
 template <int KS, int PIECES, int RW>
-hipError_t launch_paged_tiles_form(const PagedArgs& p, int64_t tiles, hipStream_t s) {
-    constexpr int kRing = 8 * PagedTile<KS>::kBytes, kMeet = RW == 4 ? 0 : RW * 64 * (16 * ((KS + 1) / 2) * 4 + 8);
-    constexpr int kBytes = kRing > kMeet ? kRing : kMeet;
-    static_assert(kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
-    static LdsCeiling ceiling;
-    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&paged_tiles_kernel<KS, PIECES, RW>), kBytes);
+hipError_t launch_paged_tiles_form(const PagedArgs& p, int64_t wgs, hipStream_t s) {
+    using L = PagedTilesLds<KS, RW>;
+    static LdsCeiling ceiling;   // per instantiation, i.e. per kernel
+    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&paged_tiles_kernel<KS, PIECES, RW>), L::kBytes);
     if (e != hipSuccess) return e;
-    paged_tiles_kernel<KS, PIECES, RW><<<dim3((unsigned)(tiles * p.splits * p.c.n_heads)), dim3(256), kBytes, s>>>(p);
+    paged_tiles_kernel<KS, PIECES, RW><<<dim3((unsigned)wgs), dim3(256), L::kBytes, s>>>(p);
     return hipGetLastError();
 }
 
 template <int PIECES, int RW>
-hipError_t launch_paged_tiles_width(const PagedArgs& p, int64_t tiles, hipStream_t s) {
+hipError_t launch_paged_tiles_width(const PagedArgs& p, int64_t wgs, hipStream_t s) {
     switch (paged_width(p.c.head_dim)) {
-        case 32: return launch_paged_tiles_form<2, PIECES, RW>(p, tiles, s);
-        case 48: return launch_paged_tiles_form<3, PIECES, RW>(p, tiles, s);
-        case 64: return launch_paged_tiles_form<4, PIECES, RW>(p, tiles, s);
-        case 96: return launch_paged_tiles_form<6, PIECES, RW>(p, tiles, s);
-        case 128: return launch_paged_tiles_form<8, PIECES, RW>(p, tiles, s);
-        case 192: return launch_paged_tiles_form<12, PIECES, RW>(p, tiles, s);
-        case 256: return launch_paged_tiles_form<16, PIECES, RW>(p, tiles, s);
+        case 32: return launch_paged_tiles_form<2, PIECES, RW>(p, wgs, s);
+        case 48: return launch_paged_tiles_form<3, PIECES, RW>(p, wgs, s);
+        case 64: return launch_paged_tiles_form<4, PIECES, RW>(p, wgs, s);
+        case 96: return launch_paged_tiles_form<6, PIECES, RW>(p, wgs, s);
+        case 128: return launch_paged_tiles_form<8, PIECES, RW>(p, wgs, s);
+        case 192: return launch_paged_tiles_form<12, PIECES, RW>(p, wgs, s);
+        case 256: return launch_paged_tiles_form<16, PIECES, RW>(p, wgs, s);
     }
     return hipErrorInvalidValue;
 }
