@@ -422,8 +422,10 @@ bl_status bl_attn8_prefill(const bl_attn8_prefill_args *args, void *stream);
  */
 #define BL_PAGE_MIN 16
 #define BL_PAGE_MAX 4096
+#define BL_PAGED_MAX_HEADS 1024      /* key heads */
 #define BL_PAGED_MAX_GROUP 64        /* query heads per key head */
 #define BL_PAGED_MAX_SEQUENCES 1024  /* of one call */
+#define BL_PAGED_MAX_POS (1 << 30)
 
 typedef struct bl_paged_cache {
     uint16_t *k_pages_dev;
@@ -444,7 +446,7 @@ int32_t bl_paged_width(int32_t head_dim);
  *   table_dev   [sequences, table_width] int32; only entries up to the call's last position of a sequence are read
  *   pos_dev     [sequences] int32
  *   start_dev   [sequences + 1] int32, rising; may be NULL: then rows == sequences
- *   max_pos     no position of the call is max_pos or beyond; 1 <= max_pos <= table_width * page_size
+ *   max_pos     no position of the call is max_pos or beyond; 1 <= max_pos <= table_width * page_size, max_pos <= BL_PAGED_MAX_POS
  * All four are read on the device, so a captured launch serves other lengths, pages and numbers of rows up to `rows`.  What they say is looked at
  * before it is used: a sequence with a negative position, with positions from max_pos on, or with rows outside 0 .. rows - 1 takes no part, its
  * rows of the outputs stay as they are, like rows that no sequence has.  Two sequences may share pages that nobody writes in the call.

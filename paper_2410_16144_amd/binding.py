@@ -50,8 +50,10 @@ BL_KV8_CHUNK = 64
 BL_ATTN8_MAX_GROUP = 64
 BL_ATTN8_MAX_BATCH = 1024
 BL_PAGE_MIN, BL_PAGE_MAX = 16, 4096
+BL_PAGED_MAX_HEADS = 1024
 BL_PAGED_MAX_GROUP = 64
 BL_PAGED_MAX_SEQUENCES = 1024
+BL_PAGED_MAX_POS = 1 << 30
 BL_NORM_PLAIN, BL_NORM_RESIDUAL, BL_NORM_GATED, BL_NORM_PREMULTIPLIED = 0, 1, 2, 3
 BL_DECODE_NORM_MAX_K = 16384
 

@@ -700,8 +700,8 @@ int32_t bl_paged_width(int32_t head_dim) {
 }
 
 static bool paged_shape_ok(int32_t n_q_heads, int32_t n_heads, int32_t head_dim, int32_t sequences, int32_t rows, int32_t max_pos) {
-    return n_heads >= 1 && n_heads <= 65535 && n_q_heads >= n_heads && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_PAGED_MAX_GROUP &&
-           bl_paged_width(head_dim) > 0 && sequences >= 1 && sequences <= BL_PAGED_MAX_SEQUENCES && rows >= 1 && rows <= (1 << 24) && max_pos >= 1;
+    return n_heads >= 1 && n_heads <= BL_PAGED_MAX_HEADS && n_q_heads >= n_heads && n_q_heads % n_heads == 0 && n_q_heads / n_heads <= BL_PAGED_MAX_GROUP &&
+           bl_paged_width(head_dim) > 0 && sequences >= 1 && sequences <= BL_PAGED_MAX_SEQUENCES && rows >= 1 && rows <= (1 << 24) && max_pos >= 1 && max_pos <= BL_PAGED_MAX_POS;
 }
 
 static bl_status check_paged(const bl_paged_cache* c, const bl_paged_rows* r, int32_t n_q_heads) {

@@ -11,12 +11,14 @@ hipError_t launch_paged_tiles_f32(const PagedArgs& p, int64_t wgs, hipStream_t s
 
 namespace {
 
+constexpr int64_t kCounters = 1 << 14;     // of any call's: figures never lie where another call counts
+
 struct PagedPlan {
     bool    rows_form;
     int     tile_rows, most, least, wanted;
     int64_t wgs, slots, slot_bytes;
     int64_t counter_bytes, figure_bytes;
-    bool launchable() const { return wgs < (1 << 24); }    // 2^32 threads
+    bool launchable() const { return wgs < (1 << 24) && slots <= kCounters; }    // 2^32 threads (and every walk has a counter: 1024 key heads)
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -25,21 +27,21 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // the sum of all tiles' mean walks (paged_cost).  A walk of `reach` positions has at most reach / per + 1 parts, and the sum of all
 // tiles' longest walks is at most twice the cost (the cost itself, where every sequence has one row): at most 2 wanted / n_heads parts more than
 // there are tiles.  A walk with several parts has reach > per, fewer than 2 reach / per parts: at most 4 wanted slots of figures.
-PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int rows, int max_pos, bool single) {
+PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int rows, int max_pos, bool single, bool bf16) {
     PagedPlan r{};
     const int found = compute_unit_count(), cus = found > 0 ? found : 256, width = paged_width(head_dim);
     const int64_t all = (int64_t)rows * group;
     r.rows_form = single && group <= kPagedFew;
     const auto tiles_of = [&](int tile_rows) { return single ? (int64_t)sequences * ceil_div(group, tile_rows) : all / tile_rows + std::min<int64_t>(sequences, rows); };
     const int resident = width > 128 ? 1 : r.rows_form && width <= 64 ? 4 : 2;         // workgroups of a compute unit, by their LDS
-    r.wanted = cus * resident;
+    r.wanted = r.rows_form ? cus * resident : cus;
     if (r.rows_form) {
         r.tile_rows = group;
         r.most = 256;
         r.least = 256;
         r.slot_bytes = (int64_t)group * (4 + head_dim) * 4;
     } else {
-        r.tile_rows = tiles_of(128) * n_heads < r.wanted ? 64 : 128;
+        r.tile_rows = !bf16 || tiles_of(128) * n_heads < cus * resident ? 64 : 128;
         r.most = 32;
         r.least = 512;
         r.slot_bytes = (int64_t)r.tile_rows * (ceil_div(width, 32) * 32 * 4 + 8);
@@ -48,7 +50,7 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
     const int64_t tiles = tiles_of(r.tile_rows), more = (single ? 1 : 2) * (int64_t)r.wanted / n_heads + 1;
     r.wgs = n_heads * std::min(tiles * r.most, tiles + more);
     r.slots = r.most > 1 ? 4 * ((int64_t)r.wanted + n_heads) : 0;
-    r.counter_bytes = 1 << 16;
+    r.counter_bytes = kCounters * 4;
     r.figure_bytes = r.slots * r.slot_bytes;
     return r;
 }
@@ -56,8 +58,12 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
 }  // namespace
 
 int64_t paged_scratch_bytes(int n_heads, int group, int head_dim, int sequences, int rows, int max_pos, bool single) {
-    const PagedPlan plan = paged_plan(n_heads, group, head_dim, sequences, rows, max_pos, single);
-    return plan.counter_bytes + plan.figure_bytes;
+    int64_t most = 0;
+    for (const bool bf16 : {false, true}) {
+        const PagedPlan plan = paged_plan(n_heads, group, head_dim, sequences, rows, max_pos, single, bf16);
+        most = std::max(most, plan.counter_bytes + plan.figure_bytes);
+    }
+    return most;
 }
 
 hipError_t launch_attn_paged(const ::bl_attn_paged_args& a, hipStream_t s) {
@@ -66,13 +72,13 @@ hipError_t launch_attn_paged(const ::bl_attn_paged_args& a, hipStream_t s) {
     p.q = a.q_dev; p.out = a.out_dev;
     p.group = a.n_q_heads / p.c.n_heads;
     p.scale = 1.4426950408889634f / sqrtf((float)p.c.head_dim);
-    const PagedPlan plan = paged_plan(p.c.n_heads, p.group, p.c.head_dim, p.c.sequences, p.c.rows, p.c.max_pos, p.c.start == nullptr);
+    const bool bf16 = a.dt == BL_BF16;
+    const PagedPlan plan = paged_plan(p.c.n_heads, p.group, p.c.head_dim, p.c.sequences, p.c.rows, p.c.max_pos, p.c.start == nullptr, bf16);
     if (!plan.launchable()) return hipErrorInvalidConfiguration;
     p.tile_rows = plan.tile_rows; p.most = plan.most; p.least = plan.least; p.rounded = plan.rows_form; p.slots = (int32_t)plan.slots; p.slot_bytes = (int32_t)plan.slot_bytes;
     p.target = (float)p.c.n_heads / (float)plan.wanted;
     p.counters = static_cast<uint32_t*>(a.scratch_dev);
     p.figures = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch_dev) + plan.counter_bytes);
-    const bool bf16 = a.dt == BL_BF16;
     return plan.rows_form ? launch_paged_rows(p, bf16, plan.wgs, s) : (bf16 ? launch_paged_tiles_bf16 : launch_paged_tiles_f32)(p, plan.wgs, s);
 }
 

@@ -94,15 +94,22 @@ struct PagedBase {
     int64_t at[2];
     bool    bad;     // the table names a page that is not there
 };
-// line: the sequence's line of the table; last: its last position.  Sixteens behind it are not looked up.
+// The table's words for 32 positions from j0 on: looked up a request ahead, since a scalar load that is waited for stands in everybody's way.  line: the
+// sequence's line of the table; last: its last position.  Sixteens behind it are not looked up.
+struct PagedEntries {
+    int page[2];
+};
+__device__ __forceinline__ PagedEntries paged_entries(const Paged& p, const int32_t* line, int j0, int last) {
+    return {scalar_word(line, min(j0, last) >> p.page_shift), scalar_word(line, min(j0 + 16, last) >> p.page_shift)};
+}
 template <int KS>
-__device__ __forceinline__ PagedBase paged_base(const Paged& p, const int32_t* line, int head, int j0, int last) {
+__device__ __forceinline__ PagedBase paged_base(const Paged& p, const PagedEntries& e, int head, int j0, int last) {
     PagedBase r;
     r.bad = false;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int j = min(j0 + 16 * h, last);
-        int page = __builtin_amdgcn_readfirstlane(scalar_word(line, j >> p.page_shift));
+        int page = __builtin_amdgcn_readfirstlane(e.page[h]);
         if ((uint32_t)page >= (uint32_t)p.pages) {
             page = 0;
             r.bad = true;
@@ -130,46 +137,41 @@ __device__ __forceinline__ void paged_piece(int s, int lane, int& row, int& byte
     byte = (VALUE ? paged_v_place<KS>(row, place) : paged_k_place<KS>(row, place)) * 16;
 }
 
+// Positions behind the sequence's last one come as they lie in their page, or as another sixteen: whatever they are, nobody sees them.
 template <int KS>
 struct PagedRequest {
-    uint32_t off[PagedTile<KS>::kKept];   // in a sixteen (or, odd KS, in 32 rows)
+    uint32_t off[PagedTile<KS>::kKept];   // in a sixteen
     template <bool VALUE>
     __device__ __forceinline__ void prepare(int lane) {
 #pragma unroll
         for (int s = 0; s < PagedTile<KS>::kKept; ++s) {
             int row, byte;
             paged_piece<KS, VALUE>(s, lane, row, byte);
-            off[s] = (uint32_t)(row * PagedTile<KS>::kRow + byte);
+            off[s] = (uint32_t)((row & 15) * PagedTile<KS>::kRow + byte);
         }
     }
-    // KS pieces on their way to LDS address dst.  limit: the last of the 32 rows that the sequence has (rows behind it repeat that one).
-    template <bool VALUE>
-    __device__ __forceinline__ void send(const uint16_t* pool, const PagedBase& base, uint32_t dst, int limit, int lane) const {
-        const uint8_t* from[2] = {reinterpret_cast<const uint8_t*>(pool) + base.at[0], reinterpret_cast<const uint8_t*>(pool) + base.at[1]};
-        constexpr int kRow = PagedTile<KS>::kRow;
-        dst = __builtin_amdgcn_readfirstlane(dst);         // (uniform already, as everything here that is no lane's)
+    // One of KS pieces of 1 KiB on its way to LDS address dst (uniform, as everything here that is no lane's), by the lanes of `who`: all or, where there
+    // is nothing to bring, none, without a branch between the products.  All lanes are active here.
+    __device__ __forceinline__ void piece(int s, const uint16_t* pool, const PagedBase& base, uint32_t dst, uint64_t who = ~0ull) const {
+        const uint8_t* at = reinterpret_cast<const uint8_t*>(pool);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(dst + 1024 * s);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-        if (PagedTile<KS>::kWhole && limit >= 31) {   // uniform
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const uint8_t* src = uniform_ptr(from[2 * s / KS]);
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                             ::"s"(dst + 1024 * s), "v"(off[s % PagedTile<KS>::kKept]), "s"(src) : "memory", "m0");
-            }
-        } else {
-            int here = lane;
-            asm volatile("" : "+v"(here));                 // (a walk's last request: its addresses take no registers for the length of the walk)
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                int row, byte;
-                paged_piece<KS, VALUE>(s, here, row, byte);
-                row = min(row, limit);
-                const uint8_t* src = (row < 16 ? from[0] : from[1]) + (row & 15) * kRow + byte;
-                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst + 1024 * s), "v"(src) : "memory", "m0");
-            }
+        if constexpr (PagedTile<KS>::kWhole) {
+            asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                         ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(uniform_ptr(at + base.at[2 * s / KS])), "s"(who) : "memory", "m0", "exec");
+        } else {   // a piece lies in both sixteens
+            const int row = (s * 64 + (int)(threadIdx.x & 63)) / (2 * KS);
+            const int64_t first = base.at[0], second = base.at[1];
+            const uint8_t* src = at + (row < 16 ? first : second) + off[s];
+            asm volatile("s_mov_b64 exec, %2\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1"
+                         ::"s"(to), "v"(src), "s"(who) : "memory", "m0", "exec");
         }
 #pragma clang diagnostic pop
+    }
+    __device__ __forceinline__ void send(const uint16_t* pool, const PagedBase& base, uint32_t dst, uint64_t who = ~0ull) const {   // all of them
+#pragma unroll
+        for (int s = 0; s < KS; ++s) piece(s, pool, base, dst, who);
     }
 };
 
@@ -304,7 +306,7 @@ __device__ __forceinline__ int paged_tiles(const PagedArgs& p, int rows) { retur
 // (Rounded up, or, where joining parts is dear, down.)
 __device__ __forceinline__ int paged_parts(const PagedArgs& p, const PagedSequence& s, int per) {
     const int reach = s.pos + s.rows;
-    return min(max((reach + p.rounded * (per - 1)) / per, 1), p.most);
+    return min(p.rounded ? (reach - 1) / per + 1 : max(reach / per, 1), p.most);
 }
 
 // Uniform numbers, in scalar registers: divisions leave them in vector ones.
@@ -357,7 +359,8 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
         const int which = __builtin_ctzll(later);
         index = item - __builtin_amdgcn_readlane(upto - sum, which);
         first_slot = __builtin_amdgcn_readlane(shared_upto - shared, which);
-        for (w.b = which * each;; ++w.b) {                 // (the item is one of this lane's sequences')
+        for (w.b = which * each;; ++w.b) {                 // (the item is one of this lane's sequences'; where rows overlap, sums may mean nothing)
+            if (w.b >= c.sequences || index < 0) return false;
             w.s = paged_sequence_uniform(c, w.b);
             int n, shared_n;
             count(w.s, n, shared_n);
@@ -377,6 +380,8 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
     w.low = w.s.pos + uniform(w.row0 / p.group);
     w.reach = w.s.pos + uniform((w.row0 + w.rows - 1) / p.group) + 1;
     w.slot = (first_slot + turn * w.parts) * c.n_heads + w.head * w.parts;
+    w.parts = min(w.parts, (w.reach + p.least - 1) / p.least);   // (a sequence's first tiles walk less than its last one)
+    if (w.part >= w.parts) return false;
     if (w.parts > 1 && w.slot + w.parts > p.slots) {       // (never, see paged_plan)
         if (w.part) return false;
         w.parts = 1;
@@ -421,7 +426,7 @@ __device__ __forceinline__ bool paged_last(const PagedArgs& p, const PagedWork& 
         if (last_one) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
-    return last_one != 0;
+    return uniform(last_one) != 0;
 }
 
 // The sum of a part's, or a wave's, figures relative to `ref`: nothing of what a row has seen nothing of; NaN weights stay NaN.

@@ -142,10 +142,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     req_v.template prepare<true>(lane);
     int chunk = c0 + wave;
     PagedBase base{{0, 0}, false};
+    PagedEntries entries{{0, 0}};
     if (chunk < c1) {
-        base = paged_base<KS>(c, line, head, 32 * chunk, reach - 1);
-        req_k.template send<false>(c.k, base, at_k, reach - 1 - 32 * chunk, lane);
-        req_v.template send<true>(c.v, base, at_v, reach - 1 - 32 * chunk, lane);
+        base = paged_base<KS>(c, paged_entries(c, line, 32 * chunk, reach - 1), head, 32 * chunk, reach - 1);
+        entries = paged_entries(c, line, 32 * (chunk + kWaves), reach - 1);
+        req_k.send(c.k, base, at_k);
+        req_v.send(c.v, base, at_v);
     }
 
     // ---- the rows: operand column i16
@@ -181,8 +183,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // every key has left the tile
         if (next < c1) {
-            base = paged_base<KS>(c, line, head, 32 * next, reach - 1);
-            req_k.template send<false>(c.k, base, at_k, reach - 1 - 32 * next, lane);
+            base = paged_base<KS>(c, entries, head, 32 * next, reach - 1);
+            entries = paged_entries(c, line, 32 * (next + kWaves), reach - 1);
+            req_k.send(c.k, base, at_k);
             wait_vm<KS>();                                 // values are here
         } else {
             wait_vm<0>();
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (next < c1) req_v.template send<true>(c.v, base, at_v, reach - 1 - 32 * next, lane);
+        if (next < c1) req_v.send(c.v, base, at_v);
     }
 
     // ---- the waves meet

@@ -13,6 +13,8 @@
 //
 // Long walks of few tiles are shared by several workgroups, the last of which adds up their sums (paged_last).
 #pragma once
+#include <type_traits>
+
 #include "bl_paged.hpp"
 
 namespace bl {
@@ -32,22 +34,26 @@ constexpr int kPagedTileParts = 32;    // workgroups that share a tile's walk
 template <int KS, int RW>
 struct PagedTilesLds {
     static constexpr int DT = (KS + 1) / 2;
-    static constexpr int kRing = 8 * PagedTile<KS>::kBytes;                             // [chunk % 2][keys, values][32 positions]
+    // Chunks in LDS: two where two workgroups share a compute unit, four (as far as they fit) where one has it to itself.
+    static constexpr int kDepth = RW == 4 || KS > 8 ? 2 : 4;
+    static constexpr int kRing = kDepth * 4 * PagedTile<KS>::kBytes;                    // [chunk % depth][keys, values][32 positions]
     static constexpr int kMeet = RW == 4 ? 0 : RW * 64 * (16 * DT * 4 + 8);             // half of the waves' sums
     static constexpr int kBytes = kRing > kMeet ? kRing : kMeet;
     static_assert(kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
 };
 
 template <int KS, int PIECES, int RW>
-__global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const PagedArgs p) {
+__global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) void paged_tiles_kernel(const PagedArgs p) {
     using T = PagedTile<KS>;
     constexpr bool kBf16 = PIECES == 1;
-    constexpr int KW = 4 / RW, kTileRows = 32 * RW, DT = (KS + 1) / 2;
-    constexpr int NB = kBf16 && KW == 1 ? 2 : 1;           // blocks of 32 keys that share a softmax step
-    constexpr int kTurns = 2 / KW / NB;
+    constexpr int kDepth = PagedTilesLds<KS, RW>::kDepth;
+    constexpr int KW = 4 / RW, DT = (KS + 1) / 2;
+    constexpr int NB = 2 / KW;                             // a wave's blocks of 32 keys in a chunk
     static_assert(RW == 4 || RW == 2, "forms");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int odd_chunk, bad_page, last_one;
+    __shared__ uint32_t odd_values[2][kPagedChunk * DT];   // [up, down][key][32 elements]: where infinities and NaN were
+    __shared__ uint32_t odd_seen[2 * DT][256];             // the same of the keys that a lane's row sees
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, g = lane >> 5;
     const int rw = wave % RW, kw = wave / RW;
@@ -67,16 +73,35 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
     PagedRequest<KS> req;
     if (value) req.template prepare<true>(lane);
     else req.template prepare<false>(lane);
-    const auto request = [&](int chunk) {
-        const int j0 = chunk * kPagedChunk + 32 * (wave & 1);
-        const PagedBase base = paged_base<KS>(c, line, head, j0, t.reach - 1);
-        if (base.bad && lane == 0) bad_page = 1;
-        const int limit = max(t.reach - 1 - j0, 0);        // (no row at all: any)
-        const uint32_t dst = to + (uint32_t)(chunk & 1) * (4 * T::kBytes);
-        if (value) req.template send<true>(c.v, base, dst, limit, lane);
-        else req.template send<false>(c.k, base, dst, limit, lane);
+    const auto first_of = [&](int chunk) { return min(chunk, c1) * kPagedChunk + 32 * (wave & 1); };
+    PagedEntries entries = paged_entries(c, line, first_of(c0), t.reach - 1);
+    // A request is prepared, and goes out piece by piece between the products: all at once, the wave stands still until the last piece has found a
+    // place (700 cycles a chunk, as many as the products of the scores).
+    PagedBase next{{0, 0}, false};
+    uint32_t next_at = 0;
+    uint64_t pieces = 0;                                   // the lanes that bring them: all or none
+    const auto prepare = [&](int chunk) __attribute__((always_inline)) {   // (one after the other)
+        pieces = 0;
+        if (chunk >= c1) return;
+        const int j0 = first_of(chunk);
+        next = paged_base<KS>(c, entries, head, j0, t.reach - 1);
+        entries = paged_entries(c, line, first_of(chunk + 1), t.reach - 1);
+        if (next.bad && lane == 0) bad_page = 1;
+        next_at = to + (uint32_t)(chunk & (kDepth - 1)) * (4 * T::kBytes);
+        pieces = ~0ull;
     };
-    request(c0);
+    const uint16_t* pool = value ? c.v : c.k;
+    constexpr int kSlots = KS * NB + 2 * NB * DT;          // of a chunk, a read and PIECES products each
+    const auto send_at = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            if (s * kSlots / KS == slot) req.piece(s, pool, next, next_at, pieces);
+    };
+#pragma unroll
+    for (int i = 0; i < kDepth - 1; ++i) {
+        prepare(c0 + i);
+        req.send(pool, next, next_at, pieces);
+    }
 
     // the wave's rows: operand column l32
     const int row = rw * 32 + l32;                         // of the tile
@@ -110,36 +135,60 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
         v_at[d] = key * T::kRow + paged_v_place<KS>(key, piece) * 16 + (lane & 1) * 8;
     }
 
-    for (int chunk = c0; chunk < c1; ++chunk) {
+    // Chunks that every row of the tile sees whole, then those that end among the rows' own positions.  (The first kind's code lies side by side: a jump
+    // costs as much as two products.)
+    const auto walk = [&](int chunk, auto which) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(which)::value;
         const int j0 = chunk * kPagedChunk;
-        const uint8_t* ring = lds + (chunk & 1) * (4 * T::kBytes);
-        wait_vm<0>();
-        __syncthreads();                                   // the chunk is here, and nobody reads the other one any more
-        if (chunk + 1 < c1) request(chunk + 1);
-        // Weights of zero may stand before values that a row does not see; infinities and NaN among those take the careful way.
+        const uint8_t* ring = lds + (chunk & (kDepth - 1)) * (4 * T::kBytes);
+        if (kDepth == 2 || chunk + 1 == c1) wait_vm<0>();
+        else if (chunk + 2 == c1) wait_vm<KS>();           // (so many requests behind the chunk's own)
+        else wait_vm<2 * KS>();
+        __syncthreads();                                   // the chunk is here, and nobody reads the one before it any more
+        prepare(chunk + kDepth - 1);
+        // Weights of zero may stand before values that a row does not see; infinities and NaN among those are put away and noted.
         bool careful = false;
-        if (j0 + kPagedChunk - 1 > t.low) {                // uniform
+        if constexpr (kMasked) {
+            uint8_t* values = lds + (ring - lds) + 2 * T::kBytes;
             uint32_t most = 0;
             for (int i = tid * 16; i < 2 * T::kBytes; i += 256 * 16) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(ring + 2 * T::kBytes + i);
+                const u32x4 x = *reinterpret_cast<const u32x4*>(values + i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = paged_exponents(most, x[j]);
             }
             if (paged_not_finite(most)) odd_chunk = chunk + 1;
+            for (int i = tid; i < kPagedChunk * DT; i += 256) odd_values[0][i] = odd_values[1][i] = 0;
             __syncthreads();
-            careful = odd_chunk == chunk + 1;
+            careful = uniform(odd_chunk) == chunk + 1;
+            if (careful) {
+#pragma unroll 1
+                for (int i = tid * 16; i < 2 * T::kBytes; i += 256 * 16) {
+                    const int key = i / T::kRow, piece = paged_v_place<KS>(key, i % T::kRow / 16);
+                    uint32_t up = 0, down = 0;
+#pragma unroll 1
+                    for (int j = 0; j < 8; ++j) {
+                        uint16_t* at = reinterpret_cast<uint16_t*>(values + i) + j;
+                        const uint32_t x = *at, size = x & 0x7fffu;
+                        if (size < 0x7f80u) continue;
+                        if (size > 0x7f80u || x < 0x8000u) up |= 1u << j;     // (NaN is both)
+                        if (size > 0x7f80u || x >= 0x8000u) down |= 1u << j;
+                        *at = 0;
+                    }
+                    if (up) atomicOr(&odd_values[0][key * DT + piece / 4], up << 8 * (piece % 4));
+                    if (down) atomicOr(&odd_values[1][key * DT + piece / 4], down << 8 * (piece % 4));
+                }
+                __syncthreads();
+            }
         }
-#pragma unroll
-        for (int turn = 0; turn < kTurns; ++turn) {
-            const int block = KW == 2 ? kw : turn * NB, j1 = j0 + 32 * block;
-            if (j1 > wave_high) continue;                  // uniform
+        const int block = KW == 2 ? kw : 0, j1 = j0 + 32 * block;
+        if (kMasked ? j1 <= wave_high : wave_high >= 0) {  // uniform
             const uint8_t* keys = ring + block * T::kBytes;
             const uint8_t* values = ring + (2 + block) * T::kBytes;
             f32x16 x[NB];
             // (four key operands are on their way from LDS at any time)
             constexpr int kReads = KS * NB, kAhead = kReads < 4 ? kReads : 4;
             s16x8 k[kAhead];
-            const auto read_k = [&](int i) {               // block i % NB, elements 16 (i / NB) ..
+            const auto read_k = [&](int i) __attribute__((always_inline)) {               // block i % NB, elements 16 (i / NB) ..
                 return *reinterpret_cast<const s16x8*>(keys + i % NB * T::kBytes + l32 * T::kRow + paged_k_place<KS>(l32, 2 * (i / NB) + g) * 16);
             };
 #pragma unroll
@@ -150,11 +199,12 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
                 const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
                 x[i % NB] = paged_mfma32<PIECES>(k[i % kAhead], q[i / NB], i < NB ? zero : x[i % NB]);
                 if (i + kAhead < kReads) k[i % kAhead] = read_k(i + kAhead);
+                send_at(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             // the first sixteen keys' value operands travel under the softmax
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const auto read_v = [&](int n, int d) {        // 16 keys, 32 elements
+            const auto read_v = [&](int n, int d) __attribute__((always_inline)) {        // 16 keys, 32 elements
                 const uint8_t* at = values + v_at[d] + n * 16 * T::kRow;
                 const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
                 const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * T::kRow));
@@ -164,13 +214,33 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
 #pragma unroll
             for (int d = 0; d < DT; ++d) v[d] = read_v(0, d);
             __builtin_amdgcn_sched_barrier(0);
-            if (j1 + 32 * NB - 1 > wave_low) {
+            if (kMasked && j1 + 32 * NB - 1 > wave_low) {
                 const int seen = limit - j1 - 4 * g;
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (32 * n + 8 * (r >> 2) + (r & 3) > seen) x[n][r] = -INFINITY;
+            }
+            if (kMasked && careful) {                      // of the keys that the row sees
+                asm volatile("");                          // (a branch: else every chunk pays for it)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    uint32_t up = 0, down = 0;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) {
+                            const int key = 32 * (block + n) + 8 * (r >> 2) + 4 * g + (r & 3);
+                            if (x[n][r] != -INFINITY) {
+                                up |= odd_values[0][key * DT + d];
+                                down |= odd_values[1][key * DT + d];
+                            }
+                            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                        }
+                    odd_seen[2 * d][tid] = up;
+                    odd_seen[2 * d + 1][tid] = down;
+                }
             }
             float most = x[0][0];
 #pragma unroll
@@ -179,7 +249,7 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, x[n][r]);
             most = over_blocks<32>(most, MaxOp());
             const bool moves = (most - run_m) * p.scale > 8.0f;   // (of each row for itself: no row's bits depend on another's)
-            if (__any(moves)) {
+            if (__builtin_expect(__any(moves), 0)) {
                 const float m_new = moves ? most : run_m;
                 const float keep = !moves ? 1.0f : run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((run_m - m_new) * p.scale);
 #pragma unroll
@@ -190,7 +260,7 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
                 run_m = m_new;
             }
             const float ref = run_m == -INFINITY ? 0.0f : run_m * p.scale;   // (a row that has seen nothing yet)
-            const auto weights = [&](int n, s16x8 (&w)[PIECES]) {   // of 16 keys
+            const auto weights = [&](int n, s16x8 (&w)[PIECES]) __attribute__((always_inline)) {   // of 16 keys
                 uint32_t words[PIECES][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -213,47 +283,43 @@ __global__ __launch_bounds__(256, KS <= 8 ? 2 : 1) void paged_tiles_kernel(const
             };
             s16x8 w[2][PIECES];
             weights(0, w[0]);
-            if (!careful) {
-                __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int n = 0; n < 2 * NB; ++n) {         // sixteen keys' products beside the next sixteen's weights
+            for (int n = 0; n < 2 * NB; ++n) {             // sixteen keys' products beside the next sixteen's weights
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        o[d] = paged_mfma32<PIECES>(v[d], w[n & 1], o[d]);
-                        if (n + 1 < 2 * NB) v[d] = read_v(n + 1, d);
-                    }
-                    if (n + 1 < 2 * NB) weights(n + 1, w[(n + 1) & 1]);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int d = 0; d < DT; ++d) {
+                    o[d] = paged_mfma32<PIECES>(v[d], w[n & 1], o[d]);
+                    if (n + 1 < 2 * NB) v[d] = read_v(n + 1, d);
+                    send_at(kReads + n * DT + d);
                 }
-            } else {
+                if (n + 1 < 2 * NB) weights(n + 1, w[(n + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (kMasked && careful) {                      // (lane and lane + 32 have the row's keys between them)
+                asm volatile("");
 #pragma unroll
-                for (int n = 0; n < 2 * NB; ++n) {
-                    if (n) weights(n, w[0]);
+                for (int d = 0; d < DT; ++d) {
+                    const uint32_t up = (odd_seen[2 * d][tid] | odd_seen[2 * d][tid ^ 32]) >> 4 * g, down = (odd_seen[2 * d + 1][tid] | odd_seen[2 * d + 1][tid ^ 32]) >> 4 * g;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        s16x8 finite, up, down;
-                        paged_put_away(read_v(n, d), finite, up, down);
-                        const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                        o[d] = paged_mfma32<PIECES>(finite, w[0], o[d]);
-                        f32x16 weighed = paged_mfma32<PIECES>(up, w[0], zero);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (weighed[r] > 0.0f) o[d][r] += INFINITY;
-                        weighed = paged_mfma32<PIECES>(down, w[0], zero);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (weighed[r] > 0.0f) o[d][r] -= INFINITY;
-                        __builtin_amdgcn_sched_barrier(0);
+                    for (int r = 0; r < 16; ++r) {
+                        const uint32_t bit = 1u << (8 * (r >> 2) + (r & 3));
+                        if (up & bit) o[d][r] += INFINITY;
+                        if (down & bit) o[d][r] -= INFINITY;
+                        if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
+        } else {
+            req.send(pool, next, next_at, pieces);
         }
-    }
+    };
+    const int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);
+    for (int chunk = c0; chunk < plain; ++chunk) walk(chunk, std::false_type{});
+    for (int chunk = plain; chunk < c1; ++chunk) walk(chunk, std::true_type{});
 
     run_l = over_blocks<32>(run_l, AddOp());
     __syncthreads();
-    if (bad_page) run_l = NAN;                             // (rows of a sequence whose table names a page that is not there)
+    if (uniform(bad_page)) run_l = NAN;                             // (rows of a sequence whose table names a page that is not there)
     if constexpr (KW == 2) {                               // the chunk's shares meet
         float* meet = reinterpret_cast<float*>(lds) + rw * (64 * 16 * DT);
         float2* meet_ml = reinterpret_cast<float2*>(reinterpret_cast<float*>(lds) + RW * 64 * 16 * DT) + rw * 64;

@@ -4,7 +4,7 @@
 namespace bl {
 
 hipError_t launch_paged_tiles_f32(const PagedArgs& p, int64_t wgs, hipStream_t s) {
-    return p.tile_rows == 128 ? launch_paged_tiles_width<3, 4>(p, wgs, s) : launch_paged_tiles_width<3, 2>(p, wgs, s);
+    return launch_paged_tiles_width<3, 2>(p, wgs, s);
 }
 
 }  // namespace bl

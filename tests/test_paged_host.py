@@ -36,13 +36,13 @@ def test_structures_as_the_header_has_them(tmp_path):
                     for n, c in names.items())
     src = tmp_path / "sizes.c"
     src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "bitlinear_decoder.h"\nint main(void) {' + lines +
-                   'printf("%d %d %d %d\\n", BL_PAGE_MIN, BL_PAGE_MAX, BL_PAGED_MAX_GROUP, BL_PAGED_MAX_SEQUENCES); return 0;}')
+                   'printf("%d %d %d %d %d %d\\n", BL_PAGE_MIN, BL_PAGE_MAX, BL_PAGED_MAX_HEADS, BL_PAGED_MAX_GROUP, BL_PAGED_MAX_SEQUENCES, BL_PAGED_MAX_POS); return 0;}')
     exe = str(tmp_path / "sizes")
     subprocess.check_call(["gcc", "-std=c11", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", exe])
     said = subprocess.check_output([exe], text=True).splitlines()
     for line, (n, c) in zip(said, names.items()):
         assert [int(x) for x in line.split()] == [ctypes.sizeof(c)] + [getattr(c, f[0]).offset for f in c._fields_], n
-    assert [int(x) for x in said[-1].split()] == [B.BL_PAGE_MIN, B.BL_PAGE_MAX, B.BL_PAGED_MAX_GROUP, B.BL_PAGED_MAX_SEQUENCES]
+    assert [int(x) for x in said[-1].split()] == [B.BL_PAGE_MIN, B.BL_PAGE_MAX, B.BL_PAGED_MAX_HEADS, B.BL_PAGED_MAX_GROUP, B.BL_PAGED_MAX_SEQUENCES, B.BL_PAGED_MAX_POS]
 
 
 def test_widths():
@@ -54,7 +54,7 @@ def test_widths():
 
 def _refusals_of_the_rows(call):
     assert call(_cache(k_pages_dev=None)) == call(_cache(v_pages_dev=None)) == call(rows=_rows(table_dev=None)) == call(rows=_rows(pos_dev=None)) == B.BL_ERR_NULL
-    for kw in (dict(n_heads=0), dict(n_heads=3), dict(n_heads=65536), dict(head_dim=62), dict(head_dim=0), dict(head_dim=260), dict(page_size=8), dict(page_size=48),
+    for kw in (dict(n_heads=0), dict(n_heads=3), dict(n_heads=1025), dict(head_dim=62), dict(head_dim=0), dict(head_dim=260), dict(page_size=8), dict(page_size=48),
                dict(page_size=8192), dict(page_size=0), dict(page_size=-32), dict(pages=0), dict(pages=-1)):
         assert call(_cache(**kw)) == B.BL_ERR_SHAPE, kw
     for kw in (dict(sequences=0), dict(sequences=1025), dict(rows=0), dict(rows=-1), dict(rows=(1 << 24) + 1), dict(table_width=0), dict(max_pos=0), dict(max_pos=161),
@@ -114,13 +114,14 @@ def test_scratch():
     for bad in ((6, 4, 64, 3, 7, 160, 0), (8, 0, 64, 3, 7, 160, 0), (8, 4, 62, 3, 7, 160, 0), (8, 4, 64, 0, 7, 160, 0), (8, 4, 64, 1025, 7, 160, 0), (8, 4, 64, 3, 0, 160, 0),
                 (8, 4, 64, 3, 7, 0, 0), (8, 4, 64, 3, 7, 160, 1), (4 * 65, 4, 64, 3, 7, 160, 0)):
         assert f(*bad) == 0, bad
-    # the counters of any call with as many key heads, whatever else
+    # the counters of any call, whatever else
     for args in ((8, 4, 64, 3, 7, 160, 0), (8, 4, 64, 3, 3, 160, 1), (8, 4, 64, 1024, 1024, 1 << 20, 1), (8, 4, 256, 1, 4096, 1 << 20, 0)):
-        assert f(*args) >= 1024 * 4 * 4 and f(*args) % 16 == 0
+        assert f(*args) >= 1 << 16 and f(*args) % 16 == 0
     # no figures where no walk can be shared
-    assert f(8, 4, 64, 3, 3, 160, 1) == 1024 * 4 * 4
+    assert f(8, 4, 64, 3, 3, 160, 1) == 1 << 16
     # and memory in bounds at the largest
-    assert f(64, 1, 256, 1024, 1024, 2147483647, 1) < 1 << 33 and f(64, 1, 256, 1, 1 << 20, 2147483647, 0) < 1 << 33
+    assert f(64, 1, 256, 1024, 1024, 1 << 30, 1) < 1 << 33 and f(64, 1, 256, 1, 1 << 20, 1 << 30, 0) < 1 << 33
+    assert f(8, 4, 64, 3, 7, (1 << 30) + 1, 0) == 0
 
 
 def test_what_the_python_side_asks_for():
