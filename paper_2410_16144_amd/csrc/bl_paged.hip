@@ -33,15 +33,17 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
     const int64_t all = (int64_t)rows * group;
     r.rows_form = single && group <= kPagedFew;
     const auto tiles_of = [&](int tile_rows) { return single ? (int64_t)sequences * ceil_div(group, tile_rows) : all / tile_rows + std::min<int64_t>(sequences, rows); };
-    const int resident = width > 128 ? 1 : r.rows_form && width <= 64 ? 4 : 2;         // workgroups of a compute unit, by their LDS
-    r.wanted = r.rows_form ? cus * resident : cus;
+    // Workgroups that a call is meant for.  Rows: as many as keep enough requests under way, no more, since every part of a walk has to be joined (64
+    // heads on 8 at 100 003 positions: one per compute unit 73.8 us, two 79.9; eight sequences of 32 heads, 584 MB: 104.4 and 113.6); rows of
+    // 64 elements and less have half the bytes under way.  Tiles: one per unit, joining is dearer still.
+    r.wanted = r.rows_form && width <= 64 ? 2 * cus : cus;
     if (r.rows_form) {
         r.tile_rows = group;
         r.most = 256;
         r.least = 256;
         r.slot_bytes = (int64_t)group * (4 + head_dim) * 4;
     } else {
-        r.tile_rows = !bf16 || tiles_of(128) * n_heads < cus * resident ? 64 : 128;
+        r.tile_rows = !bf16 || tiles_of(128) * n_heads < (width <= 128 ? 2 : 1) * cus ? 64 : 128;
         r.most = 32;
         r.least = 512;
         r.slot_bytes = (int64_t)r.tile_rows * (ceil_div(width, 32) * 32 * 4 + 8);

@@ -44,6 +44,9 @@ inline Paged paged_of(const ::bl_paged_cache& c, const ::bl_paged_rows& r) {
     return p;
 }
 
+// Uniform numbers, in scalar registers: divisions leave them in vector ones.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Numbers that nothing in a launch writes, by scalar loads (the index is uniform).
 __device__ __forceinline__ int32_t scalar_word(const int32_t* at, int64_t i) {
     return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)at)[i];
@@ -137,8 +140,9 @@ __device__ __forceinline__ void paged_piece(int s, int lane, int& row, int& byte
     byte = (VALUE ? paged_v_place<KS>(row, place) : paged_k_place<KS>(row, place)) * 16;
 }
 
-// Positions behind the sequence's last one come as they lie in their page, or as another sixteen: whatever they are, nobody sees them.
-template <int KS>
+// Positions behind the sequence's last one come as they lie in their page, or as another sixteen: whatever they are, nobody sees them.  STREAM: by
+// streaming (nontemporal) loads, for a cache that a launch reads once.
+template <int KS, bool STREAM>
 struct PagedRequest {
     uint32_t off[PagedTile<KS>::kKept];   // in a sixteen
     template <bool VALUE>
@@ -158,8 +162,13 @@ struct PagedRequest {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
         if constexpr (PagedTile<KS>::kWhole) {
-            asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
-                         ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(uniform_ptr(at + base.at[2 * s / KS])), "s"(who) : "memory", "m0", "exec");
+            const uint8_t* src = uniform_ptr(at + base.at[2 * s / KS]);
+            if constexpr (STREAM)
+                asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b64 exec, -1"
+                             ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(src), "s"(who) : "memory", "m0", "exec");
+            else
+                asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
+                             ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(src), "s"(who) : "memory", "m0", "exec");
         } else {   // a piece lies in both sixteens
             const int row = (s * 64 + (int)(threadIdx.x & 63)) / (2 * KS);
             const int64_t first = base.at[0], second = base.at[1];
@@ -308,9 +317,6 @@ __device__ __forceinline__ int paged_parts(const PagedArgs& p, const PagedSequen
     const int reach = s.pos + s.rows;
     return min(p.rounded ? (reach - 1) / per + 1 : max(reach / per, 1), p.most);
 }
-
-// Uniform numbers, in scalar registers: divisions leave them in vector ones.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // What the call walks of a sequence, in positions (its tiles' mean).
 __device__ __forceinline__ float paged_cost(const PagedArgs& p, const PagedSequence& s) {

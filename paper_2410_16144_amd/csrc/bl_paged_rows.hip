@@ -6,7 +6,9 @@
 //     follows from the positions on the device (paged_find), so that a captured launch serves any lengths.  The grid is an upper bound;
 //     workgroups without a part end at once.
 //   * A workgroup's four waves take its 32-position chunks in turn, each with a tile of keys and one of values of its own in LDS that it fills
-//     and waits for by itself: the next chunk's keys are requested when the scores are formed, its values when the sums are.
+//     and waits for by itself: the next chunk's keys are requested when the scores are formed, its values when the sums are.  Streaming loads, since
+//     nothing is read twice (32 heads of 128, ordinary and streaming, us: 8000 positions 33.1 and 30.4, 32 000 98.0 and 87.8, 5.4 and 6.0 TB/s;
+//     500 to 4000 positions the same).
 //   * Scores are formed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16): a lane has eight of the chunk's weights of ONE row, already laid out as
 //     the operand of O^T += V^T P^T, V^T by the transposing LDS read.  The contraction index runs over the positions in the order of the
 //     result registers: slots 0..3 of lane group g are positions 4 g .. 4 g + 3, slots 4..7 positions 16 + 4 g .. 16 + 4 g + 3.
@@ -14,6 +16,8 @@
 //     queries as they are, and their weights as two: off by at most 2^-16 of a weight, far below the output's rounding.
 //   * Running maxima and sums are fp32; the parts of a walk meet in scratch memory in their order, and the workgroup that draws a row's last
 //     ticket adds them up.  Nobody waits for anybody.
+#include <type_traits>
+
 #include "bl_paged.hpp"
 
 namespace bl {
@@ -50,7 +54,7 @@ __device__ __forceinline__ int figure_at(int head_dim, int row, int word) { retu
 // After every thread has left its figures.  factor: LDS of rows * parts pairs, sums of 256 quads; store(row, e, x): four outputs.
 template <typename Store>
 __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& w, float2* factor, f32x4* sums, int& last_one, const Store& store) {
-    constexpr int kThreads = 256, kAhead = 16;
+    constexpr int kThreads = 256, kAhead = 32;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (!paged_last(p, w, last_one)) return;               // uniform
     const int d = p.c.head_dim, quads = d >> 2, total = w.rows * quads, parts = w.parts;
@@ -58,15 +62,29 @@ __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& 
     const int teams = max(1, kThreads / total);            // that share an output's parts, where there are few outputs
     const int team = teams > 1 ? tid / total : 0;
     f32x4 a[kAhead];
-    const auto read = [&](int i, int n0) {                 // output quad i of parts n0, n0 + teams, ...
+    const auto read = [&](int i, int n0) {                 // output quad i of parts n0 + team, n0 + team + teams, ...
         const int row = i / quads, at = figure_at(d, row, 4 + 4 * (i - row * quads));
 #pragma unroll
         for (int h = 0; h < kAhead; ++h)
-            a[h] = paged_read(from, min(n0 + h * teams, parts - 1) * p.slot_bytes + at);
+            if (h % 4 || n0 + h * teams < parts)           // (by fours)
+                a[h] = paged_read(from, min(n0 + team + h * teams, parts - 1) * p.slot_bytes + at);
+            else
+                break;
     };
     const int i0 = teams > 1 ? tid - team * total : tid;
-    read(min(i0, total - 1), min(team, teams - 1));        // (the first of them travel with the maxima and sums)
-    for (int i = tid; i < w.rows * parts; i += kThreads) { // [row][part]
+    const int pairs = w.rows * parts;                      // [row][part]; most often a few each
+    constexpr int kPairs = 4;
+    float2 ml[kPairs];
+#pragma unroll
+    for (int h = 0; h < kPairs; ++h) {
+        const int i = min(tid + h * kThreads, pairs - 1), row = i / parts;
+        ml[h] = paged_read_pair(from, (i - row * parts) * p.slot_bytes + figure_at(d, row, 0));
+    }
+    read(min(i0, total - 1), 0);                           // (the first of the values travel with the maxima and sums)
+#pragma unroll
+    for (int h = 0; h < kPairs; ++h)
+        if (tid + h * kThreads < pairs) factor[tid + h * kThreads] = ml[h];
+    for (int i = tid + kPairs * kThreads; i < pairs; i += kThreads) {
         const int row = i / parts;
         factor[i] = paged_read_pair(from, (i - row * parts) * p.slot_bytes + figure_at(d, row, 0));
     }
@@ -86,11 +104,12 @@ __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& 
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         const int row = i / quads;
         if (team < teams)
-            for (int n0 = team; n0 < parts; n0 += kAhead * teams) {
-                if (n0 != team || i != i0) read(i, n0);
+            for (int n0 = 0; n0 < parts; n0 += kAhead * teams) {
+                if (n0 || i != i0) read(i, n0);
 #pragma unroll
                 for (int h = 0; h < kAhead; ++h) {
-                    const int n = n0 + h * teams;
+                    if (h % 4 == 0 && n0 + h * teams >= parts) break;
+                    const int n = n0 + team + h * teams;
                     if (n >= parts) continue;
                     const float2 f = factor[row * parts + n];
                     if (f.y == 0.0f && f.x == f.x) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
@@ -137,7 +156,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     // ---- requests
     uint8_t* tile = lds + wave * 2 * T::kBytes;
     const uint32_t at_k = __builtin_amdgcn_readfirstlane(lds_address(tile)), at_v = at_k + T::kBytes;
-    PagedRequest<KS> req_k, req_v;
+    PagedRequest<KS, true> req_k, req_v;
     req_k.template prepare<false>(lane);
     req_v.template prepare<true>(lane);
     int chunk = c0 + wave;
@@ -164,9 +183,11 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
 #pragma unroll
     for (int t = 0; t < KS; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (; chunk < c1; chunk += kWaves) {
+    // Chunks that the sequence has whole, then its last one.  (The first kind's code lies side by side: jumps cost as much as products.)
+    const auto walk = [&](auto which) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(which)::value;
         const int j0 = 32 * chunk, next = chunk + kWaves;
-        const bool bad = base.bad, masked = j0 + 31 > s.pos;     // uniform
+        const bool bad = base.bad;                         // uniform
         wait_vm<KS>();                                     // keys are here; the values may be on their way
         f32x4 x[2];
 #pragma unroll
@@ -190,14 +211,14 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         } else {
             wait_vm<0>();
         }
-        if (masked) {
+        if constexpr (kMasked) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (j0 + 16 * h + 4 * g + r > limit) x[h][r] = -INFINITY;
         }
-        if (bad) x[0] = x[1] = f32x4{NAN, NAN, NAN, NAN};
+        if (__builtin_expect(bad, 0)) x[0] = x[1] = f32x4{NAN, NAN, NAN, NAN};
         float most = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
         most = over_blocks<32>(over_blocks<16>(most, MaxOp()), MaxOp());
         const float m_new = fmaxf(run_m, most);
@@ -231,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
             const s16x4 e = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * T::kRow));
             return s16x8{a[0], a[1], a[2], a[3], e[0], e[1], e[2], e[3]};
         };
-        if (!masked) {
+        if constexpr (!kMasked) {
 #pragma unroll
             for (int t = 0; t < KS; ++t) o[t] = mfma16<kWeight>(read_v(t), weights, o[t] * keep);
         } else {
@@ -262,7 +283,10 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (next < c1) req_v.send(c.v, base, at_v);
-    }
+        chunk = next;
+    };
+    while (chunk < c1 && 32 * chunk + 31 <= s.pos) walk(std::false_type{});
+    while (chunk < c1) walk(std::true_type{});
 
     // ---- the waves meet
     run_l = over_blocks<32>(over_blocks<16>(run_l, AddOp()), AddOp());

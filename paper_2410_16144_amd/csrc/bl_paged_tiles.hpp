@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     // waves 0 and 1 bring a chunk's keys, 2 and 3 its values, 32 positions each
     const bool value = wave >= 2;
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * T::kBytes);
-    PagedRequest<KS> req;
+    PagedRequest<KS, false> req;
     if (value) req.template prepare<true>(lane);
     else req.template prepare<false>(lane);
     const auto first_of = [&](int chunk) { return min(chunk, c1) * kPagedChunk + 32 * (wave & 1); };
@@ -387,20 +387,30 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     for (int d = 0; d < kPieces; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum[d][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int n = 0; n < t.parts; ++n) {
-        const float2 ml = paged_read_pair(from, n * p.slot_bytes + pair);
-        f32x4 x[kPieces][4];
+    // (a read is a trip to memory: as many under way as there are registers for)
+    constexpr int kBatch = 8 / kPieces > 0 ? 8 / kPieces : 1;
+    for (int n0 = 0; n0 < t.parts; n0 += kBatch) {
+        float2 ml[kBatch];
+        f32x4 x[kBatch][kPieces][4];
 #pragma unroll
-        for (int d = 0; d < kPieces; ++d)
+        for (int n = 0; n < kBatch; ++n) {
+            const int from_part = min(n0 + n, t.parts - 1) * p.slot_bytes;
+            ml[n] = paged_read_pair(from, from_part + pair);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[d][r] = paged_read(from, n * p.slot_bytes + mine + (min(d * KW + kw, DT - 1) * 4 + r) * 1024);
-        if (ml.y == 0.0f) continue;                        // (a part that the row sees nothing of has no share, whatever it holds)
-        const float f = paged_factor(ml.x, ml.y, p.scale, ref);
-        l += f * ml.y;
+            for (int d = 0; d < kPieces; ++d)
 #pragma unroll
-        for (int d = 0; d < kPieces; ++d)
+                for (int r = 0; r < 4; ++r) x[n][d][r] = paged_read(from, from_part + mine + (min(d * KW + kw, DT - 1) * 4 + r) * 1024);
+        }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum[d][r] += f * x[d][r];
+        for (int n = 0; n < kBatch; ++n) {
+            if (n0 + n >= t.parts || ml[n].y == 0.0f) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
+            const float f = paged_factor(ml[n].x, ml[n].y, p.scale, ref);
+            l += f * ml[n].y;
+#pragma unroll
+            for (int d = 0; d < kPieces; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[d][r] += f * x[n][d][r];
+        }
     }
     if (!there) return;
     const int64_t at = paged_row_at(p, t, row);
