@@ -140,6 +140,14 @@ __device__ __forceinline__ void paged_piece(int s, int lane, int& row, int& byte
     byte = (VALUE ? paged_v_place<KS>(row, place) : paged_k_place<KS>(row, place)) * 16;
 }
 
+struct PagedSource {
+    const uint8_t* at[2];   // of the two sixteens
+};
+__device__ __forceinline__ PagedSource paged_source(const uint16_t* pool, const PagedBase& base) {
+    const uint8_t* at = reinterpret_cast<const uint8_t*>(pool);
+    return {{at + base.at[0], at + base.at[1]}};
+}
+
 // Positions behind the sequence's last one come as they lie in their page, or as another sixteen: whatever they are, nobody sees them.  STREAM: by
 // streaming (nontemporal) loads, for a cache that a launch reads once.
 template <int KS, bool STREAM>
@@ -154,33 +162,39 @@ struct PagedRequest {
             off[s] = (uint32_t)((row & 15) * PagedTile<KS>::kRow + byte);
         }
     }
-    // One of KS pieces of 1 KiB on its way to LDS address dst (uniform, as everything here that is no lane's), by the lanes of `who`: all or, where there
-    // is nothing to bring, none, without a branch between the products.  All lanes are active here.
-    __device__ __forceinline__ void piece(int s, const uint16_t* pool, const PagedBase& base, uint32_t dst, uint64_t who = ~0ull) const {
-        const uint8_t* at = reinterpret_cast<const uint8_t*>(pool);
+    // One of KS pieces of 1 KiB on its way to LDS address dst (uniform, as everything here that is no lane's), by all lanes, which are active here.  ANY:
+    // by the lanes of `who`: all or, where there is nothing to bring, none, without a branch between the products.
+    template <bool ANY = false>
+    __device__ __forceinline__ void piece(int s, const PagedSource& from, uint32_t dst, uint64_t who = ~0ull) const {
         const uint32_t to = __builtin_amdgcn_readfirstlane(dst + 1024 * s);
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
         if constexpr (PagedTile<KS>::kWhole) {
-            const uint8_t* src = uniform_ptr(at + base.at[2 * s / KS]);
+            const uint8_t* src = uniform_ptr(from.at[2 * s / KS]);
+            const uint32_t o = off[s % PagedTile<KS>::kKept];
+            static_assert(!(ANY && STREAM), "forms in use");
             if constexpr (STREAM)
-                asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt\n\ts_mov_b64 exec, -1"
-                             ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(src), "s"(who) : "memory", "m0", "exec");
-            else
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(o), "s"(src) : "memory", "m0");
+            else if constexpr (ANY)
                 asm volatile("s_mov_b64 exec, %3\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
-                             ::"s"(to), "v"(off[s % PagedTile<KS>::kKept]), "s"(src), "s"(who) : "memory", "m0", "exec");
+                             ::"s"(to), "v"(o), "s"(src), "s"(who) : "memory", "m0", "exec");
+            else
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(o), "s"(src) : "memory", "m0");
         } else {   // a piece lies in both sixteens
             const int row = (s * 64 + (int)(threadIdx.x & 63)) / (2 * KS);
-            const int64_t first = base.at[0], second = base.at[1];
-            const uint8_t* src = at + (row < 16 ? first : second) + off[s];
-            asm volatile("s_mov_b64 exec, %2\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1"
-                         ::"s"(to), "v"(src), "s"(who) : "memory", "m0", "exec");
+            const uint8_t *first = from.at[0], *second = from.at[1], *src = (row < 16 ? first : second) + off[s];
+            if constexpr (ANY)
+                asm volatile("s_mov_b64 exec, %2\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1"
+                             ::"s"(to), "v"(src), "s"(who) : "memory", "m0", "exec");
+            else
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
         }
 #pragma clang diagnostic pop
     }
-    __device__ __forceinline__ void send(const uint16_t* pool, const PagedBase& base, uint32_t dst, uint64_t who = ~0ull) const {   // all of them
+    template <bool ANY = false>
+    __device__ __forceinline__ void send(const PagedSource& from, uint32_t dst, uint64_t who = ~0ull) const {   // all of them
 #pragma unroll
-        for (int s = 0; s < KS; ++s) piece(s, pool, base, dst, who);
+        for (int s = 0; s < KS; ++s) piece<ANY>(s, from, dst, who);
     }
 };
 
@@ -388,7 +402,7 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
     w.slot = (first_slot + turn * w.parts) * c.n_heads + w.head * w.parts;
     w.parts = min(w.parts, (w.reach + p.least - 1) / p.least);   // (a sequence's first tiles walk less than its last one)
     if (w.part >= w.parts) return false;
-    if (w.parts > 1 && w.slot + w.parts > p.slots) {       // (never, see paged_plan)
+    if (w.parts > 1 && (uint32_t)w.slot > (uint32_t)(p.slots - w.parts)) {   // (never, see paged_plan)
         if (w.part) return false;
         w.parts = 1;
     }

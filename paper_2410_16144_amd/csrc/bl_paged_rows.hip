@@ -165,8 +165,8 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     if (chunk < c1) {
         base = paged_base<KS>(c, paged_entries(c, line, 32 * chunk, reach - 1), head, 32 * chunk, reach - 1);
         entries = paged_entries(c, line, 32 * (chunk + kWaves), reach - 1);
-        req_k.send(c.k, base, at_k);
-        req_v.send(c.v, base, at_v);
+        req_k.send(paged_source(c.k, base), at_k);
+        req_v.send(paged_source(c.v, base), at_v);
     }
 
     // ---- the rows: operand column i16
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         if (next < c1) {
             base = paged_base<KS>(c, entries, head, 32 * next, reach - 1);
             entries = paged_entries(c, line, 32 * (next + kWaves), reach - 1);
-            req_k.send(c.k, base, at_k);
+            req_k.send(paged_source(c.k, base), at_k);
             wait_vm<KS>();                                 // values are here
         } else {
             wait_vm<0>();
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (next < c1) req_v.send(c.v, base, at_v);
+        if (next < c1) req_v.send(paged_source(c.v, base), at_v);
         chunk = next;
     };
     while (chunk < c1 && 32 * chunk + 31 <= s.pos) walk(std::false_type{});

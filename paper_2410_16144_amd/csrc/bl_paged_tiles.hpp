@@ -1,9 +1,14 @@
 // bl_attn_paged for many rows: prompts, pieces of prompts, drafted tokens.
 //
 // One workgroup = a tile of 32 RW consecutive rows of one sequence and key head (a row is one query head of one token, token by token, so that
-// the query heads of a key head share what is read of it) against the positions 0 .. its last row's, 64 at a time through LDS, two chunks deep: one
-// barrier per chunk, behind which the next one is requested.  Its four waves are RW sets of 32 rows times 4 / RW shares of a chunk's keys.  Two
-// workgroups fit a compute unit (head sizes up to 128): one is in its products while the other is in its softmax.
+// the query heads of a key head share what is read of it) against the positions 0 .. its last row's, 64 at a time through a ring of chunks in LDS with one
+// barrier a chunk.  Its four waves are RW sets of 32 rows times 4 / RW shares of a chunk's keys:
+//   * RW = 4, where there are tiles of 128 rows for two workgroups on every compute unit (head sizes up to 128): one is in its products while the other
+//     is in its softmax.  4096 rows of 32 heads on 8, 128 wide: 158 us, 870 TFLOP/s; without exponentials, requests and reads of LDS it would be 125,
+//     which is what the products alone run at (a library product of 4096 cubed: 1150 TFLOP/s).
+//   * RW = 2, tiles of 64 rows, for fewer: a workgroup has the unit to itself, with four chunks in its ring (an eighth faster than two).  Bound by the chain
+//     of one chunk -- scores, maximum, weights, sums, 0.66 us, of which the products are 0.21 -- with nobody to fill its gaps; eight waves on chunks of 128
+//     take 0.60 per 64 positions, but 2.5 us more for their longer start and end (512 rows behind 512: 20.9 and 22.7 us), so four it is.
 //
 // Scores are formed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16): a lane has 16 of 32 keys' weights of ONE row, laid out as the operand of
 // O^T += V^T P^T; V^T by the transposing LDS read (slots 0..3 of lane half g are keys 4 g .. 4 g + 3 of sixteen, slots 4..7 keys 8 + 4 g ..).
@@ -34,7 +39,7 @@ constexpr int kPagedTileParts = 32;    // workgroups that share a tile's walk
 template <int KS, int RW>
 struct PagedTilesLds {
     static constexpr int DT = (KS + 1) / 2;
-    // Chunks in LDS: two where two workgroups share a compute unit, four (as far as they fit) where one has it to itself.
+    // Chunks in the ring: two where two workgroups share a compute unit, four (as far as they fit) where one has it to itself.
     static constexpr int kDepth = RW == 4 || KS > 8 ? 2 : 4;
     static constexpr int kRing = kDepth * 4 * PagedTile<KS>::kBytes;                    // [chunk % depth][keys, values][32 positions]
     static constexpr int kMeet = RW == 4 ? 0 : RW * 64 * (16 * DT * 4 + 8);             // half of the waves' sums
@@ -74,33 +79,52 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     if (value) req.template prepare<true>(lane);
     else req.template prepare<false>(lane);
     const auto first_of = [&](int chunk) { return min(chunk, c1) * kPagedChunk + 32 * (wave & 1); };
-    PagedEntries entries = paged_entries(c, line, first_of(c0), t.reach - 1);
+    // The table is looked at once for 32 chunks: a lane has the address of one of the wave's sixteens, two a chunk.  (Word by word, each chunk waited
+    // for its words and then computed 64-bit addresses in the only wave of its unit: 0.72 us a chunk.)
+    uint32_t low = 0, high = 0;
+    int held = c0;                                         // the first of the chunks
+    const auto look = [&](int chunk) __attribute__((always_inline)) {
+        held = chunk;
+        const int j = min(first_of(chunk + (lane >> 1)) + 16 * (lane & 1), t.reach - 1);
+        int page = line[j >> c.page_shift];
+        if ((uint32_t)page >= (uint32_t)c.pages) {
+            if (chunk + (lane >> 1) < c1) bad_page = 1;
+            page = 0;
+        }
+        const int inside = j & ((1 << c.page_shift) - 1) & ~15;
+        const uint64_t at = reinterpret_cast<uint64_t>(value ? c.v : c.k) + ((((int64_t)page * c.n_heads + head) << c.page_shift) + inside) * T::kRow;
+        low = (uint32_t)at;
+        high = (uint32_t)(at >> 32);
+    };
+    look(c0);
     // A request is prepared, and goes out piece by piece between the products: all at once, the wave stands still until the last piece has found a
     // place (700 cycles a chunk, as many as the products of the scores).
-    PagedBase next{{0, 0}, false};
+    PagedSource next{{nullptr, nullptr}};
     uint32_t next_at = 0;
     uint64_t pieces = 0;                                   // the lanes that bring them: all or none
     const auto prepare = [&](int chunk) __attribute__((always_inline)) {   // (one after the other)
-        pieces = 0;
-        if (chunk >= c1) return;
-        const int j0 = first_of(chunk);
-        next = paged_base<KS>(c, entries, head, j0, t.reach - 1);
-        entries = paged_entries(c, line, first_of(chunk + 1), t.reach - 1);
-        if (next.bad && lane == 0) bad_page = 1;
+        if (__builtin_expect(chunk - held >= 32, 0)) look(chunk);
+        const int i = 2 * (chunk - held);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            next.at[h] = reinterpret_cast<const uint8_t*>((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, i + h) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, i + h));
         next_at = to + (uint32_t)(chunk & (kDepth - 1)) * (4 * T::kBytes);
         pieces = ~0ull;
     };
-    const uint16_t* pool = value ? c.v : c.k;
+    const auto prepare_if = [&](int chunk) __attribute__((always_inline)) {
+        pieces = 0;
+        if (chunk < c1) prepare(chunk);
+    };
     constexpr int kSlots = KS * NB + 2 * NB * DT;          // of a chunk, a read and PIECES products each
-    const auto send_at = [&](int slot) __attribute__((always_inline)) {
+    const auto send_at = [&](int slot, auto sure) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            if (s * kSlots / KS == slot) req.piece(s, pool, next, next_at, pieces);
+            if (s * kSlots / KS == slot) req.template piece<!decltype(sure)::value>(s, next, next_at, pieces);
     };
 #pragma unroll
     for (int i = 0; i < kDepth - 1; ++i) {
-        prepare(c0 + i);
-        req.send(pool, next, next_at, pieces);
+        prepare_if(c0 + i);
+        req.template send<true>(next, next_at, pieces);
     }
 
     // the wave's rows: operand column l32
@@ -137,15 +161,15 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 
     // Chunks that every row of the tile sees whole, then those that end among the rows' own positions.  (The first kind's code lies side by side: a jump
     // costs as much as two products.)
-    const auto walk = [&](int chunk, auto which) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(which)::value;
+    // `sure`: chunks whose request, kDepth - 1 chunks on, is there to be made, so that it is known how many requests are behind the chunk's own.
+    const auto walk = [&](int chunk, auto which, auto sure) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(which)::value, kSure = decltype(sure)::value;
         const int j0 = chunk * kPagedChunk;
         const uint8_t* ring = lds + (chunk & (kDepth - 1)) * (4 * T::kBytes);
-        if (kDepth == 2 || chunk + 1 == c1) wait_vm<0>();
-        else if (chunk + 2 == c1) wait_vm<KS>();           // (so many requests behind the chunk's own)
-        else wait_vm<2 * KS>();
+        wait_vm<kSure ? (kDepth - 2) * KS : 0>();
         __syncthreads();                                   // the chunk is here, and nobody reads the one before it any more
-        prepare(chunk + kDepth - 1);
+        if constexpr (kSure) prepare(chunk + kDepth - 1);
+        else prepare_if(chunk + kDepth - 1);
         // Weights of zero may stand before values that a row does not see; infinities and NaN among those are put away and noted.
         bool careful = false;
         if constexpr (kMasked) {
@@ -199,7 +223,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
                 x[i % NB] = paged_mfma32<PIECES>(k[i % kAhead], q[i / NB], i < NB ? zero : x[i % NB]);
                 if (i + kAhead < kReads) k[i % kAhead] = read_k(i + kAhead);
-                send_at(i);
+                send_at(i, sure);
                 __builtin_amdgcn_sched_barrier(0);
             }
             // the first sixteen keys' value operands travel under the softmax
@@ -290,7 +314,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 for (int d = 0; d < DT; ++d) {
                     o[d] = paged_mfma32<PIECES>(v[d], w[n & 1], o[d]);
                     if (n + 1 < 2 * NB) v[d] = read_v(n + 1, d);
-                    send_at(kReads + n * DT + d);
+                    send_at(kReads + n * DT + d, sure);
                 }
                 if (n + 1 < 2 * NB) weights(n + 1, w[(n + 1) & 1]);
                 __builtin_amdgcn_sched_barrier(0);
@@ -310,12 +334,14 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 }
             }
         } else {
-            req.send(pool, next, next_at, pieces);
+            req.template send<!kSure>(next, next_at, pieces);
         }
     };
     const int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);
-    for (int chunk = c0; chunk < plain; ++chunk) walk(chunk, std::false_type{});
-    for (int chunk = plain; chunk < c1; ++chunk) walk(chunk, std::true_type{});
+    int chunk = c0;
+    for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{});
+    for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{});
+    for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{});
 
     run_l = over_blocks<32>(run_l, AddOp());
     __syncthreads();
@@ -388,7 +414,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum[d][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // (a read is a trip to memory: as many under way as there are registers for)
-    constexpr int kBatch = 8 / kPieces > 0 ? 8 / kPieces : 1;
+    constexpr int kBatch = kPieces > 1 ? 1 : 8;
     for (int n0 = 0; n0 < t.parts; n0 += kBatch) {
         float2 ml[kBatch];
         f32x4 x[kBatch][kPieces][4];
