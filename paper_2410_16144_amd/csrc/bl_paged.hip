@@ -14,8 +14,8 @@ namespace {
 constexpr int64_t kCounters = 1 << 14;     // of any call's: figures never lie where another call counts
 
 struct PagedPlan {
-    bool    rows_form;
-    int     tile_rows, most, least, wanted;
+    bool    rows_form, shallow;
+    int     tile_rows, most, least, join, wanted;
     int64_t wgs, slots, slot_bytes;
     int64_t counter_bytes, figure_bytes;
     bool launchable() const { return wgs < (1 << 24) && slots <= kCounters; }    // 2^32 threads (and every walk has a counter: 1024 key heads)
@@ -35,17 +35,25 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
     const auto tiles_of = [&](int tile_rows) { return single ? (int64_t)sequences * ceil_div(group, tile_rows) : all / tile_rows + std::min<int64_t>(sequences, rows); };
     // Workgroups that a call is meant for.  Rows: as many as keep enough requests under way, no more, since every part of a walk has to be joined (64
     // heads on 8 at 100 003 positions: one per compute unit 73.8 us, two 79.9; eight sequences of 32 heads, 584 MB: 104.4 and 113.6); rows of
-    // 64 elements and less have half the bytes under way.  Tiles: one per unit, joining is dearer still.
+    // 64 elements and less have half the bytes under way.  Tiles: one per unit, joining is dearer still (600 rows behind 512 of 32 heads: 24 us, for two 40).
     r.wanted = r.rows_form && width <= 64 ? 2 * cus : cus;
     if (r.rows_form) {
+        // 128, 256, 512, 1024 positions: 32 heads at 1000 positions 13.4, 14.3, 17.1, 19.0 us; 64 on 8 at 8000 23.7, 19.3, 18.7, 22.9.
         r.tile_rows = group;
         r.most = 256;
         r.least = 256;
         r.slot_bytes = (int64_t)group * (4 + head_dim) * 4;
     } else {
-        r.tile_rows = !bf16 || tiles_of(128) * n_heads < (width <= 128 ? 2 : 1) * cus ? 64 : 128;
-        r.most = 32;
-        r.least = 512;
+        // 128 rows where nearly two such tiles come on every unit (32 heads, 1024 rows behind as many: 49.7 us, 64 rows 42.4; 1700: 70.4 and 77.3; 4096 on
+        // 8 key heads: 153 and 218); tiles of 64 by two on a unit where there are more of them than units (1024 rows behind 4096: 97 us, by one 117), else
+        // by one (512 behind 512: 23.4 and 21.4).  Starts are the device's, so the last goes by full tiles.
+        r.tile_rows = !bf16 || 2 * tiles_of(128) * n_heads < (width <= 128 ? 3 : 2) * cus ? 64 : 128;
+        r.shallow = (single ? tiles_of(64) : ceil_div(all, 64)) * n_heads > cus;
+        // As 32, 64, 128 positions (paged_parts): 5 rows of 32 heads on 8 behind 1500 positions 14.0, 14.4, 15.6 us, behind 4000 18.3, 17.2, 19.1, behind
+        // 16 000 28.4, 26.3, 28.7; by 512 positions a part 17.8, 17.1, 30.7.
+        r.most = kPagedTileParts;
+        r.least = 256;
+        r.join = 64;
         r.slot_bytes = (int64_t)r.tile_rows * (ceil_div(width, 32) * 32 * 4 + 8);
     }
     r.most = (int)std::min<int64_t>(r.most, ceil_div(max_pos, r.least));
@@ -77,7 +85,7 @@ hipError_t launch_attn_paged(const ::bl_attn_paged_args& a, hipStream_t s) {
     const bool bf16 = a.dt == BL_BF16;
     const PagedPlan plan = paged_plan(p.c.n_heads, p.group, p.c.head_dim, p.c.sequences, p.c.rows, p.c.max_pos, p.c.start == nullptr, bf16);
     if (!plan.launchable()) return hipErrorInvalidConfiguration;
-    p.tile_rows = plan.tile_rows; p.most = plan.most; p.least = plan.least; p.rounded = plan.rows_form; p.slots = (int32_t)plan.slots; p.slot_bytes = (int32_t)plan.slot_bytes;
+    p.tile_rows = plan.tile_rows; p.most = plan.most; p.least = plan.least; p.join = plan.join; p.shallow = plan.shallow; p.slots = (int32_t)plan.slots; p.slot_bytes = (int32_t)plan.slot_bytes;
     p.target = (float)p.c.n_heads / (float)plan.wanted;
     p.counters = static_cast<uint32_t*>(a.scratch_dev);
     p.figures = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch_dev) + plan.counter_bytes);

@@ -297,6 +297,7 @@ __device__ __forceinline__ void paged_store(void* out, int64_t at, const f32x4& 
 // may be shared by several workgroups.  How many follows on the device from all positions that the call walks: each workgroup is meant to have
 // an equal share of them, `least` at least.  The grid is an upper bound; workgroups beyond what there is to do end at once.
 
+constexpr int kPagedTileParts = 32;   // workgroups that share a tile's walk at most
 constexpr int kPagedFew = 16;         // rows of a sequence and key head up to which the rows form takes them
 
 struct PagedArgs {
@@ -310,8 +311,9 @@ struct PagedArgs {
     int32_t     tile_rows;
     int32_t     most;          // workgroups of a walk
     int32_t     least;         // positions that are worth one
-    int32_t     rounded;       // whether a walk of a part and a bit is two (else one)
+    int32_t     join;          // positions that are walked while a part is joined; 0: nothing to speak of
     int32_t     slots;         // of figures
+    int32_t     shallow;       // tiles of 64 rows: whether two workgroups are to share a compute unit
     float       target;        // key heads / workgroups that the call is meant for
     float       scale;         // log2(e) / sqrt(head_dim)
 };
@@ -326,10 +328,11 @@ struct PagedWork {
 };
 
 __device__ __forceinline__ int paged_tiles(const PagedArgs& p, int rows) { return (int)(((int64_t)rows * p.group + p.tile_rows - 1) / p.tile_rows); }
-// (Rounded up, or, where joining parts is dear, down.)
+// Parts of a walk with `per` positions each: rounded up, or, where joining a part takes as long as `p.join` positions (tiles), down and by no more than
+// makes walking (reach / parts) and joining (parts * join) the shortest together.
 __device__ __forceinline__ int paged_parts(const PagedArgs& p, const PagedSequence& s, int per) {
     const int reach = s.pos + s.rows;
-    return min(p.rounded ? (reach - 1) / per + 1 : max(reach / per, 1), p.most);
+    return min(p.join == 0 ? (reach - 1) / per + 1 : max(reach / max(per, (int)sqrtf((float)p.join * (float)reach)), 1), p.most);
 }
 
 // What the call walks of a sequence, in positions (its tiles' mean).

@@ -3,12 +3,13 @@
 // One workgroup = a tile of 32 RW consecutive rows of one sequence and key head (a row is one query head of one token, token by token, so that
 // the query heads of a key head share what is read of it) against the positions 0 .. its last row's, 64 at a time through a ring of chunks in LDS with one
 // barrier a chunk.  Its four waves are RW sets of 32 rows times 4 / RW shares of a chunk's keys:
-//   * RW = 4, where there are tiles of 128 rows for two workgroups on every compute unit (head sizes up to 128): one is in its products while the other
-//     is in its softmax.  4096 rows of 32 heads on 8, 128 wide: 158 us, 870 TFLOP/s; without exponentials, requests and reads of LDS it would be 125,
+//   * RW = 4, tiles of 128 rows, two workgroups on a compute unit (head sizes up to 128): one is in its products while the other is in its softmax.
+//     4096 rows of 32 heads on 8, 128 wide: 158 us, 870 TFLOP/s; without exponentials, requests and reads of LDS it would be 125,
 //     which is what the products alone run at (a library product of 4096 cubed: 1150 TFLOP/s).
-//   * RW = 2, tiles of 64 rows, for fewer: a workgroup has the unit to itself, with four chunks in its ring (an eighth faster than two).  Bound by the chain
-//     of one chunk -- scores, maximum, weights, sums, 0.66 us, of which the products are 0.21 -- with nobody to fill its gaps; eight waves on chunks of 128
-//     take 0.60 per 64 positions, but 2.5 us more for their longer start and end (512 rows behind 512: 20.9 and 22.7 us), so four it is.
+//   * RW = 2, tiles of 64 rows, for fewer, also by two on a unit with a ring of two chunks, or by one with a ring of four (kDepth).  One alone is bound by
+//     the chain of its chunk -- scores, maximum, weights, sums, 0.66 us, of which the products are 0.21 -- with nobody to fill its gaps; eight waves on chunks
+//     of 128 take 0.60 per 64 positions, but 2.5 us more for their longer start and end (512 rows behind 512: 20.9 and 22.7 us), so four it is.
+// Which when: paged_plan.
 //
 // Scores are formed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16): a lane has 16 of 32 keys' weights of ONE row, laid out as the operand of
 // O^T += V^T P^T; V^T by the transposing LDS read (slots 0..3 of lane half g are keys 4 g .. 4 g + 3 of sixteen, slots 4..7 keys 8 + 4 g ..).
@@ -34,24 +35,19 @@ __device__ __forceinline__ f32x16 paged_mfma32(const s16x8& a, const s16x8 (&b)[
     return c;
 }
 
-constexpr int kPagedTileParts = 32;    // workgroups that share a tile's walk
-
-template <int KS, int RW>
+template <int KS, int RW, int DEPTH>
 struct PagedTilesLds {
     static constexpr int DT = (KS + 1) / 2;
-    // Chunks in the ring: two where two workgroups share a compute unit, four (as far as they fit) where one has it to itself.
-    static constexpr int kDepth = RW == 4 || KS > 8 ? 2 : 4;
-    static constexpr int kRing = kDepth * 4 * PagedTile<KS>::kBytes;                    // [chunk % depth][keys, values][32 positions]
+    static constexpr int kRing = DEPTH * 4 * PagedTile<KS>::kBytes;                    // [chunk % depth][keys, values][32 positions]
     static constexpr int kMeet = RW == 4 ? 0 : RW * 64 * (16 * DT * 4 + 8);             // half of the waves' sums
     static constexpr int kBytes = kRing > kMeet ? kRing : kMeet;
     static_assert(kBytes <= kMaxDecodeLds, "fits the LDS ceiling");
 };
 
-template <int KS, int PIECES, int RW>
+template <int KS, int PIECES, int RW, int kDepth>
 __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) void paged_tiles_kernel(const PagedArgs p) {
     using T = PagedTile<KS>;
     constexpr bool kBf16 = PIECES == 1;
-    constexpr int kDepth = PagedTilesLds<KS, RW>::kDepth;
     constexpr int KW = 4 / RW, DT = (KS + 1) / 2;
     constexpr int NB = 2 / KW;                             // a wave's blocks of 32 keys in a chunk
     static_assert(RW == 4 || RW == 2, "forms");
@@ -394,69 +390,70 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             for (int r = 0; r < 4; ++r) paged_leave(slot, mine + (d * 4 + r) * 1024, f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]});
         if (g == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(run_m), __float_as_uint(run_l)}, slot, pair, 0, kDeviceScope);
     }
-    if (!paged_last(p, t, last_one) || !used) return;      // uniform
+    if (!paged_last(p, t, last_one)) return;               // uniform
+    // Pieces of 32 rows by 32 elements, by all waves.  A read is a trip to memory: all parts' maxima in one, the figures of eight parts in one.
     const __amdgpu_buffer_rsrc_t from = paged_resource(paged_slot(p, t.slot));
-    float m = -INFINITY, l = 0.0f;
-    constexpr int kSome = 8;
-    for (int n0 = 0; n0 < t.parts; n0 += kSome) {
-        float2 ml[kSome];
+    constexpr int kSome = 8, kLots = kPagedTileParts / kSome;
+    static_assert(kPagedTileParts % kSome == 0, "whole lots");
+    const int pieces_used = (t.rows + 31) / 32 * DT;
+#pragma unroll 1
+    for (int piece = wave; piece < pieces_used; piece += 4) {
+        const int set = piece / DT, d = piece - set * DT, of = set * 32 + l32;
+        const int figures = (piece * 256 + lane) * 16, pairs = RW * DT * 4096 + of * 8;
+        float2 ml[kPagedTileParts];
 #pragma unroll
-        for (int n = 0; n < kSome; ++n) ml[n] = paged_read_pair(from, min(n0 + n, t.parts - 1) * p.slot_bytes + pair);
+        for (int b = 0; b < kLots; ++b)
+            if (b * kSome < t.parts) {
 #pragma unroll
-        for (int n = 0; n < kSome; ++n) m = fmaxf(m, ml[n].x);
-    }
-    const float ref = m == -INFINITY ? 0.0f : m * p.scale;
-    // the waves of the same rows have every KW-th 32 elements each
-    constexpr int kPieces = (DT + KW - 1) / KW;
-    f32x4 sum[kPieces][4];
+                for (int n = b * kSome; n < (b + 1) * kSome; ++n) ml[n] = paged_read_pair(from, min(n, t.parts - 1) * p.slot_bytes + pairs);
+            }
+        float m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int d = 0; d < kPieces; ++d)
+        for (int b = 0; b < kLots; ++b)
+            if (b * kSome < t.parts) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[d][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    // (a read is a trip to memory: as many under way as there are registers for)
-    constexpr int kBatch = kPieces > 1 ? 1 : 8;
-    for (int n0 = 0; n0 < t.parts; n0 += kBatch) {
-        float2 ml[kBatch];
-        f32x4 x[kBatch][kPieces][4];
+                for (int n = b * kSome; n < (b + 1) * kSome; ++n) m = fmaxf(m, ml[n].x);
+            }
+        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
+        f32x4 sum[4] = {};
+#pragma unroll 1
+        for (int n0 = 0; n0 < t.parts; n0 += kSome) {
+            float2 part[kSome];
+            f32x4 x[kSome][4];
 #pragma unroll
-        for (int n = 0; n < kBatch; ++n) {
-            const int from_part = min(n0 + n, t.parts - 1) * p.slot_bytes;
-            ml[n] = paged_read_pair(from, from_part + pair);
+            for (int n = 0; n < kSome; ++n) {
+                const int of_part = min(n0 + n, t.parts - 1) * p.slot_bytes;
+                part[n] = paged_read_pair(from, of_part + pairs);
 #pragma unroll
-            for (int d = 0; d < kPieces; ++d)
+                for (int r = 0; r < 4; ++r) x[n][r] = paged_read(from, of_part + figures + r * 1024);
+            }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[n][d][r] = paged_read(from, from_part + mine + (min(d * KW + kw, DT - 1) * 4 + r) * 1024);
+            for (int n = 0; n < kSome; ++n) {
+                if (n0 + n >= t.parts || part[n].y == 0.0f) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
+                const float f = paged_factor(part[n].x, part[n].y, p.scale, ref);
+                l += f * part[n].y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] += f * x[n][r];
+            }
         }
-#pragma unroll
-        for (int n = 0; n < kBatch; ++n) {
-            if (n0 + n >= t.parts || ml[n].y == 0.0f) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
-            const float f = paged_factor(ml[n].x, ml[n].y, p.scale, ref);
-            l += f * ml[n].y;
-#pragma unroll
-            for (int d = 0; d < kPieces; ++d)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum[d][r] += f * x[n][d][r];
-        }
-    }
-    if (!there) return;
-    const int64_t at = paged_row_at(p, t, row);
-    const float inv = 1.0f / l;
-#pragma unroll
-    for (int d = 0; d < kPieces; ++d)
+        if (of >= t.rows) continue;
+        const int64_t at = paged_row_at(p, t, of);
+        const float inv = 1.0f / l;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int e = 32 * (d * KW + kw) + 8 * r + 4 * g;
-            if (e < c.head_dim) paged_store<kBf16>(p.out, at + e, sum[d][r] * inv);
+            const int e = 32 * d + 8 * r + 4 * g;
+            if (e < c.head_dim) paged_store<kBf16>(p.out, at + e, sum[r] * inv);
         }
+    }
 }
 
-template <int KS, int PIECES, int RW>
+template <int KS, int PIECES, int RW, int DEPTH = (RW == 4 || KS > 8 ? 2 : 4)>
 hipError_t launch_paged_tiles_form(const PagedArgs& p, int64_t wgs, hipStream_t s) {
-    using L = PagedTilesLds<KS, RW>;
+    using L = PagedTilesLds<KS, RW, DEPTH>;
     static LdsCeiling ceiling;   // per instantiation, i.e. per kernel
-    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&paged_tiles_kernel<KS, PIECES, RW>), L::kBytes);
+    const hipError_t e = ceiling.ensure(reinterpret_cast<const void*>(&paged_tiles_kernel<KS, PIECES, RW, DEPTH>), L::kBytes);
     if (e != hipSuccess) return e;
-    paged_tiles_kernel<KS, PIECES, RW><<<dim3((unsigned)wgs), dim3(256), L::kBytes, s>>>(p);
+    paged_tiles_kernel<KS, PIECES, RW, DEPTH><<<dim3((unsigned)wgs), dim3(256), L::kBytes, s>>>(p);
     return hipGetLastError();
 }
 
@@ -466,8 +463,14 @@ hipError_t launch_paged_tiles_width(const PagedArgs& p, int64_t wgs, hipStream_t
         case 32: return launch_paged_tiles_form<2, PIECES, RW>(p, wgs, s);
         case 48: return launch_paged_tiles_form<3, PIECES, RW>(p, wgs, s);
         case 64: return launch_paged_tiles_form<4, PIECES, RW>(p, wgs, s);
-        case 96: return launch_paged_tiles_form<6, PIECES, RW>(p, wgs, s);
-        case 128: return launch_paged_tiles_form<8, PIECES, RW>(p, wgs, s);
+        case 96:
+            if constexpr (PIECES == 1 && RW == 2)
+                if (p.shallow) return launch_paged_tiles_form<6, PIECES, RW, 2>(p, wgs, s);
+            return launch_paged_tiles_form<6, PIECES, RW>(p, wgs, s);
+        case 128:
+            if constexpr (PIECES == 1 && RW == 2)
+                if (p.shallow) return launch_paged_tiles_form<8, PIECES, RW, 2>(p, wgs, s);
+            return launch_paged_tiles_form<8, PIECES, RW>(p, wgs, s);
         case 192: return launch_paged_tiles_form<12, PIECES, RW>(p, wgs, s);
         case 256: return launch_paged_tiles_form<16, PIECES, RW>(p, wgs, s);
     }
