@@ -153,6 +153,15 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     const int c0 = uniform((int)((int64_t)chunks * w.part / w.parts)), c1 = uniform((int)((int64_t)chunks * (w.part + 1) / w.parts));
     const int32_t* line = c.table + (int64_t)w.b * c.table_width;
 
+    // ---- the rows: operand column i16
+    const int token = i16 / p.group;
+    const bool there = i16 < rows;
+    const int64_t row_at = there ? paged_row_at(p, w, i16) : 0;
+    const int limit = s.pos + token;                       // the last position that the row sees
+    s16x8 q[kSteps][PIECES];
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) paged_query<PIECES>(p.q, row_at, 32 * t + 8 * g, c.head_dim, there, q[t]);
+
     // ---- requests
     uint8_t* tile = lds + wave * 2 * T::kBytes;
     const uint32_t at_k = __builtin_amdgcn_readfirstlane(lds_address(tile)), at_v = at_k + T::kBytes;
@@ -163,20 +172,16 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     PagedBase base{{0, 0}, false};
     PagedEntries entries{{0, 0}};
     if (chunk < c1) {
-        base = paged_base<KS>(c, paged_entries(c, line, 32 * chunk, reach - 1), head, 32 * chunk, reach - 1);
+        const PagedEntries first = paged_entries(c, line, 32 * chunk, reach - 1);
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+            for (int n = 0; n < PIECES; ++n) asm volatile("" : "+v"(q[t][n]));   // (the rows arrive while the table is looked at: no wait of theirs later)
+        base = paged_base<KS>(c, first, head, 32 * chunk, reach - 1);
         entries = paged_entries(c, line, 32 * (chunk + kWaves), reach - 1);
         req_k.send(paged_source(c.k, base), at_k);
         req_v.send(paged_source(c.v, base), at_v);
     }
-
-    // ---- the rows: operand column i16
-    const int token = i16 / p.group;
-    const bool there = i16 < rows;
-    const int64_t row_at = there ? paged_row_at(p, w, i16) : 0;
-    const int limit = s.pos + token;                       // the last position that the row sees
-    s16x8 q[kSteps][PIECES];
-#pragma unroll
-    for (int t = 0; t < kSteps; ++t) paged_query<PIECES>(p.q, row_at, 32 * t + 8 * g, c.head_dim, there, q[t]);
 
     f32x4 o[KS];
     float run_m = -INFINITY, run_l = 0.0f;                 // run_l: over this lane group's positions only

@@ -68,6 +68,19 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     if (tid == 0) odd_chunk = bad_page = 0;
     __syncthreads();
 
+    // the wave's rows: operand column l32
+    const int row = rw * 32 + l32;                         // of the tile
+    const bool there = row < t.rows;
+    const int limit = t.s.pos + (t.row0 + row) / p.group;  // the last position that the row sees
+    const int wave_low = t.s.pos + uniform((t.row0 + rw * 32) / p.group);
+    const int wave_high = rw * 32 < t.rows ? t.s.pos + uniform((t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group) : -1;
+    s16x8 q[KS][PIECES];
+    {
+        const int64_t row_at = there ? paged_row_at(p, t, row) : 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) paged_query<PIECES>(p.q, row_at, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
+    }
+
     // waves 0 and 1 bring a chunk's keys, 2 and 3 its values, 32 positions each
     const bool value = wave >= 2;
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * T::kBytes);
@@ -93,6 +106,10 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         high = (uint32_t)(at >> 32);
     };
     look(c0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) asm volatile("" : "+v"(q[ks][i]));   // (here they have arrived, under the look at the table: no wait of theirs later)
     // A request is prepared, and goes out piece by piece between the products: all at once, the wave stands still until the last piece has found a
     // place (700 cycles a chunk, as many as the products of the scores).
     PagedSource next{{nullptr, nullptr}};
@@ -122,23 +139,6 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         prepare_if(c0 + i);
         req.template send<true>(next, next_at, pieces);
     }
-
-    // the wave's rows: operand column l32
-    const int row = rw * 32 + l32;                         // of the tile
-    const bool there = row < t.rows;
-    const int limit = t.s.pos + (t.row0 + row) / p.group;  // the last position that the row sees
-    const int wave_low = t.s.pos + uniform((t.row0 + rw * 32) / p.group);
-    const int wave_high = rw * 32 < t.rows ? t.s.pos + uniform((t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group) : -1;
-    s16x8 q[KS][PIECES];
-    {
-        const int64_t row_at = there ? paged_row_at(p, t, row) : 0;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) paged_query<PIECES>(p.q, row_at, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) asm volatile("" : "+v"(q[ks][i]));   // (here they have arrived: no wait of theirs in the loop)
 
     f32x16 o[DT];
     float run_m = -INFINITY, run_l = 0.0f;                 // run_l: over this lane half's keys only
