@@ -501,9 +501,11 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  * pieces of prompts and any mixture; without start_dev it is made for single tokens.
  *   q_dev, out_dev  [rows, n_q_heads * head_dim] fp32 or bf16 (dt, both the same), 8-byte aligned; must not overlap
  *   scratch_dev     bl_attn_paged_scratch_bytes(...) bytes, 256-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
- *                   any other call with as many key heads and no greater need.  Calls that may overlap in time must not share it.
- * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with
- * weights rounded to bf16; everything else is fp32.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
+ *                   any other call with no greater need.  Calls that may overlap in time must not share it.
+ * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with weights as
+ * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32.  How a walk is cut, and so the order of sums, follows from all sequences
+ * of the call: a row's bits may differ between calls of different company.
+ * What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
  * that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
  * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
  * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,

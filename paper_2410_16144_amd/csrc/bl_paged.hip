@@ -34,9 +34,11 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
     r.rows_form = single && group <= kPagedFew;
     const auto tiles_of = [&](int tile_rows) { return single ? (int64_t)sequences * ceil_div(group, tile_rows) : all / tile_rows + std::min<int64_t>(sequences, rows); };
     // Workgroups that a call is meant for.  Rows: as many as keep enough requests under way, no more, since every part of a walk has to be joined (64
-    // heads on 8 at 100 003 positions: one per compute unit 73.8 us, two 79.9; eight sequences of 32 heads, 584 MB: 104.4 and 113.6); rows of
-    // 64 elements and less have half the bytes under way.  Tiles: one per unit, joining is dearer still (600 rows behind 512 of 32 heads: 24 us, for two 40).
-    r.wanted = r.rows_form && width <= 64 ? 2 * cus : cus;
+    // heads on 8 at 100 003 positions: one per compute unit 73.8 us, two 79.9; eight sequences of 32 heads, 584 MB: 104.4 and 113.6); but rows of 64 elements
+    // and less have half the bytes under way, and many sequences of unlike lengths want smaller parts more than few of them (32 heads on 8 over 60 to
+    // 4000 positions: 64 sequences 54.9 us with two per unit, 61.1 with one, 128 97 and 108; of like lengths the same, 88).
+    // Tiles: one per unit, joining is dearer still (600 rows behind 512 of 32 heads: 24 us, for two 40).
+    r.wanted = r.rows_form && (width <= 64 || (int64_t)sequences * n_heads >= 2 * cus) ? 2 * cus : cus;
     if (r.rows_form) {
         // 128, 256, 512, 1024 positions: 32 heads at 1000 positions 13.4, 14.3, 17.1, 19.0 us; 64 on 8 at 8000 23.7, 19.3, 18.7, 22.9.
         r.tile_rows = group;

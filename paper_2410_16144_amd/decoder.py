@@ -261,7 +261,7 @@ class PagedCache:
                g_k: Optional[torch.Tensor] = None, eps: float = EPS, q_dtype: Optional[torch.dtype] = None, q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """bl_paged_append: the rows' keys (normed per head by g_k [head_dim], rotated) and values into their pages; returns the queries (normed by g_q,
         rotated), in q_dtype (default: q's) or in q_out.  q [rows, n_q_heads * head_dim], k, v [rows, n_heads * head_dim], fp32 or bf16, rows anywhere.
-        table: the rotary table, up to rows.max_pos; None: no rotation."""
+        table: the rotary table, up to rows.max_pos; None: no rotation.  Rows that no sequence has: see attn_paged."""
         c = B.calls()
         q_dtype = q.dtype if q_dtype is None else q_dtype
         r = None
@@ -308,8 +308,8 @@ class PagedRows:
 
 
 def paged_scratch(n_heads: int, cache: PagedCache, rows: PagedRows) -> torch.Tensor:
-    """Scratch memory for attn_paged calls of n_heads query heads with as many sequences and rows (or fewer): zero, and kept usable by every call.  Calls
-    that may overlap in time need one each."""
+    """Scratch memory for attn_paged calls of n_heads query heads with as many sequences, rows and positions (or fewer): zero, and kept usable by every
+    call.  One for rows with a start serves calls without, too.  Calls that may overlap in time need one each."""
     bytes_ = B.bl_attn_paged_scratch_bytes(n_heads, cache.n_heads, cache.head_dim, rows.sequences, rows.rows, rows.max_pos, rows.start is None)
     if bytes_ == 0:
         raise B.BitLinearError(B.BL_ERR_SHAPE, "paged_scratch")
@@ -328,7 +328,7 @@ def _check_paged(q, cache, rows, scratch, out):
 
 def attn_paged(q: torch.Tensor, cache: PagedCache, rows: PagedRows, scratch: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """bl_attn_paged: every row of q ([rows, n_heads * head_dim] fp32 or bf16, as PagedCache.append leaves it) against its sequence's positions up to its
-    own.  Rows that no sequence has stay as they are in out."""
+    own.  Rows that no sequence has stay as they are in out (and hold anything where it is not given)."""
     c = B.calls()
     r = c.attn_paged(cache.args, cache.k, rows.args, rows.table, q, scratch, out) if c else None
     if r is not None:
