@@ -468,7 +468,7 @@ typedef struct bl_paged_rows {
  *   (y[i], y[i + head_dim/2]) rotated by the table's row of the token's position, as bl_attn_decode rotates (without a table: as they are)
  *   q_dev        [rows, ld_q >= n_q_heads * head_dim], k_dev [rows, ld_k], v_dev [rows, ld_v >= n_heads * head_dim], fp32 or bf16 (dt), aligned
  *                to the element
- *   q_out_dev    [rows, n_q_heads * head_dim] fp32 or bf16 (q_out_dt), 16-byte aligned; must not overlap the inputs
+ *   q_out_dev    [rows, n_q_heads * head_dim] fp32 or bf16 (q_out_dt), 16-byte aligned; must not overlap the inputs or the pages
  *   gamma_q_dev, gamma_k_dev   [head_dim] fp32, either may be NULL
  *   rope_table_dev   the table of bl_rope_table, max_pos rows or more; may be NULL
  * A position whose page number is outside 0 .. pages - 1 is not stored.
@@ -499,15 +499,14 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  * Attention over the pages: the row of position p attends to positions 0 .. p of its sequence, which are in the cache already (bl_paged_append),
  * scores scaled by 1 / sqrt(head_dim).  Query head i reads key head i / (n_q_heads / cache->n_heads).  One call serves single tokens, prompts,
  * pieces of prompts and any mixture; without start_dev it is made for single tokens.
- *   q_dev, out_dev  [rows, n_q_heads * head_dim] fp32 or bf16 (dt, both the same), 8-byte aligned; must not overlap
+ *   q_dev, out_dev  [rows, n_q_heads * head_dim] fp32 or bf16 (dt, both the same), 8-byte aligned; out_dev overlaps nothing else of the call
  *   scratch_dev     bl_attn_paged_scratch_bytes(...) bytes, 256-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
  *                   any other call with no greater need.  Calls that may overlap in time must not share it.
  * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with weights as
  * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32.  How a walk is cut, and so the order of sums, follows from all sequences
- * of the call: a row's bits may differ between calls of different company.
- * What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
- * that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
- * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
+ * of the call: a row's bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a
+ * key or a value that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a
+ * page are NaN, other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
  * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,
  *         BL_ERR_HIP.
  */

@@ -720,6 +720,11 @@ static bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_b
     return x < y + b_bytes && y < x + a_bytes;
 }
 
+static bool overlaps_pages(const bl_paged_cache* c, const void* out, uint64_t bytes) {
+    const uint64_t pool = (uint64_t)c->pages * c->n_heads * c->page_size * bl_paged_width(c->head_dim) * 2;
+    return overlap(c->k_pages_dev, pool, out, bytes) || overlap(c->v_pages_dev, pool, out, bytes);
+}
+
 bl_status bl_paged_append(const bl_paged_append_args* a, void* stream) {
     if (!a || !a->q_dev || !a->k_dev || !a->v_dev || !a->q_out_dev) return BL_ERR_NULL;
     const bl_status s = check_paged(a->cache, a->rows, a->n_q_heads);
@@ -733,6 +738,7 @@ bl_status bl_paged_append(const bl_paged_append_args* a, void* stream) {
         if (overlap(x[i], (uint64_t)((T - 1) * ld[i] + heads[i] * d) * e, a->q_out_dev, out_bytes)) return BL_ERR_SHAPE;
         if (!aligned(x[i], e)) return BL_ERR_ALIGN;
     }
+    if (overlaps_pages(a->cache, a->q_out_dev, out_bytes)) return BL_ERR_SHAPE;
     if (!aligned(a->q_out_dev, 16) || !aligned(a->gamma_q_dev, 4) || !aligned(a->gamma_k_dev, 4) || !aligned(a->rope_table_dev, 8)) return BL_ERR_ALIGN;
     drop_stale_hip_error();
     return shape_status(bl::launch_paged_append(*a, static_cast<hipStream_t>(stream)));
@@ -749,7 +755,10 @@ bl_status bl_attn_paged(const bl_attn_paged_args* a, void* stream) {
     if (s != BL_OK) return s;
     if (a->dt != BL_F32 && a->dt != BL_BF16) return BL_ERR_DTYPE;
     const uint64_t bytes = (uint64_t)a->rows->rows * a->n_q_heads * a->cache->head_dim * (a->dt == BL_BF16 ? 2 : 4);
-    if (overlap(a->q_dev, bytes, a->out_dev, bytes)) return BL_ERR_SHAPE;
+    const uint64_t scratch = bl_attn_paged_scratch_bytes(a->n_q_heads, a->cache->n_heads, a->cache->head_dim, a->rows->sequences, a->rows->rows, a->rows->max_pos,
+                                                         a->rows->start_dev == nullptr);
+    if (overlap(a->q_dev, bytes, a->out_dev, bytes) || overlap(a->scratch_dev, scratch, a->out_dev, bytes) || overlaps_pages(a->cache, a->out_dev, bytes))
+        return BL_ERR_SHAPE;
     if (!aligned(a->q_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 256)) return BL_ERR_ALIGN;
     drop_stale_hip_error();
     return shape_status(bl::launch_attn_paged(*a, static_cast<hipStream_t>(stream)));

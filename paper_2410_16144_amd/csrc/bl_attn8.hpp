@@ -1,7 +1,6 @@
 // What the kernels of the attention over 8-bit caches share: arguments, the operands' numbers, and how the workgroups of a row meet.
 #pragma once
 #include "bl_attn8_plan.hpp"
-#include "bl_figures.hpp"
 #include "bl_kv8.hpp"
 #include "bl_lanes.hpp"
 #include "bl_quant_device.hpp"
@@ -54,6 +53,15 @@ __device__ __forceinline__ bool attn8_takes_part(const Attn8Args& p, int pos) { 
 __device__ __forceinline__ int64_t attn8_row_at(const Attn8Args& p, int head, int row) {
     const int token = divided(row, p.by_group);
     return ((int64_t)token * p.n_heads * p.group + head * p.group + row - token * p.group) * p.head_dim;
+}
+
+__device__ __forceinline__ float2 read_figure(float2* at) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<unsigned long long*>(at), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+__device__ __forceinline__ void leave_figure(float2* at, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(at), (unsigned long long)__float_as_uint(x) | (unsigned long long)__float_as_uint(y) << 32,
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 __device__ __forceinline__ int attn8_sets(int positions, int set) { return (positions + (1 << set) - 1) >> set; }

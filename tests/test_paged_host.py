@@ -87,6 +87,7 @@ def test_refusals_of_append():
         assert call(q=FAR + off) == B.BL_ERR_SHAPE, off
     assert call(k=FAR + 64) == call(v=FAR) == B.BL_ERR_SHAPE
     assert call(q=FAR - out_bytes, g_q=P + 2) == call(q=FAR + out_bytes, g_q=P + 2) == B.BL_ERR_ALIGN      # (nothing wrong with q)
+    assert call(_cache(k_pages_dev=FAR + 16)) == call(_cache(v_pages_dev=FAR - 16)) == B.BL_ERR_SHAPE
     assert call(_cache(n_heads=1), _rows(rows=1 << 24), n_q=64, ld_q=4096) == B.BL_ERR_SHAPE               # 2^32 threads
 
 
@@ -106,6 +107,11 @@ def test_refusals_of_the_attention():
         assert call(**kw) == B.BL_ERR_ALIGN, kw
     for off in (0, 8, 7 * 512 * 4 - 8, 8 - 7 * 512 * 4):
         assert call(q=FAR + off) == B.BL_ERR_SHAPE
+    pool = 10 * 4 * 32 * 64 * 2
+    for far in (dict(k_pages_dev=FAR + 16), dict(v_pages_dev=FAR - pool + 16)):
+        assert call(_cache(**far)) == B.BL_ERR_SHAPE, far
+    assert call(_cache(k_pages_dev=FAR - pool), q=P + 4) == B.BL_ERR_ALIGN                                 # (nothing wrong with the pages)
+    assert call(scratch=FAR + 256) == call(scratch=FAR - 256) == B.BL_ERR_SHAPE
     assert call(_cache(n_heads=1), _rows(rows=1 << 24), n_q=64) == B.BL_ERR_SHAPE                          # 2^32 threads
 
 
