@@ -168,25 +168,29 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     PagedRequest<KS, true> req_k, req_v;
     req_k.template prepare<false>(lane);
     req_v.template prepare<true>(lane);
-    int chunk = c0 + wave;
+    int chunk;
     PagedBase base{{0, 0}, false};
     PagedEntries entries{{0, 0}};
-    if (chunk < c1) {
-        const PagedEntries first = paged_entries(c, line, 32 * chunk, reach - 1);
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t)
-#pragma unroll
-            for (int n = 0; n < PIECES; ++n) asm volatile("" : "+v"(q[t][n]));   // (the rows arrive while the table is looked at: no wait of theirs later)
-        base = paged_base<KS>(c, first, head, 32 * chunk, reach - 1);
-        entries = paged_entries(c, line, 32 * (chunk + kWaves), reach - 1);
-        req_k.send(paged_source(c.k, base), at_k);
-        req_v.send(paged_source(c.v, base), at_v);
-    }
-
     f32x4 o[KS];
-    float run_m = -INFINITY, run_l = 0.0f;                 // run_l: over this lane group's positions only
+    float run_m, run_l;                                    // run_l: over this lane group's positions only
+    const auto begin = [&]() __attribute__((always_inline)) {
+        chunk = c0 + wave;
+        if (chunk < c1) {
+            const PagedEntries first = paged_entries(c, line, 32 * chunk, reach - 1);
 #pragma unroll
-    for (int t = 0; t < KS; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int t = 0; t < kSteps; ++t)
+#pragma unroll
+                for (int n = 0; n < PIECES; ++n) asm volatile("" : "+v"(q[t][n]));   // (the rows arrive while the table is looked at: no wait of theirs later)
+            base = paged_base<KS>(c, first, head, 32 * chunk, reach - 1);
+            entries = paged_entries(c, line, 32 * (chunk + kWaves), reach - 1);
+            req_k.send(paged_source(c.k, base), at_k);
+            req_v.send(paged_source(c.v, base), at_v);
+        }
+        run_m = -INFINITY;
+        run_l = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    };
 
     // Chunks that the sequence has whole, then its last one.  (The first kind's code lies side by side: jumps cost as much as products.)
     const auto walk = [&](auto which) __attribute__((always_inline)) {
@@ -290,8 +294,22 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         if (next < c1) req_v.send(paged_source(c.v, base), at_v);
         chunk = next;
     };
-    while (chunk < c1 && 32 * chunk + 31 <= s.pos) walk(std::false_type{});
-    while (chunk < c1) walk(std::true_type{});
+    // The pieces of a weight times an infinity add up to NaN.  So a walk whose sums are not finite is walked again with such values put away throughout.
+    for (bool again = false;; again = true) {
+        begin();
+        const bool plain = !again && chunk < c1 && 32 * chunk + 31 <= s.pos;
+        if (plain)
+            do walk(std::false_type{});
+            while (chunk < c1 && 32 * chunk + 31 <= s.pos);
+        while (chunk < c1) walk(std::true_type{});
+        if (!plain) break;
+        float odd = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd = fmaf(o[t][r], 0.0f, odd);
+        if (!__any(odd != odd)) break;
+    }
 
     // ---- the waves meet
     run_l = over_blocks<32>(over_blocks<16>(run_l, AddOp()), AddOp());

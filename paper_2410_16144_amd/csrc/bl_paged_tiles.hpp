@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     constexpr int NB = 2 / KW;                             // a wave's blocks of 32 keys in a chunk
     static_assert(RW == 4 || RW == 2, "forms");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ int odd_chunk, bad_page, last_one;
+    __shared__ int odd_chunk, odd_sums, bad_page, last_one;
     __shared__ uint32_t odd_values[2][kPagedChunk * DT];   // [up, down][key][32 elements]: where infinities and NaN were
     __shared__ uint32_t odd_seen[2 * DT][256];             // the same of the keys that a lane's row sees
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     const int head = t.head, chunks = (t.reach + kPagedChunk - 1) / kPagedChunk;
     const int c0 = uniform((int)((int64_t)chunks * t.part / t.parts)), c1 = uniform((int)((int64_t)chunks * (t.part + 1) / t.parts));
     const int32_t* line = c.table + (int64_t)t.b * c.table_width;
-    if (tid == 0) odd_chunk = bad_page = 0;
+    if (tid == 0) odd_chunk = odd_sums = bad_page = 0;
     __syncthreads();
 
     // the wave's rows: operand column l32
@@ -134,18 +134,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         for (int s = 0; s < KS; ++s)
             if (s * kSlots / KS == slot) req.template piece<!decltype(sure)::value>(s, next, next_at, pieces);
     };
-#pragma unroll
-    for (int i = 0; i < kDepth - 1; ++i) {
-        prepare_if(c0 + i);
-        req.template send<true>(next, next_at, pieces);
-    }
-
     f32x16 o[DT];
-    float run_m = -INFINITY, run_l = 0.0f;                 // run_l: over this lane half's keys only
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    float run_m, run_l;                                    // run_l: over this lane half's keys only
     int v_at[DT];                                          // of the transposing reads
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
@@ -333,14 +323,37 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             req.template send<!kSure>(next, next_at, pieces);
         }
     };
-    const int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);
-    int chunk = c0;
-    for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{});
-    for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{});
-    for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{});
-
+    // A weight's pieces times an infinity add up to NaN, as a weight of zero does.  So a walk whose sums are not finite is walked again with such values put
+    // away throughout.
+    for (int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);; plain = c0) {
+#pragma unroll
+        for (int i = 0; i < kDepth - 1; ++i) {
+            prepare_if(c0 + i);
+            req.template send<true>(next, next_at, pieces);
+        }
+        run_m = -INFINITY;
+        run_l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+        int chunk = c0;
+        for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{});
+        for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{});
+        for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{});
+        if (plain > c0) {
+            float odd = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) odd = fmaf(o[d][r], 0.0f, odd);
+            if (odd != odd) odd_sums = 1;
+        }
+        __syncthreads();
+        if (plain == c0 || !uniform(odd_sums)) break;
+        look(c0);
+    }
     run_l = over_blocks<32>(run_l, AddOp());
-    __syncthreads();
     if (uniform(bad_page)) run_l = NAN;                             // (rows of a sequence whose table names a page that is not there)
     if constexpr (KW == 2) {                               // the chunk's shares meet
         float* meet = reinterpret_cast<float*>(lds) + rw * (64 * 16 * DT);

@@ -242,28 +242,21 @@ def test_packed_sequences_in_every_form(dev, dec, heads, n, d, page, before, new
     _attend(dec, dev, heads, n, d, page, before, new, G, 90 + d, extra=extra)
 
 
-@pytest.mark.parametrize("extra", [0, 2200, 7000])
-@pytest.mark.parametrize("d", [64, 96, 128])
-@pytest.mark.parametrize("before,new", [(0, 65), (100, 40), (63, 1), (500, 130)])
-def test_values_that_are_not_finite_in_every_form(dev, dec, d, before, new, extra):
-    """Several positions among the new ones hold them; a row is what the formula makes of those that it sees."""
+def _with_odd_values(dec, dev, d, before, new, at, dtype, extra=0, single=False):
+    """Values of the positions `at` that are not finite; a row is what the formula makes of those that it sees."""
     heads, n = 8, 2
     srv = Server(dec, dev, n, d, 16, [before + new], 95)
     srv.fill(0, before + new)
-    at = sorted({before + new - 1, before + new // 2, before + new // 3, max(0, before - 1)})
     clean = srv.v[0].clone()
     odd = torch.zeros((before + new, n, d))
     for i, p in enumerate(at):
         for e, x in ((i, math.inf), (d - 1 - i, -math.inf), (d // 2 + i, math.nan), (20, math.inf if i % 2 else -math.inf)):
             odd[p, :, e] = x
             clean[p, :, e] = 0
-    for p in at:
-        page, slot = int(srv.lines[0, p // 16]), p % 16
-        v = clean[p] + odd[p].double()
-        srv.cache.v[page, :, slot, :d] = v.to(G).to(dev)
-    q = torch.zeros((new + extra, heads * d), dtype=G, device=dev)
-    q[:new] = _queries(srv.g, new, heads, d, G, dev)
-    rows = srv.rows(dec, [before], [new], total=new + extra)
+        srv.cache.v[int(srv.lines[0, p // 16]), :, p % 16, :d] = (clean[p] + odd[p].double()).to(G).to(dev)
+    q = torch.zeros((new + extra, heads * d), dtype=dtype, device=dev)
+    q[:new] = _queries(srv.g, new, heads, d, dtype, dev)
+    rows = srv.rows(dec, [before], [new], single, total=new + extra)
     out = dec.attn_paged(q, srv.cache, rows, dec.paged_scratch(heads, srv.cache, rows))[:new].double().cpu().view(new, heads, d)
     seen = before + 1 + torch.arange(new)
     want, S, V = _want(q[:new].double().cpu().view(new, heads, d), srv.k[0], clean, heads // n, seen)
@@ -275,7 +268,26 @@ def test_values_that_are_not_finite_in_every_form(dev, dec, d, before, new, extr
     finite = torch.isfinite(touched)
     assert torch.equal(out.isnan(), touched.isnan())
     assert torch.equal(out[touched.isinf()].float(), touched[touched.isinf()])
-    _close(torch.where(finite, out, want), want, S, V, d, G)
+    _close(torch.where(finite, out, want), want, S, V, d, dtype)
+
+
+@pytest.mark.parametrize("extra", [0, 2200, 7000])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("before,new", [(0, 65), (100, 40), (63, 1), (500, 130)])
+def test_values_that_are_not_finite_in_every_form(dev, dec, d, before, new, extra):
+    at = sorted({before + new - 1, before + new // 2, before + new // 3, max(0, before - 1)})
+    _with_odd_values(dec, dev, d, before, new, at, G, extra)
+
+
+@pytest.mark.parametrize("dtype", [F, G])
+@pytest.mark.parametrize("d", [48, 64, 100, 128, 256])
+@pytest.mark.parametrize("before,new,at", [(900, 1, [5, 300, 700]), (900, 1, [899]), (900, 70, [0, 899]), (2600, 5, [64, 1300, 2500]), (90, 90, [100, 170])])
+@pytest.mark.parametrize("single", [True, False])
+def test_values_that_are_not_finite_far_behind(dev, dec, dtype, d, before, new, at, single):
+    """Where every row sees the whole chunk: the pieces of a weight must not make NaN of an infinity."""
+    if single and new > 1:
+        before, new = before + new - 1, 1
+    _with_odd_values(dec, dev, d, before, new, at, dtype, single=single)
 
 
 # ---------------------------------------------------------------------------------------------------- limits
