@@ -418,7 +418,8 @@ bl_status bl_attn8_prefill(const bl_attn8_prefill_args *args, void *stream);
  *   n_heads      key heads; head_dim a multiple of 4 (4 .. BL_ATTN_MAX_HEAD_DIM)
  *   page_size    positions of a page, a power of two, BL_PAGE_MIN .. BL_PAGE_MAX
  *   k_pages_dev, v_pages_dev   [pages][n_heads][page_size][bl_paged_width(head_dim)] bf16 bit patterns, 16-byte aligned
- * The elements behind head_dim of a row are written as zero with their row; rows that were never written may hold anything.
+ * The elements behind head_dim of a row are written as zero with their row (whoever fills rows by other means does the same); rows that were never
+ * written may hold anything.
  */
 #define BL_PAGE_MIN 16
 #define BL_PAGE_MAX 4096
@@ -446,6 +447,7 @@ int32_t bl_paged_width(int32_t head_dim);
  *   table_dev   [sequences, table_width] int32; only entries up to the call's last position of a sequence are read
  *   pos_dev     [sequences] int32
  *   start_dev   [sequences + 1] int32, rising; may be NULL: then rows == sequences
+ *   rows        1 .. 2^24; sequences 1 .. BL_PAGED_MAX_SEQUENCES
  *   max_pos     no position of the call is max_pos or beyond; 1 <= max_pos <= table_width * page_size, max_pos <= BL_PAGED_MAX_POS
  * All four are read on the device, so a captured launch serves other lengths, pages and numbers of rows up to `rows`.  What they say is looked at
  * before it is used: a sequence with a negative position, with positions from max_pos on, or with rows outside 0 .. rows - 1 takes no part, its
@@ -503,10 +505,11 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  *   scratch_dev     bl_attn_paged_scratch_bytes(...) bytes, 256-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
  *                   any other call with no greater need.  Calls that may overlap in time must not share it.
  * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with weights as
- * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32.  How a walk is cut, and so the order of sums, follows from all sequences
- * of the call: a row's bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a
- * key or a value that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a
- * page are NaN, other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
+ * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32 (sums of values by weights of up to 2^8, divided at the end: values
+ * within a walk's length of fp32's largest may overflow).  How a walk is cut, and so the order of sums, follows from all sequences of the call: a row's
+ * bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
+ * that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
+ * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
  * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,
  *         BL_ERR_HIP.
  */

@@ -303,6 +303,8 @@ class PagedRows:
             if start is not None:
                 raise ValueError("rows: how many rows the call has at most")
             rows = n
+        if not (1 <= rows <= 1 << 24 and 1 <= max_pos <= B.BL_PAGED_MAX_POS and 1 <= n <= B.BL_PAGED_MAX_SEQUENCES):
+            raise B.BitLinearError(B.BL_ERR_SHAPE, "PagedRows")
         self.table, self.pos, self.start, self.max_pos, self.rows, self.sequences = table, pos, start, max_pos, rows, n
         self.args = B.PagedRows(table.data_ptr(), pos.data_ptr(), start.data_ptr() if start is not None else None, int(table.shape[1]), n, rows, max_pos)
 

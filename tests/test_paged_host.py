@@ -151,6 +151,10 @@ def test_what_the_python_side_asks_for():
         a.update(bad)
         with pytest.raises(AssertionError):
             decoder.PagedRows(**a)
+    for bad in (dict(max_pos=0), dict(max_pos=(1 << 32) + 5), dict(rows=(1 << 32) + 3, start=torch.zeros(4, dtype=torch.int32)), dict(pos=pos[:0], table=table[:0])):
+        with pytest.raises(B.BitLinearError) as e:
+            decoder.PagedRows(**dict(dict(table=table, pos=pos, max_pos=32), **bad))
+        assert e.value.status == B.BL_ERR_SHAPE
     q = torch.zeros((3, 400))
     with pytest.raises(AssertionError):
         decoder.attn_paged(q, c, r, torch.zeros(1 << 20, dtype=torch.uint8))       # not on a device
