@@ -130,9 +130,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     };
     constexpr int kSlots = KS * NB + 2 * NB * DT;          // of a chunk, a read and PIECES products each
     const auto send_at = [&](int slot, auto sure) __attribute__((always_inline)) {
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-            if (s * kSlots / KS == slot) req.template piece<!decltype(sure)::value>(s, next, next_at, pieces);
+        const int s = (slot * KS + kSlots - 1) / kSlots;   // the piece whose place this is, if any
+        if (s < KS && s * kSlots / KS == slot) req.template piece<!decltype(sure)::value>(s, next, next_at, pieces);
     };
     f32x16 o[DT];
     float run_m, run_l;                                    // run_l: over this lane half's keys only
@@ -191,7 +190,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             }
         }
         const int block = KW == 2 ? kw : 0, j1 = j0 + 32 * block;
-        if (kMasked ? j1 <= wave_high : wave_high >= 0) {  // uniform
+        // (Uniform.  Wide heads: a branch would cost registers for a second set of sums, which these have to fetch from memory in every chunk.)
+        if (KS > 8 || (kMasked ? j1 <= wave_high : wave_high >= 0)) {
             const uint8_t* keys = ring + block * T::kBytes;
             const uint8_t* values = ring + (2 + block) * T::kBytes;
             f32x16 x[NB];
