@@ -51,8 +51,8 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
         // by one (512 behind 512: 23.4 and 21.4).  Starts are the device's, so the last goes by full tiles.
         r.tile_rows = !bf16 || 2 * tiles_of(128) * n_heads < (width <= 128 ? 3 : 2) * cus ? 64 : 128;
         r.shallow = (single ? tiles_of(64) : ceil_div(all, 64)) * n_heads > cus;
-        // As 32, 64, 128 positions (paged_parts): 5 rows of 32 heads on 8 behind 1500 positions 14.0, 14.4, 15.6 us, behind 4000 18.3, 17.2, 19.1, behind
-        // 16 000 28.4, 26.3, 28.7; by 512 positions a part 17.8, 17.1, 30.7.
+        // As 32, 64, 128 positions (paged_parts): 5 rows of 32 heads on 8 behind 1500 positions 13.7, 14.3, 15.4 us, behind 4000 16.7, 18.0, 19.1, behind
+        // 16 000 24.8, 24.9, 26.7; 64 rows of 12 heads behind 16 000 39.4, 36.7, 35.9; 16 rows of 64 heads on 8 behind 3000 21.8, 20.1, 21.8.
         r.most = kPagedTileParts;
         r.least = 256;
         r.join = 64;

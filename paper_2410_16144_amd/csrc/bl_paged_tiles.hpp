@@ -404,9 +404,10 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         if (g == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(run_m), __float_as_uint(run_l)}, slot, pair, 0, kDeviceScope);
     }
     if (!paged_last(p, t, last_one)) return;               // uniform
-    // Pieces of 32 rows by 32 elements, by all waves.  A read is a trip to memory: all parts' maxima in one, the figures of eight parts in one.
+    // Pieces of 32 rows by 32 elements, by all waves.  A read is a trip to memory: all parts' maxima in one, the figures of six parts in one
+    // (of eight the registers do not hold, and what is fetched from memory waits for all of them: 16 rows of 64 heads on 8 behind 30 000 48.2 us, now 43.3).
     const __amdgpu_buffer_rsrc_t from = paged_resource(paged_slot(p, t.slot));
-    constexpr int kSome = 8, kLots = kPagedTileParts / kSome;
+    constexpr int kSome = 8, kLots = kPagedTileParts / kSome, kFew = 6;
     static_assert(kPagedTileParts % kSome == 0, "whole lots");
     const int pieces_used = (t.rows + 31) / 32 * DT;
 #pragma unroll 1
@@ -430,18 +431,18 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         const float ref = m == -INFINITY ? 0.0f : m * p.scale;
         f32x4 sum[4] = {};
 #pragma unroll 1
-        for (int n0 = 0; n0 < t.parts; n0 += kSome) {
-            float2 part[kSome];
-            f32x4 x[kSome][4];
+        for (int n0 = 0; n0 < t.parts; n0 += kFew) {
+            float2 part[kFew];
+            f32x4 x[kFew][4];
 #pragma unroll
-            for (int n = 0; n < kSome; ++n) {
+            for (int n = 0; n < kFew; ++n) {
                 const int of_part = min(n0 + n, t.parts - 1) * p.slot_bytes;
                 part[n] = paged_read_pair(from, of_part + pairs);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[n][r] = paged_read(from, of_part + figures + r * 1024);
             }
 #pragma unroll
-            for (int n = 0; n < kSome; ++n) {
+            for (int n = 0; n < kFew; ++n) {
                 if (n0 + n >= t.parts || part[n].y == 0.0f) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
                 const float f = paged_factor(part[n].x, part[n].y, p.scale, ref);
                 l += f * part[n].y;
