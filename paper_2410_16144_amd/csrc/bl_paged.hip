@@ -15,7 +15,7 @@ constexpr int64_t kCounters = 1 << 14;     // of any call's: figures never lie w
 
 struct PagedPlan {
     bool    rows_form, shallow;
-    int     tile_rows, most, least, join, wanted;
+    int     tile_rows, most, wanted;
     int64_t wgs, slots, slot_bytes;
     int64_t counter_bytes, figure_bytes;
     bool launchable() const { return wgs < (1 << 24) && slots <= kCounters; }    // 2^32 threads (and every walk has a counter: 1024 key heads)
@@ -43,7 +43,6 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
         // 128, 256, 512, 1024 positions: 32 heads at 1000 positions 13.4, 14.3, 17.1, 19.0 us; 64 on 8 at 8000 23.7, 19.3, 18.7, 22.9.
         r.tile_rows = group;
         r.most = 256;
-        r.least = 256;
         r.slot_bytes = (int64_t)group * (4 + head_dim) * 4;
     } else {
         // 128 rows where nearly two such tiles come on every unit (32 heads, 1024 rows behind as many: 49.7 us, 64 rows 42.4; 1700: 70.4 and 77.3; 4096 on
@@ -54,11 +53,9 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
         // As 32, 64, 128 positions (paged_parts): 5 rows of 32 heads on 8 behind 1500 positions 13.7, 14.3, 15.4 us, behind 4000 16.7, 18.0, 19.1, behind
         // 16 000 24.8, 24.9, 26.7; 64 rows of 12 heads behind 16 000 39.4, 36.7, 35.9; 16 rows of 64 heads on 8 behind 3000 21.8, 20.1, 21.8.
         r.most = kPagedTileParts;
-        r.least = 256;
-        r.join = 64;
         r.slot_bytes = (int64_t)r.tile_rows * (ceil_div(width, 32) * 32 * 4 + 8);
     }
-    r.most = (int)std::min<int64_t>(r.most, ceil_div(max_pos, r.least));
+    r.most = (int)std::min<int64_t>(r.most, ceil_div(max_pos, kPagedLeast));
     const int64_t tiles = tiles_of(r.tile_rows), more = (single ? 1 : 2) * (int64_t)r.wanted / n_heads + 1;
     r.wgs = n_heads * std::min(tiles * r.most, tiles + more);
     r.slots = r.most > 1 ? 4 * ((int64_t)r.wanted + n_heads) : 0;
@@ -87,7 +84,7 @@ hipError_t launch_attn_paged(const ::bl_attn_paged_args& a, hipStream_t s) {
     const bool bf16 = a.dt == BL_BF16;
     const PagedPlan plan = paged_plan(p.c.n_heads, p.group, p.c.head_dim, p.c.sequences, p.c.rows, p.c.max_pos, p.c.start == nullptr, bf16);
     if (!plan.launchable()) return hipErrorInvalidConfiguration;
-    p.tile_rows = plan.tile_rows; p.most = plan.most; p.least = plan.least; p.join = plan.join; p.shallow = plan.shallow; p.slots = (int32_t)plan.slots; p.slot_bytes = (int32_t)plan.slot_bytes;
+    p.tile_rows = plan.tile_rows; p.most = plan.most; p.tile_shift = __builtin_ctz(plan.tile_rows); p.join = 64.0f; p.shallow = plan.shallow; p.slots = (int32_t)plan.slots; p.slot_bytes = (int32_t)plan.slot_bytes;
     p.target = (float)p.c.n_heads / (float)plan.wanted;
     p.counters = static_cast<uint32_t*>(a.scratch_dev);
     p.figures = reinterpret_cast<float*>(static_cast<uint8_t*>(a.scratch_dev) + plan.counter_bytes);

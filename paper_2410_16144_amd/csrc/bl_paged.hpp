@@ -295,9 +295,10 @@ __device__ __forceinline__ void paged_store(void* out, int64_t at, const f32x4& 
 //
 // A sequence's rows of one key head (tokens x query heads of the group, token by token) go by tiles; a tile's walk over the positions up to its last row's
 // may be shared by several workgroups.  How many follows on the device from all positions that the call walks: each workgroup is meant to have
-// an equal share of them, `least` at least.  The grid is an upper bound; workgroups beyond what there is to do end at once.
+// an equal share of them, kPagedLeast at least.  The grid is an upper bound; workgroups beyond what there is to do end at once.
 
 constexpr int kPagedTileParts = 32;   // workgroups that share a tile's walk at most
+constexpr int kPagedLeast = 256;      // positions that are worth a workgroup
 constexpr int kPagedFew = 16;         // rows of a sequence and key head up to which the rows form takes them
 
 struct PagedArgs {
@@ -308,10 +309,10 @@ struct PagedArgs {
     float*      figures;       // [slot]: maxima, sums and weighted values of a tile's rows, as each form has them
     int32_t     slot_bytes;
     int32_t     group;         // query heads per key head
-    int32_t     tile_rows;
+    int32_t     tile_rows;     // a power of two, or (rows form) the group
+    int32_t     tile_shift;
     int32_t     most;          // workgroups of a walk
-    int32_t     least;         // positions that are worth one
-    int32_t     join;          // positions that are walked while a part is joined; 0: nothing to speak of
+    float       join;          // tiles: positions that are walked while a part is joined
     int32_t     slots;         // of figures
     int32_t     shallow;       // tiles of 64 rows: whether two workgroups are to share a compute unit
     float       target;        // key heads / workgroups that the call is meant for
@@ -327,20 +328,25 @@ struct PagedWork {
     int slot;                  // of the walk's first part; its others' behind it
 };
 
-__device__ __forceinline__ int paged_tiles(const PagedArgs& p, int rows) { return (int)(((int64_t)rows * p.group + p.tile_rows - 1) / p.tile_rows); }
-// Parts of a walk with `per` positions each: rounded up, or, where joining a part takes as long as `p.join` positions (tiles), down and by no more than
+// (Every workgroup passes all of this once: with 64-bit divisions, a hundred instructions each, a call took 0.5 us more, one in several parts 1.)
+template <bool ROWS>
+__device__ __forceinline__ int paged_tiles(const PagedArgs& p, int rows) { return ROWS ? rows : (rows * p.group + p.tile_rows - 1) >> p.tile_shift; }   // (2^30 at most)
+// Parts of a walk with `per` positions each: rounded up, or (tiles, where joining a part takes as long as `join` positions) down and by no more than
 // makes walking (reach / parts) and joining (parts * join) the shortest together.
+template <bool ROWS>
 __device__ __forceinline__ int paged_parts(const PagedArgs& p, const PagedSequence& s, int per) {
     const int reach = s.pos + s.rows;
-    return min(p.join == 0 ? (reach - 1) / per + 1 : max(reach / max(per, (int)sqrtf((float)p.join * (float)reach)), 1), p.most);
+    return min(ROWS ? (reach - 1) / per + 1 : max(reach / max(per, (int)sqrtf(p.join * (float)reach)), 1), p.most);
 }
 
 // What the call walks of a sequence, in positions (its tiles' mean).
+template <bool ROWS>
 __device__ __forceinline__ float paged_cost(const PagedArgs& p, const PagedSequence& s) {
-    return s.rows ? (float)paged_tiles(p, s.rows) * ((float)(s.pos + s.rows) - 0.5f * (float)(s.rows - 1)) : 0.0f;
+    return s.rows ? (float)paged_tiles<ROWS>(p, s.rows) * ((float)(s.pos + s.rows) - 0.5f * (float)(s.rows - 1)) : 0.0f;
 }
 
 // By every wave for itself, a lane for every (sequences / 64) of them.  False: nothing to do.
+template <bool ROWS>
 __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWork& w) {
     const Paged& c = p.c;
     const int item = uniform((int)blockIdx.x / c.n_heads), items = uniform((int)gridDim.x / c.n_heads);
@@ -348,24 +354,24 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
     const int each = (c.sequences + 63) >> 6;
     int index = item, first_slot = 0, per;
     // (a little more than the quotient, so that there are never more parts than the grid has: see paged_plan)
-    const auto share = [&](float cost) { return __builtin_amdgcn_readfirstlane(max(p.least, (int)fminf(cost * p.target * 1.0001f, 2.0e9f) + 1)); };
+    const auto share = [&](float cost) { return __builtin_amdgcn_readfirstlane(max(kPagedLeast, (int)fminf(cost * p.target * 1.0001f, 2.0e9f) + 1)); };
     if (c.sequences == 1) {
         w.b = 0;
         w.s = paged_sequence_uniform(c, 0);
-        per = share(paged_cost(p, w.s));
+        per = share(paged_cost<ROWS>(p, w.s));
     } else {
         PagedSequence mine{0, 0, 0};
         float cost = 0.0f;
         for (int i = 0; i < each; ++i)
             if (lane * each + i < c.sequences) {
                 mine = paged_sequence(c, lane * each + i);
-                cost += paged_cost(p, mine);
+                cost += paged_cost<ROWS>(p, mine);
             }
         per = share(over_lanes<64>(cost, AddOp()));
         int sum = 0, shared = 0;
         const auto count = [&](const PagedSequence& s, int& n, int& shared_n) {
-            const int parts = s.rows ? paged_parts(p, s, per) : 0;
-            n = parts ? paged_tiles(p, s.rows) * parts : 0;
+            const int parts = s.rows ? paged_parts<ROWS>(p, s, per) : 0;
+            n = parts ? paged_tiles<ROWS>(p, s.rows) * parts : 0;
             shared_n = parts > 1 ? n : 0;
         };
         for (int i = 0; i < each; ++i)
@@ -393,8 +399,8 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
         }
     }
     if (w.s.rows == 0) return false;
-    const int tiles = uniform(paged_tiles(p, w.s.rows)), all = w.s.rows * p.group;
-    w.parts = uniform(paged_parts(p, w.s, per));
+    const int tiles = uniform(paged_tiles<ROWS>(p, w.s.rows)), all = w.s.rows * p.group;
+    w.parts = uniform(paged_parts<ROWS>(p, w.s, per));
     const int turn = uniform(index / w.parts);
     w.part = index - turn * w.parts;
     if (turn >= tiles || item - w.part + w.parts > items) return false;   // (a walk that the grid has no room for, as where sequences overlap: nobody's)
@@ -403,13 +409,19 @@ __device__ __forceinline__ bool paged_work(const PagedArgs& p, int lane, PagedWo
     w.low = w.s.pos + uniform(w.row0 / p.group);
     w.reach = w.s.pos + uniform((w.row0 + w.rows - 1) / p.group) + 1;
     w.slot = (first_slot + turn * w.parts) * c.n_heads + w.head * w.parts;
-    w.parts = min(w.parts, (w.reach + p.least - 1) / p.least);   // (a sequence's first tiles walk less than its last one)
+    w.parts = min(w.parts, (w.reach + kPagedLeast - 1) / kPagedLeast);   // (a sequence's first tiles walk less than its last one)
     if (w.part >= w.parts) return false;
     if (w.parts > 1 && (uint32_t)w.slot > (uint32_t)(p.slots - w.parts)) {   // (never, see paged_plan)
         if (w.part) return false;
         w.parts = 1;
     }
     return true;
+}
+
+// The first of a walk's chunks that part n has (there are as many chunks as parts at least).
+__device__ __forceinline__ int paged_first(const PagedWork& w, int chunks, int n) {
+    const int each = uniform(chunks / w.parts);
+    return n * each + min(n, chunks - each * w.parts);
 }
 
 __device__ __forceinline__ int64_t paged_row_at(const PagedArgs& p, const PagedWork& w, int row) {   // of q and out; row of the tile

@@ -147,10 +147,10 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     const Paged& c = p.c;
 
     PagedWork w;
-    if (!paged_work(p, lane, w)) return;
+    if (!paged_work<true>(p, lane, w)) return;
     const PagedSequence& s = w.s;
     const int reach = w.reach, chunks = (reach + 31) >> 5, head = w.head, rows = w.rows;
-    const int c0 = uniform((int)((int64_t)chunks * w.part / w.parts)), c1 = uniform((int)((int64_t)chunks * (w.part + 1) / w.parts));
+    const int c0 = paged_first(w, chunks, w.part), c1 = paged_first(w, chunks, w.part + 1);
     const int32_t* line = c.table + (int64_t)w.b * c.table_width;
 
     // ---- the rows: operand column i16

@@ -61,9 +61,9 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     const Paged& c = p.c;
 
     PagedWork t;
-    if (!paged_work(p, lane, t)) return;
+    if (!paged_work<false>(p, lane, t)) return;
     const int head = t.head, chunks = (t.reach + kPagedChunk - 1) / kPagedChunk;
-    const int c0 = uniform((int)((int64_t)chunks * t.part / t.parts)), c1 = uniform((int)((int64_t)chunks * (t.part + 1) / t.parts));
+    const int c0 = paged_first(t, chunks, t.part), c1 = paged_first(t, chunks, t.part + 1);
     const int32_t* line = c.table + (int64_t)t.b * c.table_width;
     if (tid == 0) odd_chunk = odd_sums = bad_page = 0;
     __syncthreads();
