@@ -3,7 +3,7 @@
 // Bound by the cache's bytes: 4 head_dim bytes per position and key head for at most 64 products each, a hundredth of what the matrix cores do
 // meanwhile.  So the launch is about spreading the positions of all sequences evenly over the chip and keeping enough requests under way.
 //   * Every sequence's walk is cut into equal parts of about (all positions) / (workgroups), 256 positions at least; which part a workgroup has
-//     follows from the positions on the device (paged_find), so that a captured launch serves any lengths.  The grid is an upper bound;
+//     follows from the positions on the device (paged_work), so that a captured launch serves any lengths.  The grid is an upper bound;
 //     workgroups without a part end at once.
 //   * A workgroup's four waves take its 32-position chunks in turn, each with a tile of keys and one of values of its own in LDS that it fills
 //     and waits for by itself: the next chunk's keys are requested when the scores are formed, its values when the sums are.  Streaming loads, since
