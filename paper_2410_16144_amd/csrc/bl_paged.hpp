@@ -464,9 +464,14 @@ __device__ __forceinline__ bool paged_last(const PagedArgs& p, const PagedWork& 
     return uniform(last_one) != 0;
 }
 
-// The sum of a part's, or a wave's, figures relative to `ref`: nothing of what a row has seen nothing of; NaN weights stay NaN.
+// The weight of a finite score is above zero, however small: what an infinite value is multiplied by must not be zero, or NaN comes of it, and only where
+// one part of a walk, or one order of its chunks, has it so.  (The smallest number there is: of finite values nothing comes of it that counts.)
+__device__ __forceinline__ float paged_above_zero(float x) { return x < 0x1p-149f ? 0x1p-149f : x; }   // (NaN stays)
+
+// What a part's, or a wave's, figures are multiplied by to be relative to `ref`: nothing where a row has seen nothing, or scores of -infinity alone (whose
+// sums may be NaN, and stay it); NaN weights stay NaN.
 __device__ __forceinline__ float paged_factor(float m, float l, float scale, float ref) {
-    return m == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : __builtin_amdgcn_exp2f(fmaf(m, scale, -ref));
+    return m == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : paged_above_zero(__builtin_amdgcn_exp2f(fmaf(m, scale, -ref)));
 }
 
 }  // namespace bl

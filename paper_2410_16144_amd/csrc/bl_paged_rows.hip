@@ -97,7 +97,10 @@ __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& 
         const float ref = m == -INFINITY ? 0.0f : m * p.scale;
         for (int n = lane; n < parts; n += 64) l += paged_factor(mine[n].x, mine[n].y, p.scale, ref) * mine[n].y;
         l = over_lanes<64>(l, AddOp());
-        for (int n = lane; n < parts; n += 64) mine[n].x = paged_factor(mine[n].x, mine[n].y, p.scale, ref) / l;
+        for (int n = lane; n < parts; n += 64) {
+            const float f = paged_factor(mine[n].x, mine[n].y, p.scale, ref), share = f / l;
+            mine[n].x = f == 0.0f ? share : paged_above_zero(share);
+        }
     }
     __syncthreads();
     for (int i = i0; i < total; i += kThreads) {
@@ -110,10 +113,7 @@ __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& 
                 for (int h = 0; h < kAhead; ++h) {
                     if (h % 4 == 0 && n0 + h * teams >= parts) break;
                     const int n = n0 + team + h * teams;
-                    if (n >= parts) continue;
-                    const float2 f = factor[row * parts + n];
-                    if (f.y == 0.0f && f.x == f.x) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
-                    sum += f.x * a[h];
+                    if (n < parts) sum += factor[row * parts + n].x * a[h];
                 }
             }
         if (teams > 1) {                                   // (all outputs in one turn)
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     };
 
     // Chunks that the sequence has whole, then its last one.  (The first kind's code lies side by side: jumps cost as much as products.)
-    const auto walk = [&](auto which) __attribute__((always_inline)) {
+    const auto walk = [&](auto which, bool careful) __attribute__((always_inline)) {
         constexpr bool kMasked = decltype(which)::value;
         const int j0 = 32 * chunk, next = chunk + kWaves;
         const bool bad = base.bad;                         // uniform
@@ -232,7 +232,8 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         most = over_blocks<32>(over_blocks<16>(most, MaxOp()), MaxOp());
         const float m_new = fmaxf(run_m, most);
         const float ref = m_new == -INFINITY ? 0.0f : m_new * p.scale;   // (a row that has seen nothing yet)
-        const float keep = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
+        float keep = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
+        if (kMasked && careful) keep = paged_above_zero(keep);
         run_m = m_new;
         run_l *= keep;
         uint32_t words[kWeight][4];
@@ -265,14 +266,23 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
 #pragma unroll
             for (int t = 0; t < KS; ++t) o[t] = mfma16<kWeight>(read_v(t), weights, o[t] * keep);
         } else {
-            // The end of the walk.  What lies behind the sequence's last row is nobody's (zero here); among several tokens' rows a weight of
-            // zero may stand before a value that the row does not see: infinities and NaN are counted apart, by whom they weigh with.
+            // The end of the walk: what lies behind the sequence's last row is nobody's (zero here).
             s16x8 mine;                                    // of the operand: positions that the sequence has
 #pragma unroll
             for (int r = 0; r < 8; ++r) mine[r] = j0 + (r < 4 ? 0 : 16) + 4 * g + (r & 3) < reach ? (short)-1 : (short)0;
+            s16x8 seen[1], lost[1];                        // one where the row sees the position; where its score is -infinity
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                seen[0][r] = mine[r] & (short)0x3f80;
+                lost[0][r] = x[r >> 2][r & 3] == -INFINITY ? seen[0][r] : (short)0;
+            }
 #pragma unroll
             for (int t = 0; t < KS; ++t) {
                 const s16x8 v = read_v(t) & mine;
+                if (!careful) {                            // uniform
+                    o[t] = mfma16<kWeight>(v, weights, o[t] * keep);
+                    continue;
+                }
                 s16x8 finite, up, down;
                 paged_put_away(v, finite, up, down);
                 f32x4 x_t = mfma16<kWeight>(finite, weights, o[t] * keep);
@@ -280,11 +290,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
                 const u32x4 any = __builtin_bit_cast(u32x4, either);
                 if (__any((any[0] | any[1] | any[2] | any[3]) != 0)) {
                     const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const f32x4 n_up = mfma16<kWeight>(up, weights, zero), n_down = mfma16<kWeight>(down, weights, zero);
+                    const f32x4 n_up = mfma16<1>(up, seen, zero), n_down = mfma16<1>(down, seen, zero), n_lost = mfma16<1>(either, lost, zero);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         if (n_up[r] > 0.0f) x_t[r] += INFINITY;
                         if (n_down[r] > 0.0f) x_t[r] -= INFINITY;
+                        if (n_lost[r] > 0.0f) x_t[r] = NAN;
                     }
                 }
                 o[t] = x_t;
@@ -294,21 +305,22 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         if (next < c1) req_v.send(paged_source(c.v, base), at_v);
         chunk = next;
     };
-    // The pieces of a weight times an infinity add up to NaN.  So a walk whose sums are not finite is walked again with such values put away throughout.
+    // The pieces of a weight times an infinity add up to NaN, and so does a weight that is rounded to zero.  So a walk whose sums are not finite is walked again
+    // with such values put away throughout: a value counts by who sees it, not by what is left of its weight.
     for (bool again = false;; again = true) {
         begin();
-        const bool plain = !again && chunk < c1 && 32 * chunk + 31 <= s.pos;
-        if (plain)
-            do walk(std::false_type{});
+        if (!again && chunk < c1 && 32 * chunk + 31 <= s.pos)
+            do walk(std::false_type{}, false);
             while (chunk < c1 && 32 * chunk + 31 <= s.pos);
-        while (chunk < c1) walk(std::true_type{});
-        if (!plain) break;
-        float odd = 0.0f;
+        while (chunk < c1) walk(std::true_type{}, again);
+        if (again) break;
+        f32x4 odd = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < KS; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) odd = fmaf(o[t][r], 0.0f, odd);
-        if (!__any(odd != odd)) break;
+            for (int r = 0; r < 4; ++r) odd[r] = fmaf(o[t][r], 0.0f, odd[r]);
+        const float any = (odd[0] + odd[1]) + (odd[2] + odd[3]);
+        if (!__any(any != any)) break;
     }
 
     // ---- the waves meet
@@ -336,7 +348,6 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < kWaves; ++n) {
-            if (ml[n].y == 0.0f) continue;                 // (a wave that had no chunk, or none that the row sees)
             const float f = paged_factor(ml[n].x, ml[n].y, p.scale, ref);
             l += f * ml[n].y;
             sum += f * *reinterpret_cast<const f32x4*>(meet + (n * kPagedFew + r) * L::kPitch + e);
