@@ -232,8 +232,9 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                     for (int r = 0; r < 16; ++r)
                         if (32 * n + 8 * (r >> 2) + (r & 3) > seen) x[n][r] = -INFINITY;
             }
-            if (kMasked && careful) {                      // of the keys that the row sees
+            if (kMasked && careful) {                      // of the keys that the row sees; both, which is NaN, where the score is -infinity and the weight zero
                 asm volatile("");                          // (a branch: else every chunk pays for it)
+                const int seen = limit - j1 - 4 * g;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     uint32_t up = 0, down = 0;
@@ -242,9 +243,10 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int key = 32 * (block + n) + 8 * (r >> 2) + 4 * g + (r & 3);
-                            if (x[n][r] != -INFINITY) {
-                                up |= odd_values[0][key * DT + d];
-                                down |= odd_values[1][key * DT + d];
+                            if (32 * n + 8 * (r >> 2) + (r & 3) <= seen) {
+                                const uint32_t u = odd_values[0][key * DT + d], w = odd_values[1][key * DT + d];
+                                up |= x[n][r] == -INFINITY ? u | w : u;
+                                down |= x[n][r] == -INFINITY ? u | w : w;
                             }
                             if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                         }
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             const bool moves = (most - run_m) * p.scale > 8.0f;   // (of each row for itself: no row's bits depend on another's)
             if (__builtin_expect(__any(moves), 0)) {
                 const float m_new = moves ? most : run_m;
-                const float keep = !moves ? 1.0f : run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((run_m - m_new) * p.scale);
+                const float keep = !moves ? 1.0f : run_m == -INFINITY ? 0.0f : paged_above_zero(__builtin_amdgcn_exp2f((run_m - m_new) * p.scale));
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -369,8 +371,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         if (kw == 0) {
             const float2 other = meet_ml[lane];
             const float m = fmaxf(run_m, other.x), ref = m == -INFINITY ? 0.0f : m * p.scale;
-            const float f0 = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
-            const float f1 = other.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(other.x, p.scale, -ref));
+            const float f0 = paged_factor(run_m, run_l, p.scale, ref), f1 = paged_factor(other.x, other.y, p.scale, ref);
             run_l = run_l * f0 + other.y * f1;
             run_m = m;
 #pragma unroll
@@ -443,7 +444,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             }
 #pragma unroll
             for (int n = 0; n < kFew; ++n) {
-                if (n0 + n >= t.parts || part[n].y == 0.0f) continue;   // (a part that the row sees nothing of has no share, whatever it holds)
+                if (n0 + n >= t.parts) continue;
                 const float f = paged_factor(part[n].x, part[n].y, p.scale, ref);
                 l += f * part[n].y;
 #pragma unroll

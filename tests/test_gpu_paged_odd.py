@@ -96,7 +96,7 @@ PLACES = [(300, 10, [250]), (300, 250, [10]), (300, 299, [5, 150]), (300, 3, [29
 @pytest.mark.parametrize("before,large,at", PLACES)
 @pytest.mark.parametrize("d", [48, 64, 128, 256])
 @pytest.mark.parametrize("dtype", [F, G])
-@pytest.mark.parametrize("form", ["single"])
+@pytest.mark.parametrize("form", ["single", "many heads", "packed"])
 def test_values_that_are_not_finite_beside_a_score_that_outweighs_them(dev, dec, before, large, at, d, dtype, form):
     """All weights but one underflow in 32 bits; they are above zero all the same."""
     n, group = 2, 18 if form == "many heads" else 3
@@ -113,7 +113,7 @@ def test_values_that_are_not_finite_beside_a_score_that_outweighs_them(dev, dec,
 
 
 @pytest.mark.parametrize("dtype", [F, G])
-@pytest.mark.parametrize("form", ["single"])
+@pytest.mark.parametrize("form", ["single", "packed"])
 @pytest.mark.parametrize("company", [[], [9000], [4000, 100, 2000, 700, 5000, 3000, 1]])
 def test_what_is_not_finite_does_not_depend_on_how_walks_are_cut(dev, dec, dtype, form, company):
     """The same sequence alone and beside others, whose lengths decide how many workgroups share its walk."""
@@ -127,7 +127,7 @@ def test_what_is_not_finite_does_not_depend_on_how_walks_are_cut(dev, dec, dtype
     assert (want[0, :, 3] == INF).all() and want[0, :, 4:6].isnan().all() and torch.isfinite(want[0, :, :3]).all()
 
 
-@pytest.mark.parametrize("before,new,at", [(300, 1, 100), (300, 1, 300), (6000, 1, 3000)])
+@pytest.mark.parametrize("before,new,at", [(300, 1, 100), (300, 1, 300), (6000, 1, 3000), (300, 4, 100), (300, 4, 302), (100, 70, 120), (2000, 66, 2010)])
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("dtype", [G])
 def test_an_infinite_value_of_a_weight_of_zero(dev, dec, before, new, at, d, dtype):
@@ -140,3 +140,17 @@ def test_an_infinite_value_of_a_weight_of_zero(dev, dec, before, new, at, d, dty
     out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, dtype, new == 1, 4)
     want = check(out, qd, srv.k[0], srv.v[0], 4, seen, dtype)
     assert want[-1, :4, 7:10].isnan().all() and torch.isfinite(want[-1, :4, :7]).all() and torch.isfinite(want[-1, 4:]).all()
+
+
+@pytest.mark.parametrize("extra", [0, 2200, 7000])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("before,new", [(0, 65), (100, 40), (500, 130)])
+def test_values_and_large_scores_in_every_form_of_the_tiles(dev, dec, d, before, new, extra):
+    """A row's largest score is a late one; before it and behind it values that are not finite, some of which only later rows see."""
+    srv, k, v = _sequence(dec, dev, d, before, new, seed=4)
+    k[before + new // 2] = 8.0
+    for i, p in enumerate((0, before + new // 4, before + new // 2 + 3, before + new - 1)):
+        v[p, :, i], v[p, :, d - 1 - i], v[p, 0, 30 + i], v[p, 1, 25] = INF, -INF, NAN, INF if i % 2 else -INF
+    q = torch.full((new, 6, d), 8.0)
+    out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, G, False, 3, extra)
+    check(out, qd, srv.k[0], srv.v[0], 3, seen, G)
