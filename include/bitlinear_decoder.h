@@ -508,7 +508,9 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32 (sums of values by weights of up to 2^8, divided at the end: values
  * within a walk's length of fp32's largest may overflow).  How a walk is cut, and so the order of sums, follows from all sequences of the call: a row's
  * bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
- * that is not finite makes of the rows that see it what the formula does.  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
+ * that is not finite makes of the rows that see it what the formula does: a score of NaN or +infinity, or scores of -infinity alone, make the row NaN; the
+ * weight of a finite score is above zero, however small, that of -infinity is zero, and zero times an infinite value is NaN.  (fp32 queries: an element
+ * below 2^-96 in size makes NaN of an infinite key.)  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
  * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
  * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,
  *         BL_ERR_HIP.

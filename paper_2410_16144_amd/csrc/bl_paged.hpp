@@ -227,6 +227,18 @@ __device__ __forceinline__ void paged_split(float a, float b, uint32_t (&out)[PI
     }
 }
 
+// A query's three pieces before a key that is infinite: pieces of zero would make NaN of it, where the element itself makes an infinity.  So the lower two
+// are 2^-126 at least, with the element's sign, where the element is 2^-96 or more (what that adds, 2^-29 of a product at most, its rounding takes away).
+__device__ __forceinline__ void paged_no_zero(uint32_t (&pieces)[3]) {   // of two elements
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const auto halves = [](uint32_t x) { return __builtin_bit_cast(u16x2, x & 0x7fff7fffu); };
+    const u16x2 from = {0x0f00, 0x0f00}, most = {0x0080, 0x0080};   // bf16's 2^-97, 2^-126
+    const u16x2 least = __builtin_elementwise_min(__builtin_elementwise_sub_sat(halves(pieces[0]), from), most);
+#pragma unroll
+    for (int i = 1; i < 3; ++i)
+        pieces[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(halves(pieces[i]), least)) | (pieces[0] & 0x80008000u);
+}
+
 // Eight elements e .. e + 7 of a row's query (zeros from head_dim on and in rows that are not there, whose row_at is another's; head_dim is a multiple of
 // four, e of eight) as operand pieces.  fp32 is loaded by every lane: in a branch, each load would be waited for by its cutting into pieces (12 heads of 64 at
 // position 17: 7.2 us, so 6.7); bf16 has nothing to cut, and idle lanes' loads would cost it 0.3 us.
@@ -250,6 +262,7 @@ __device__ __forceinline__ void paged_query(const void* q, int64_t row_at, int e
             for (int j = 0; j < 2; ++j) {
                 uint32_t two[PIECES];
                 paged_split<PIECES>(in ? x[2 * j] : 0.0f, in ? x[2 * j + 1] : 0.0f, two);
+                paged_no_zero(two);
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) parts[i][2 * h + j] = two[i];
             }

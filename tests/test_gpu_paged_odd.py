@@ -47,8 +47,8 @@ def check(out, q, k, v, group, seen, dtype):
     T, heads, d = q.shape
     got = out.double().cpu().view(T, heads, d)
     want, plain, S, V = formula(q, k, v, group, seen)
-    assert torch.equal(got.isnan(), want.isnan())
-    assert torch.equal(got[want.isinf()], want[want.isinf()])
+    wrong = int((got.isnan() != want.isnan()).sum()), int((got[want.isinf()] != want[want.isinf()]).sum())
+    assert wrong == (0, 0), "outputs that are NaN or not, of infinities, against the formula"
     finite = torch.isfinite(want)
     ok = ~plain.isnan().any(-1)                                          # (rows of NaN have no tolerance)
     if ok.any():
@@ -127,9 +127,36 @@ def test_what_is_not_finite_does_not_depend_on_how_walks_are_cut(dev, dec, dtype
     assert (want[0, :, 3] == INF).all() and want[0, :, 4:6].isnan().all() and torch.isfinite(want[0, :, :3]).all()
 
 
+# A key's infinities make scores of both signs, or NaN where the query has a zero; +infinity makes its rows NaN.
+@pytest.mark.parametrize("before,new,at", [(300, 1, [100]), (300, 1, [300]), (40, 1, [0, 39]), (0, 1, [0]), (6000, 1, [3000]), (300, 4, [100, 301]), (100, 70, [120]), (6000, 3, [64]),
+                                           (0, 5, [2]), (0, 130, [70])])
+@pytest.mark.parametrize("d", [48, 64, 128, 256])
+@pytest.mark.parametrize("dtype", [F, G])
+@pytest.mark.parametrize("values", ["short", "full", "tiny"])
+def test_keys_that_are_not_finite(dev, dec, before, new, at, d, dtype, values):
+    """Head 0 meets -infinity, head 1 +infinity, head 2 zero times infinity, head 3 infinities of both signs, head 4 does not meet it (its key head has none)."""
+    srv, k, v = _sequence(dec, dev, d, before, new, seed=1)
+    k[at, 0, 5] = INF
+    k[at, 0, 9] = -INF
+    v[at[0], 0, 7] = 3.0
+    size = {"short": 1.0, "full": 1.0 + 2.0 ** -12 + 2.0 ** -20, "tiny": 2.0 ** -90}[values]
+    q = torch.randn((new, 8, d), generator=srv.g).to(G).float() * size
+    q[..., 5], q[..., 9] = size, 0.5 * size                              # inf and -inf: NaN
+    q[:, 0, 5], q[:, 0, 9] = -size, size                                 # -inf twice
+    q[:, 1, 5], q[:, 1, 9] = size, -size                                 # +inf twice
+    q[:, 2, 5], q[:, 2, 9] = 0.0, size
+    q[:, 3] = size
+    out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, dtype, new == 1, 4)
+    if dtype == G:
+        assert torch.equal(qd, q.to(G).double())
+    want = check(out, qd, srv.k[0], srv.v[0], 4, seen, dtype)
+    last = want[-1]
+    assert last[1:4].isnan().all() and torch.isfinite(last[4:]).all() and (torch.isfinite(last[0]).all() or before + new == len(at))
+
+
 @pytest.mark.parametrize("before,new,at", [(300, 1, 100), (300, 1, 300), (6000, 1, 3000), (300, 4, 100), (300, 4, 302), (100, 70, 120), (2000, 66, 2010)])
 @pytest.mark.parametrize("d", [64, 128, 256])
-@pytest.mark.parametrize("dtype", [G])
+@pytest.mark.parametrize("dtype", [F, G])
 def test_an_infinite_value_of_a_weight_of_zero(dev, dec, before, new, at, d, dtype):
     """A score of -infinity is a weight of zero: zero times an infinite value is NaN, of a finite one nothing."""
     srv, k, v = _sequence(dec, dev, d, before, new, seed=2)
@@ -140,6 +167,20 @@ def test_an_infinite_value_of_a_weight_of_zero(dev, dec, before, new, at, d, dty
     out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, dtype, new == 1, 4)
     want = check(out, qd, srv.k[0], srv.v[0], 4, seen, dtype)
     assert want[-1, :4, 7:10].isnan().all() and torch.isfinite(want[-1, :4, :7]).all() and torch.isfinite(want[-1, 4:]).all()
+
+
+@pytest.mark.parametrize("before,new", [(300, 1), (5000, 1), (300, 40), (0, 3)])
+@pytest.mark.parametrize("dtype", [F, G])
+def test_rows_that_see_scores_of_minus_infinity_alone(dev, dec, before, new, dtype):
+    """NaN: there is no largest score to be relative to.  The other key head's rows are untouched."""
+    d = 64
+    srv, k, v = _sequence(dec, dev, d, before, new, seed=3)
+    k[:, 0, 5] = INF
+    q = torch.randn((new, 6, d), generator=srv.g).to(G).float()
+    q[..., 5] = -1.0
+    out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, dtype, new == 1, 3)
+    want = check(out, qd, srv.k[0], srv.v[0], 3, seen, dtype)
+    assert want[:, :3].isnan().all() and torch.isfinite(want[:, 3:]).all()
 
 
 @pytest.mark.parametrize("extra", [0, 2200, 7000])
