@@ -481,10 +481,10 @@ __device__ __forceinline__ bool paged_last(const PagedArgs& p, const PagedWork& 
 // one part of a walk, or one order of its chunks, has it so.  (The smallest number there is: of finite values nothing comes of it that counts.)
 __device__ __forceinline__ float paged_above_zero(float x) { return x < 0x1p-149f ? 0x1p-149f : x; }   // (NaN stays)
 
-// What a part's, or a wave's, figures are multiplied by to be relative to `ref`: nothing where a row has seen nothing, or scores of -infinity alone (whose
-// sums may be NaN, and stay it); NaN weights stay NaN.
-__device__ __forceinline__ float paged_factor(float m, float l, float scale, float ref) {
-    return m == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : paged_above_zero(__builtin_amdgcn_exp2f(fmaf(m, scale, -ref)));
+// What a part's, or a wave's, figures are multiplied by to be relative to the maximum `top`: nothing where a row has seen nothing, or scores of -infinity alone
+// (whose sums may be NaN, and stay it); NaN weights stay NaN.
+__device__ __forceinline__ float paged_factor(float m, float l, float scale, float top) {
+    return m == -INFINITY ? (l == 0.0f ? 0.0f : NAN) : paged_above_zero(__builtin_amdgcn_exp2f((m - top) * scale));
 }
 
 }  // namespace bl

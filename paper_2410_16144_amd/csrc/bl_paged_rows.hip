@@ -94,11 +94,10 @@ __device__ __forceinline__ void join_parts(const PagedArgs& p, const PagedWork& 
         float m = -INFINITY, l = 0.0f;
         for (int n = lane; n < parts; n += 64) m = fmaxf(m, mine[n].x);
         m = over_lanes<64>(m, MaxOp());
-        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
-        for (int n = lane; n < parts; n += 64) l += paged_factor(mine[n].x, mine[n].y, p.scale, ref) * mine[n].y;
+        for (int n = lane; n < parts; n += 64) l += paged_factor(mine[n].x, mine[n].y, p.scale, m) * mine[n].y;
         l = over_lanes<64>(l, AddOp());
         for (int n = lane; n < parts; n += 64) {
-            const float f = paged_factor(mine[n].x, mine[n].y, p.scale, ref), share = f / l;
+            const float f = paged_factor(mine[n].x, mine[n].y, p.scale, m), share = f / l;
             mine[n].x = f == 0.0f ? share : paged_above_zero(share);
         }
     }
@@ -231,8 +230,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         float most = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])), fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
         most = over_blocks<32>(over_blocks<16>(most, MaxOp()), MaxOp());
         const float m_new = fmaxf(run_m, most);
-        const float ref = m_new == -INFINITY ? 0.0f : m_new * p.scale;   // (a row that has seen nothing yet)
-        float keep = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fmaf(run_m, p.scale, -ref));
+        // (The difference first: a maximum of 2^31 or more, rounded after its product with the scale, makes exponents beyond fp32's of its own weight.)
+        const float top = m_new == -INFINITY ? 0.0f : m_new;             // (a row that has seen nothing yet)
+        float keep = run_m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((run_m - top) * p.scale);
         if (kMasked && careful) keep = paged_above_zero(keep);
         run_m = m_new;
         run_l *= keep;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int r = 0; r < 4; r += 2) {
-                const float u = __builtin_amdgcn_exp2f(fmaf(x[h][r], p.scale, -ref)), v = __builtin_amdgcn_exp2f(fmaf(x[h][r + 1], p.scale, -ref));
+                const float u = __builtin_amdgcn_exp2f((x[h][r] - top) * p.scale), v = __builtin_amdgcn_exp2f((x[h][r + 1] - top) * p.scale);
                 run_l += u;
                 run_l += v;
                 uint32_t two[kWeight];
@@ -344,11 +344,10 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
             ml[n] = meet_ml[n * kPagedFew + r];
             m = fmaxf(m, ml[n].x);
         }
-        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int n = 0; n < kWaves; ++n) {
-            const float f = paged_factor(ml[n].x, ml[n].y, p.scale, ref);
+            const float f = paged_factor(ml[n].x, ml[n].y, p.scale, m);
             l += f * ml[n].y;
             sum += f * *reinterpret_cast<const f32x4*>(meet + (n * kPagedFew + r) * L::kPitch + e);
         }

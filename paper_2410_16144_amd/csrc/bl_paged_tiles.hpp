@@ -26,6 +26,7 @@
 namespace bl {
 
 constexpr int kPagedChunk = 64;
+constexpr float kPagedLargeScore = 1024.0f;   // exponents of two: up to here a maximum's rounding is 2^-14 of one at most
 
 template <int PIECES>
 __device__ __forceinline__ f32x16 paged_mfma32(const s16x8& a, const s16x8 (&b)[PIECES], f32x16 c) {
@@ -147,7 +148,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     // Chunks that every row of the tile sees whole, then those that end among the rows' own positions.  (The first kind's code lies side by side: a jump
     // costs as much as two products.)
     // `sure`: chunks whose request, kDepth - 1 chunks on, is there to be made, so that it is known how many requests are behind the chunk's own.
-    const auto walk = [&](int chunk, auto which, auto sure) __attribute__((always_inline)) {
+    // `again`: of the second kind, a walk that was not right the first time (below).
+    const auto walk = [&](int chunk, auto which, auto sure, bool again) __attribute__((always_inline)) {
         constexpr bool kMasked = decltype(which)::value, kSure = decltype(sure)::value;
         const int j0 = chunk * kPagedChunk;
         const uint8_t* ring = lds + (chunk & (kDepth - 1)) * (4 * T::kBytes);
@@ -271,13 +273,16 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 run_l *= keep;
                 run_m = m_new;
             }
-            const float ref = run_m == -INFINITY ? 0.0f : run_m * p.scale;   // (a row that has seen nothing yet)
+            float ref = run_m == -INFINITY ? 0.0f : run_m * p.scale;         // (a row that has seen nothing yet)
+            const float off = kMasked && again && fabsf(ref) > kPagedLargeScore ? run_m : 0.0f;
+            if (kMasked && off != 0.0f) ref = 0.0f;
+            const auto exponent = [&](float score) { return fmaf(kMasked ? score - off : score, p.scale, -ref); };
             const auto weights = [&](int n, s16x8 (&w)[PIECES]) __attribute__((always_inline)) {   // of 16 keys
                 uint32_t words[PIECES][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float a = __builtin_amdgcn_exp2f(fmaf(x[n >> 1][8 * (n & 1) + 2 * j], p.scale, -ref));
-                    const float b = __builtin_amdgcn_exp2f(fmaf(x[n >> 1][8 * (n & 1) + 2 * j + 1], p.scale, -ref));
+                    const float a = __builtin_amdgcn_exp2f(exponent(x[n >> 1][8 * (n & 1) + 2 * j]));
+                    const float b = __builtin_amdgcn_exp2f(exponent(x[n >> 1][8 * (n & 1) + 2 * j + 1]));
                     uint32_t two[PIECES];
                     paged_split<PIECES>(a, b, two);
                     // (a sum of the weights that the values are multiplied by: where one weight outweighs the others, its rounding cancels)
@@ -326,8 +331,10 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         }
     };
     // A weight's pieces times an infinity add up to NaN, as a weight of zero does.  So a walk whose sums are not finite is walked again with such values put
-    // away throughout.
-    for (int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);; plain = c0) {
+    // away throughout.  So is one with a large maximum, whose product with the scale is rounded by as much as exponents count (from 2^31 on beyond fp32's
+    // largest): there, row by row, the difference is formed first.  (In every chunk of the first walk that costs 2 % of a long prompt.)
+    bool again = false;
+    for (int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);; plain = c0, again = true) {
 #pragma unroll
         for (int i = 0; i < kDepth - 1; ++i) {
             prepare_if(c0 + i);
@@ -340,19 +347,23 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
         int chunk = c0;
-        for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{});
-        for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{});
-        for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{});
-        if (plain > c0) {
-            float odd = 0.0f;
+        for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{}, false);
+        for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{}, false);
+        for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{}, again);
+        if (!again) {
+            bool odd = run_m != -INFINITY && fabsf(run_m * p.scale) > kPagedLargeScore;
+            if (plain > c0) {
+                float sums = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) odd = fmaf(o[d][r], 0.0f, odd);
-            if (odd != odd) odd_sums = 1;
+                    for (int r = 0; r < 16; ++r) sums = fmaf(o[d][r], 0.0f, sums);
+                odd = odd || sums != sums;
+            }
+            if (odd) odd_sums = 1;
         }
         __syncthreads();
-        if (plain == c0 || !uniform(odd_sums)) break;
+        if (again || !uniform(odd_sums)) break;
         look(c0);
     }
     run_l = over_blocks<32>(run_l, AddOp());
@@ -370,8 +381,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         __syncthreads();
         if (kw == 0) {
             const float2 other = meet_ml[lane];
-            const float m = fmaxf(run_m, other.x), ref = m == -INFINITY ? 0.0f : m * p.scale;
-            const float f0 = paged_factor(run_m, run_l, p.scale, ref), f1 = paged_factor(other.x, other.y, p.scale, ref);
+            const float m = fmaxf(run_m, other.x);
+            const float f0 = paged_factor(run_m, run_l, p.scale, m), f1 = paged_factor(other.x, other.y, p.scale, m);
             run_l = run_l * f0 + other.y * f1;
             run_m = m;
 #pragma unroll
@@ -429,7 +440,6 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
                 for (int n = b * kSome; n < (b + 1) * kSome; ++n) m = fmaxf(m, ml[n].x);
             }
-        const float ref = m == -INFINITY ? 0.0f : m * p.scale;
         f32x4 sum[4] = {};
 #pragma unroll 1
         for (int n0 = 0; n0 < t.parts; n0 += kFew) {
@@ -445,7 +455,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
             for (int n = 0; n < kFew; ++n) {
                 if (n0 + n >= t.parts) continue;
-                const float f = paged_factor(part[n].x, part[n].y, p.scale, ref);
+                const float f = paged_factor(part[n].x, part[n].y, p.scale, m);
                 l += f * part[n].y;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[r] += f * x[n][r];

@@ -10,7 +10,7 @@ import math
 
 import pytest
 
-from test_gpu_paged import F, G, Server, _close, _gen, dec, dev   # noqa: F401 (fixtures)
+from test_gpu_paged import F, G, H, U, Server, _close, _gen, dec, dev   # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -195,3 +195,25 @@ def test_values_and_large_scores_in_every_form_of_the_tiles(dev, dec, d, before,
     q = torch.full((new, 6, d), 8.0)
     out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, G, False, 3, extra)
     check(out, qd, srv.k[0], srv.v[0], 3, seen, G)
+
+
+@pytest.mark.parametrize("power", [8, 20, 29, 31, 40, 70, 110])
+@pytest.mark.parametrize("heads,d,before,new", [(4, 64, 300, 1), (4, 128, 6000, 1), (4, 256, 40, 1), (36, 64, 300, 1), (4, 48, 300, 70), (4, 128, 6000, 3), (4, 256, 130, 40), (4, 64, 0, 1)])
+@pytest.mark.parametrize("dtype", [F, G])
+def test_scores_of_any_size(dev, dec, power, heads, d, before, new, dtype):
+    """Queries of +-2^power and keys of small whole numbers: scores are exact in every order of their sums, and those below the largest by a step or more weigh less than
+    exp(-2^8 / 16).  What is left are sums of equal weights: divisions and sums, 40 u of the largest value, and bf16's roundings of weights and outputs.  In the tiles
+    a maximum below 2^10 (in exponents of two) is rounded, by 2^-15 at most; weights relative to two such ones are off by 2^-14 ln 2, outputs by twice that."""
+    srv, k, v = _sequence(dec, dev, d, before, new, seed=5)
+    k = torch.randint(-3, 4, k.shape, generator=srv.g).to(G)
+    if before > 100:
+        k[before - 60], k[70] = k[3], k[3]                               # (equal scores far apart)
+    q = (torch.randint(0, 2, (new, heads, d), generator=srv.g) * 2 - 1) * 2.0 ** power
+    q[..., 0, :] = torch.where(k[min(3, before), 0] < 0, -1.0, 1.0) * 2.0 ** power
+    out, qd, seen = _attend(dec, dev, srv, q, k, v, before, new, dtype, new == 1, heads // 2)
+    want, plain, S, V = formula(qd, srv.k[0], srv.v[0], heads // 2, seen)
+    got = out.double().cpu().view_as(want)
+    assert torch.isfinite(got).all()
+    worst = ((got - want).abs().amax(-1) / V).max().item()
+    tiles = new > 1 or heads // 2 > 16
+    assert worst <= (2 * H if dtype == G else 0) + 40 * U + (2.0 ** -13 if tiles and power == 8 else 0)
