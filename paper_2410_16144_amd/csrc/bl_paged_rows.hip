@@ -153,10 +153,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
     const int32_t* line = c.table + (int64_t)w.b * c.table_width;
 
     // ---- the rows: operand column i16
-    const int token = i16 / p.group;
     const bool there = i16 < rows;
     const int64_t row_at = there ? paged_row_at(p, w, i16) : 0;
-    const int limit = s.pos + token;                       // the last position that the row sees
+    const int limit = reach - 1;                           // the last position that is seen, by columns without a row too: what lies behind it is no reason to walk again
     s16x8 q[kSteps][PIECES];
 #pragma unroll
     for (int t = 0; t < kSteps; ++t) paged_query<PIECES>(p.q, row_at, 32 * t + 8 * g, c.head_dim, there, q[t]);

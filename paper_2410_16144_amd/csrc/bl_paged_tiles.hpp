@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     // the wave's rows: operand column l32
     const int row = rw * 32 + l32;                         // of the tile
     const bool there = row < t.rows;
-    const int limit = t.s.pos + (t.row0 + row) / p.group;  // the last position that the row sees
+    // The last position that the row sees.  (A column without a row sees what the last row sees: what lies behind that is no reason to walk again.)
+    const int limit = min(t.s.pos + (t.row0 + row) / p.group, t.reach - 1);
     const int wave_low = t.s.pos + uniform((t.row0 + rw * 32) / p.group);
     const int wave_high = rw * 32 < t.rows ? t.s.pos + uniform((t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group) : -1;
     s16x8 q[KS][PIECES];
@@ -157,12 +158,16 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
         __syncthreads();                                   // the chunk is here, and nobody reads the one before it any more
         if constexpr (kSure) prepare(chunk + kDepth - 1);
         else prepare_if(chunk + kDepth - 1);
-        // Weights of zero may stand before values that a row does not see; infinities and NaN among those are put away and noted.
+        // Weights of zero may stand before values that a row does not see; infinities and NaN among those are put away and noted.  What lies behind the
+        // sequence's last row is nobody's: zero.
         bool careful = false;
         if constexpr (kMasked) {
             uint8_t* values = lds + (ring - lds) + 2 * T::kBytes;
             uint32_t most = 0;
-            for (int i = tid * 16; i < 2 * T::kBytes; i += 256 * 16) {
+            const int end = min(kPagedChunk, t.reach - j0) * T::kRow;
+#pragma unroll 1
+            for (int i = end + tid * 16; i < 2 * T::kBytes; i += 256 * 16) *reinterpret_cast<u32x4*>(values + i) = u32x4{0, 0, 0, 0};
+            for (int i = tid * 16; i < end; i += 256 * 16) {
                 const u32x4 x = *reinterpret_cast<const u32x4*>(values + i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = paged_exponents(most, x[j]);

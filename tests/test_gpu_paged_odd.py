@@ -217,3 +217,35 @@ def test_scores_of_any_size(dev, dec, power, heads, d, before, new, dtype):
     worst = ((got - want).abs().amax(-1) / V).max().item()
     tiles = new > 1 or heads // 2 > 16
     assert worst <= (2 * H if dtype == G else 0) + 40 * U + (2.0 ** -13 if tiles and power == 8 else 0)
+
+
+@pytest.mark.parametrize("heads,new,before", [(4, 1, 60000), (2, 9, 20000), (34, 1, 20000)])
+@pytest.mark.parametrize("dtype", [F, G])
+def test_what_nobody_wrote_costs_nothing(dev, dec, heads, new, before, dtype):
+    """Columns of an operand that have no row do not see what lies behind the last position: a walk is not repeated because of it.  (It took twice as long.)"""
+    d = 128
+    srv, k, v = _sequence(dec, dev, d, before, new, page=64, seed=6)
+    srv.put(0, k, v)
+    q = (torch.randn((new, heads * d), generator=srv.g)).to(dtype).to(dev)
+    rows = srv.rows(dec, [before], [new], new == 1)
+    scratch = dec.paged_scratch(heads, srv.cache, rows)
+    last, inside = int(srv.lines[0, (before + new - 1) // 64]), (before + new - 1) % 64 + 1
+    assert inside % 32                                                   # the last chunk ends inside a page
+
+    def time(fill):
+        for pool in (srv.cache.k, srv.cache.v):
+            pool[last, :, inside:] = fill
+        best = math.inf
+        for _ in range(15):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(20):
+                out = dec.attn_paged(q, srv.cache, rows, scratch)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best, out
+    time(0.0)
+    (zeros, a), (nans, b) = time(0.0), time(NAN)
+    assert torch.equal(a, b)
+    assert nans <= 1.2 * zeros, (nans, zeros)
