@@ -318,7 +318,8 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (kMasked && careful) {                      // (lane and lane + 32 have the row's keys between them)
-                asm volatile("");
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (each has read nothing yet of what the other wrote)
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const uint32_t up = (odd_seen[2 * d][tid] | odd_seen[2 * d][tid ^ 32]) >> 4 * g, down = (odd_seen[2 * d + 1][tid] | odd_seen[2 * d + 1][tid ^ 32]) >> 4 * g;
