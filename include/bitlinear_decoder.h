@@ -451,7 +451,9 @@ int32_t bl_paged_width(int32_t head_dim);
  *   max_pos     no position of the call is max_pos or beyond; 1 <= max_pos <= table_width * page_size, max_pos <= BL_PAGED_MAX_POS
  * All four are read on the device, so a captured launch serves other lengths, pages and numbers of rows up to `rows`.  What they say is looked at
  * before it is used: a sequence with a negative position, with positions from max_pos on, or with rows outside 0 .. rows - 1 takes no part, its
- * rows of the outputs stay as they are, like rows that no sequence has.  Two sequences may share pages that nobody writes in the call.
+ * rows of the outputs stay as they are, like rows that no sequence has.  Where starts fall all the same, the others' rows are right: those that two
+ * sequences claim are one's or the other's, and if the sequences claim more rows in all than the call has, some may stay as they are.  Two sequences may
+ * share pages that nobody writes in the call.
  */
 typedef struct bl_paged_rows {
     const int32_t *table_dev;

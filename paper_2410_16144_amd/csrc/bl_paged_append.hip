@@ -53,15 +53,43 @@ __device__ __forceinline__ void append_store(void* to, int64_t at, const float (
     }
 }
 
-// The sequence that row t belongs to: as many as end at t or before.  (Uniform t.)
-__device__ __forceinline__ int sequence_of(const Paged& c, int t, int lane) {
-    if (!c.start) return t;
-    if (c.sequences == 1) return 0;
+// The sequence that row t belongs to; no rows if none has it.  (Uniform t.)  Where starts rise, as many end at t or before.  Starts that fall hide nobody's
+// rows but their own: where that one does not have the row, everyone is asked (with up to 64 sequences nobody need be if all end at t or before).
+__device__ __forceinline__ PagedSequence sequence_of(const Paged& c, int t, int lane, int& of) {
+    const auto has = [&](const PagedSequence& s) { return t >= s.first && t < s.first + s.rows; };
+    of = c.start ? 0 : t;
+    if (!c.start || c.sequences == 1) return paged_sequence_uniform(c, of);
     const int each = (c.sequences + 63) >> 6;              // at most 16
     int b = 0;
     if (each > 1) b = each * __popcll(__ballot(c.start[min((lane + 1) * each, c.sequences)] <= t));
     const int i = b + lane;
-    return b + __popcll(__ballot((each == 1 || lane < each) && i < c.sequences && c.start[min(i, c.sequences - 1) + 1] <= t));
+    of = uniform(b + __popcll(__ballot((each == 1 || lane < each) && i < c.sequences && c.start[min(i, c.sequences - 1) + 1] <= t)));
+    if (of < c.sequences) {
+        const PagedSequence s = paged_sequence_uniform(c, of);
+        if (has(s)) return s;
+    } else if (each == 1) {
+        return {0, 0, 0};
+    }
+#pragma unroll 1
+    for (int from = 0; from < c.sequences; from += 256) {
+        bool mine[4];                                      // (the loads of 256 travel together)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int n = from + 64 * u + lane, at = min(n, c.sequences - 1);
+            const int first = c.start[at], end = c.start[at + 1];
+            mine[u] = (n < c.sequences) & (t >= first) & (t < end);
+        }
+        if (!__any(mine[0] || mine[1] || mine[2] || mine[3])) continue;
+#pragma unroll 1
+        for (int n = from; n < min(from + 256, c.sequences); ++n) {
+            const PagedSequence s = paged_sequence_uniform(c, n);
+            if (has(s)) {
+                of = n;
+                return s;
+            }
+        }
+    }
+    return {0, 0, 0};
 }
 
 // L lanes have a head, NV times V elements and their partners each (V divides half the head size, NV V L reaches it).  bf16 by 16 bytes a lane: 2000 rows
@@ -93,9 +121,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs p) {
         a[n] = *reinterpret_cast<const vec_t*>(src + e);
         b[n] = *reinterpret_cast<const vec_t*>(src + half + e);
     }
-    const int of = uniform(sequence_of(c, t, lane));
-    if (of >= c.sequences) return;
-    const PagedSequence s = paged_sequence_uniform(c, of);
+    int of;
+    const PagedSequence s = sequence_of(c, t, lane, of);
     if (t < s.first || t >= s.first + s.rows) return;
     const int at = s.pos + t - s.first;
     const int page = uniform(scalar_word(c.table, (int64_t)of * c.table_width + (at >> c.page_shift)));
