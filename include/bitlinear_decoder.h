@@ -472,7 +472,8 @@ typedef struct bl_paged_rows {
  *   (y[i], y[i + head_dim/2]) rotated by the table's row of the token's position, as bl_attn_decode rotates (without a table: as they are)
  *   q_dev        [rows, ld_q >= n_q_heads * head_dim], k_dev [rows, ld_k], v_dev [rows, ld_v >= n_heads * head_dim], fp32 or bf16 (dt), aligned
  *                to the element
- *   q_out_dev    [rows, n_q_heads * head_dim] fp32 or bf16 (q_out_dt), 16-byte aligned; must not overlap the inputs or the pages
+ *   q_out_dev    [rows, n_q_heads * head_dim] fp32 or bf16 (q_out_dt), 16-byte aligned; must not overlap the inputs or the pages, nor keys' pages values',
+ *                nor pages the table, positions, starts, norms or angles (BL_ERR_SHAPE)
  *   gamma_q_dev, gamma_k_dev   [head_dim] fp32, either may be NULL
  *   rope_table_dev   the table of bl_rope_table, max_pos rows or more; may be NULL
  * A position whose page number is outside 0 .. pages - 1 is not stored.
@@ -505,7 +506,8 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  * pieces of prompts and any mixture; without start_dev it is made for single tokens.
  *   q_dev, out_dev  [rows, n_q_heads * head_dim] fp32 or bf16 (dt, both the same), 8-byte aligned; out_dev overlaps nothing else of the call
  *   scratch_dev     bl_attn_paged_scratch_bytes(...) bytes, 256-byte aligned, ZERO-FILLED before the first call; every call leaves it usable for
- *                   any other call with no greater need.  Calls that may overlap in time must not share it.
+ *                   any other call with no greater need.  Calls that may overlap in time must not share it.  It overlaps nothing else of the call
+ *                   (BL_ERR_SHAPE, as for out_dev).
  * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with weights as
  * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32 (sums of values by weights of up to 2^8, divided at the end: values
  * within a walk's length of fp32's largest may overflow).  How a walk is cut, and so the order of sums, follows from all sequences of the call: a row's

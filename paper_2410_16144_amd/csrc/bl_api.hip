@@ -720,9 +720,16 @@ static bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_b
     return x < y + b_bytes && y < x + a_bytes;
 }
 
+static uint64_t pool_bytes(const bl_paged_cache* c) { return (uint64_t)c->pages * c->n_heads * c->page_size * bl_paged_width(c->head_dim) * 2; }
+
 static bool overlaps_pages(const bl_paged_cache* c, const void* out, uint64_t bytes) {
-    const uint64_t pool = (uint64_t)c->pages * c->n_heads * c->page_size * bl_paged_width(c->head_dim) * 2;
-    return overlap(c->k_pages_dev, pool, out, bytes) || overlap(c->v_pages_dev, pool, out, bytes);
+    return overlap(c->k_pages_dev, pool_bytes(c), out, bytes) || overlap(c->v_pages_dev, pool_bytes(c), out, bytes);
+}
+
+// Whether what a launch writes lies over the description that it reads.
+static bool overlaps_rows(const bl_paged_rows* r, const void* out, uint64_t bytes) {
+    return overlap(r->table_dev, (uint64_t)r->sequences * r->table_width * 4, out, bytes) || overlap(r->pos_dev, (uint64_t)r->sequences * 4, out, bytes) ||
+           (r->start_dev && overlap(r->start_dev, (uint64_t)(r->sequences + 1) * 4, out, bytes));
 }
 
 bl_status bl_paged_append(const bl_paged_append_args* a, void* stream) {
@@ -740,6 +747,14 @@ bl_status bl_paged_append(const bl_paged_append_args* a, void* stream) {
     }
     if (overlaps_pages(a->cache, a->q_out_dev, out_bytes)) return BL_ERR_SHAPE;
     if (!aligned(a->q_out_dev, 16) || !aligned(a->gamma_q_dev, 4) || !aligned(a->gamma_k_dev, 4) || !aligned(a->rope_table_dev, 8)) return BL_ERR_ALIGN;
+    const uint64_t pool = pool_bytes(a->cache);
+    if (overlap(a->cache->k_pages_dev, pool, a->cache->v_pages_dev, pool)) return BL_ERR_SHAPE;
+    const struct { const void* at; uint64_t bytes; } written[3] = {{a->q_out_dev, out_bytes}, {a->cache->k_pages_dev, pool}, {a->cache->v_pages_dev, pool}};
+    for (const auto& w : written)
+        if (overlaps_rows(a->rows, w.at, w.bytes) || (a->gamma_q_dev && overlap(a->gamma_q_dev, (uint64_t)d * 4, w.at, w.bytes)) ||
+            (a->gamma_k_dev && overlap(a->gamma_k_dev, (uint64_t)d * 4, w.at, w.bytes)) ||
+            (a->rope_table_dev && overlap(a->rope_table_dev, (uint64_t)a->rows->max_pos * d * 4, w.at, w.bytes)))
+            return BL_ERR_SHAPE;
     drop_stale_hip_error();
     return shape_status(bl::launch_paged_append(*a, static_cast<hipStream_t>(stream)));
 }
@@ -760,6 +775,9 @@ bl_status bl_attn_paged(const bl_attn_paged_args* a, void* stream) {
     if (overlap(a->q_dev, bytes, a->out_dev, bytes) || overlap(a->scratch_dev, scratch, a->out_dev, bytes) || overlaps_pages(a->cache, a->out_dev, bytes))
         return BL_ERR_SHAPE;
     if (!aligned(a->q_dev, 8) || !aligned(a->out_dev, 8) || !aligned(a->scratch_dev, 256)) return BL_ERR_ALIGN;
+    if (overlap(a->q_dev, bytes, a->scratch_dev, scratch) || overlaps_pages(a->cache, a->scratch_dev, scratch) || overlaps_rows(a->rows, a->scratch_dev, scratch) ||
+        overlaps_rows(a->rows, a->out_dev, bytes))
+        return BL_ERR_SHAPE;
     drop_stale_hip_error();
     return shape_status(bl::launch_attn_paged(*a, static_cast<hipStream_t>(stream)));
 }
