@@ -509,7 +509,8 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  *                   any other call with no greater need.  Calls that may overlap in time must not share it.  It overlaps nothing else of the call
  *                   (BL_ERR_SHAPE, as for out_dev).
  * Arithmetic: fp32 queries and softmax weights enter the products as sums of three bf16 numbers (all 24 bits), bf16 queries as they are with weights as
- * sums of two (single tokens, 16 bits) or rounded to bf16; everything else is fp32 (sums of values by weights of up to 2^8, divided at the end: values
+ * sums of two (16 bits; without start_dev, up to 16 query heads per key head) or rounded to bf16 (2^-8 of a weight at most, as much as
+ * the output's own rounding; whoever wants more bits passes fp32 queries, see q_out_dt of bl_paged_append); everything else is fp32 (sums of values by weights of up to 2^8, divided at the end: values
  * within a walk's length of fp32's largest may overflow).  How a walk is cut, and so the order of sums, follows from all sequences of the call: a row's
  * bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
  * that is not finite makes of the rows that see it what the formula does: a score of NaN or +infinity, or scores of -infinity alone, make the row NaN; the

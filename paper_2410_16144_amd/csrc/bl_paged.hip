@@ -37,7 +37,8 @@ PagedPlan paged_plan(int n_heads, int group, int head_dim, int sequences, int ro
     // heads on 8 at 100 003 positions: one per compute unit 73.8 us, two 79.9; eight sequences of 32 heads, 584 MB: 104.4 and 113.6); but rows of 64 elements
     // and less have half the bytes under way, and many sequences of unlike lengths want smaller parts more than few of them (32 heads on 8 over 60 to
     // 4000 positions: 64 sequences 54.9 us with two per unit, 61.1 with one, 128 97 and 108; of like lengths the same, 88).
-    // Tiles: one per unit, joining is dearer still (600 rows behind 512 of 32 heads: 24 us, for two 40).
+    // Tiles: one per unit, joining is dearer still (for one and for two: 600 rows behind 512 of 32 heads, tiles by two on a unit either way, 24.4 and 38.0 us; 512 behind
+    // 512 19.8 and 33.1; 16 rows of 64 heads on 8 behind 30 000 39 and 57; 300 rows of 32 on 8 behind 8000 84 and 77; 2000 rows of 16 heads of 256 79 and 103).
     r.wanted = r.rows_form && (width <= 64 || (int64_t)sequences * n_heads >= 2 * cus) ? 2 * cus : cus;
     if (r.rows_form) {
         // 128, 256, 512, 1024 positions: 32 heads at 1000 positions 13.4, 14.3, 17.1, 19.0 us; 64 on 8 at 8000 23.7, 19.3, 18.7, 22.9.

@@ -4,11 +4,11 @@
 // the query heads of a key head share what is read of it) against the positions 0 .. its last row's, 64 at a time through a ring of chunks in LDS with one
 // barrier a chunk.  Its four waves are RW sets of 32 rows times 4 / RW shares of a chunk's keys:
 //   * RW = 4, tiles of 128 rows, two workgroups on a compute unit (head sizes up to 128): one is in its products while the other is in its softmax.
-//     4096 rows of 32 heads on 8, 128 wide: 158 us, 870 TFLOP/s; without exponentials, requests and reads of LDS it would be 125,
+//     4096 rows of 32 heads on 8, 128 wide: 155 us, 890 TFLOP/s; without exponentials, requests and reads of LDS it would be 125,
 //     which is what the products alone run at (a library product of 4096 cubed: 1150 TFLOP/s).
 //   * RW = 2, tiles of 64 rows, for fewer, also by two on a unit with a ring of two chunks, or by one with a ring of four (kDepth).  One alone is bound by
 //     the chain of its chunk -- scores, maximum, weights, sums, 0.66 us, of which the products are 0.21 -- with nobody to fill its gaps; eight waves on chunks
-//     of 128 take 0.60 per 64 positions, but 2.5 us more for their longer start and end (512 rows behind 512: 20.9 and 22.7 us), so four it is.
+//     of 128 take 0.60 per 64 positions, but 2.5 us more for their longer start and end (512 rows behind 512: 22.7 us, with four 20.9, since then 19.6), so four it is.
 // Which when: paged_plan.
 //
 // Scores are formed transposed, S^T = K Q^T (v_mfma_f32_32x32x16_bf16): a lane has 16 of 32 keys' weights of ONE row, laid out as the operand of
@@ -26,7 +26,7 @@
 namespace bl {
 
 constexpr int kPagedChunk = 64;
-constexpr float kPagedLargeScore = 1024.0f;   // exponents of two: up to here a maximum's rounding is 2^-14 of one at most
+constexpr float kPagedLargeScore = 1024.0f;   // exponents of two: up to here a maximum's rounding is 2^-15 of one at most
 
 template <int PIECES>
 __device__ __forceinline__ f32x16 paged_mfma32(const s16x8& a, const s16x8 (&b)[PIECES], f32x16 c) {
