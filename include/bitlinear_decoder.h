@@ -515,7 +515,7 @@ bl_status bl_paged_append(const bl_paged_append_args *args, void *stream);
  * bits may differ between calls of different company.  What a row does not see has no part in it, infinities and NaN included; a query, a key or a value
  * that is not finite makes of the rows that see it what the formula does: a score of NaN or +infinity, or scores of -infinity alone, make the row NaN; the
  * weight of a finite score is above zero, however small, that of -infinity is zero, and zero times an infinite value is NaN.  (fp32 queries: an element
- * below 2^-96 in size makes NaN of an infinite key.)  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
+ * below 2^-133 in size may count as zero.)  Page numbers outside 0 .. pages - 1: the rows that see such a page are NaN,
  * other rows of the same sequence in the same call may be.  A call repeated gives the same bits.
  * Errors: BL_ERR_NULL, BL_ERR_SHAPE (also n_q_heads not a multiple of cache->n_heads, a launch of 2^32 threads), BL_ERR_DTYPE, BL_ERR_ALIGN,
  *         BL_ERR_HIP.

@@ -149,14 +149,34 @@ __device__ __forceinline__ PagedSource paged_source(const uint16_t* pool, const 
 }
 
 // Positions behind the sequence's last one come as they lie in their page, or as another sixteen: whatever they are, nobody sees them.  STREAM: by
-// streaming (nontemporal) loads, for a cache that a launch reads once.
-template <int KS, bool STREAM>
+// streaming (nontemporal) loads, for a cache that a launch reads once.  LEAN: a lane's offsets are worked out from one at each request, for kernels that have no
+// registers for eight (from scratch memory each came behind the request before it: 655 rows of 16 heads of 256 on 2 behind 3316 positions, fp32, 395 us, like this 274).
+template <int KS, bool STREAM, bool LEAN = false>
 struct PagedRequest {
-    uint32_t off[PagedTile<KS>::kKept];   // in a sixteen
+    static_assert(!LEAN || KS == 16, "forms in use");
+    uint32_t off[LEAN ? 1 : PagedTile<KS>::kKept];   // in a sixteen
+    bool     value;                                  // LEAN
+    __device__ __forceinline__ uint32_t offset(int s) const {
+        if constexpr (LEAN) {                              // piece s has rows 2 s and 2 s + 1; its places differ from piece 0's by what paged_k_place or paged_v_place make of 2 s
+            uint32_t first = off[0];
+            asm volatile("" : "+v"(first));
+            s %= PagedTile<KS>::kKept;
+            return (first ^ (value ? 128u * (s & 1) : 32u * s)) + 1024u * s;
+        } else {
+            return off[s % PagedTile<KS>::kKept];
+        }
+    }
     template <bool VALUE>
     __device__ __forceinline__ void prepare(int lane) {
+        value = VALUE;
+        if constexpr (LEAN) {
+            int row, byte;
+            paged_piece<KS, VALUE>(0, lane, row, byte);
+            off[0] = (uint32_t)(row * PagedTile<KS>::kRow + byte);
+            return;
+        }
 #pragma unroll
-        for (int s = 0; s < PagedTile<KS>::kKept; ++s) {
+        for (int s = 0; s < (LEAN ? 0 : PagedTile<KS>::kKept); ++s) {
             int row, byte;
             paged_piece<KS, VALUE>(s, lane, row, byte);
             off[s] = (uint32_t)((row & 15) * PagedTile<KS>::kRow + byte);
@@ -171,7 +191,7 @@ struct PagedRequest {
 #pragma clang diagnostic ignored "-Winline-asm"
         if constexpr (PagedTile<KS>::kWhole) {
             const uint8_t* src = uniform_ptr(from.at[2 * s / KS]);
-            const uint32_t o = off[s % PagedTile<KS>::kKept];
+            const uint32_t o = offset(s);
             static_assert(!(ANY && STREAM), "forms in use");
             if constexpr (STREAM)
                 asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(o), "s"(src) : "memory", "m0");
@@ -227,18 +247,6 @@ __device__ __forceinline__ void paged_split(float a, float b, uint32_t (&out)[PI
     }
 }
 
-// A query's three pieces before a key that is infinite: pieces of zero would make NaN of it, where the element itself makes an infinity.  So the lower two
-// are 2^-126 at least, with the element's sign, where the element is 2^-96 or more (what that adds, 2^-29 of a product at most, its rounding takes away).
-__device__ __forceinline__ void paged_no_zero(uint32_t (&pieces)[3]) {   // of two elements
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    const auto halves = [](uint32_t x) { return __builtin_bit_cast(u16x2, x & 0x7fff7fffu); };
-    const u16x2 from = {0x0f00, 0x0f00}, most = {0x0080, 0x0080};   // bf16's 2^-97, 2^-126
-    const u16x2 least = __builtin_elementwise_min(__builtin_elementwise_sub_sat(halves(pieces[0]), from), most);
-#pragma unroll
-    for (int i = 1; i < 3; ++i)
-        pieces[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(halves(pieces[i]), least)) | (pieces[0] & 0x80008000u);
-}
-
 // Eight elements e .. e + 7 of a row's query (zeros from head_dim on and in rows that are not there, whose row_at is another's; head_dim is a multiple of
 // four, e of eight) as operand pieces.  fp32 is loaded by every lane: in a branch, each load would be waited for by its cutting into pieces (12 heads of 64 at
 // position 17: 7.2 us, so 6.7); bf16 has nothing to cut, and idle lanes' loads would cost it 0.3 us.
@@ -262,7 +270,6 @@ __device__ __forceinline__ void paged_query(const void* q, int64_t row_at, int e
             for (int j = 0; j < 2; ++j) {
                 uint32_t two[PIECES];
                 paged_split<PIECES>(in ? x[2 * j] : 0.0f, in ? x[2 * j + 1] : 0.0f, two);
-                paged_no_zero(two);
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) parts[i][2 * h + j] = two[i];
             }
@@ -279,6 +286,28 @@ __device__ __forceinline__ uint32_t paged_exponents(uint32_t most, uint32_t word
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(a, b));
 }
 __device__ __forceinline__ bool paged_not_finite(uint32_t most) { return (most & 0xffffu) == 0x7f80u || most >> 16 == 0x7f80u; }
+
+// Keys before queries of several pieces: a piece of zero times an infinity is NaN, where the query's element makes an infinity of it.  So the keys' numbers that
+// are not finite are multiplied apart, by the elements' signs (of zero: zero).
+__device__ __forceinline__ void paged_apart(const s16x8& k, s16x8& finite, s16x8& odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        odd[i] = (k[i] & 0x7f80) == 0x7f80 ? k[i] : (short)0;
+        finite[i] = k[i] ^ odd[i];
+    }
+}
+template <int PIECES>
+__device__ __forceinline__ s16x8 paged_signs(const s16x8 (&q)[PIECES]) {
+    s16x8 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        short any = 0;
+#pragma unroll
+        for (int n = 0; n < PIECES; ++n) any |= q[n][i] & 0x7fff;
+        r[i] = any ? (short)((q[0][i] & 0x8000) | 0x3f80) : (short)0;
+    }
+    return r;
+}
 
 // Values with infinities and NaN put away: the finite ones, and ones where +infinity (or NaN) and -infinity (or NaN) were.
 __device__ __forceinline__ void paged_put_away(const s16x8& v, s16x8& finite, s16x8& up, s16x8& down) {

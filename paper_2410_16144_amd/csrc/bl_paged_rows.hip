@@ -206,7 +206,18 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
                 s16x8 k = {0, 0, 0, 0, 0, 0, 0, 0};
                 if (KS % 2 == 0 || t + 1 < kSteps || g < 2)
                     k = *reinterpret_cast<const s16x8*>(tile + row * T::kRow + paged_k_place<KS>(row, 4 * t + g) * 16);
-                x[h] = mfma16<PIECES>(k, q[t], x[h]);
+                if (kMasked && !kBf16 && careful) {        // uniform
+                    s16x8 finite, odd;
+                    paged_apart(k, finite, odd);
+                    x[h] = mfma16<PIECES>(finite, q[t], x[h]);
+                    const u32x4 any = __builtin_bit_cast(u32x4, odd);
+                    if (__any((any[0] | any[1] | any[2] | any[3]) != 0)) {
+                        const s16x8 signs[1] = {paged_signs<PIECES>(q[t])};
+                        x[h] = mfma16<1>(odd, signs, x[h]);
+                    }
+                } else {
+                    x[h] = mfma16<PIECES>(k, q[t], x[h]);
+                }
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // every key has left the tile
@@ -304,8 +315,8 @@ __global__ __launch_bounds__(64 * kWaves) void paged_rows_kernel(const PagedArgs
         if (next < c1) req_v.send(paged_source(c.v, base), at_v);
         chunk = next;
     };
-    // The pieces of a weight times an infinity add up to NaN, and so does a weight that is rounded to zero.  So a walk whose sums are not finite is walked again
-    // with such values put away throughout: a value counts by who sees it, not by what is left of its weight.
+    // The pieces of a weight times an infinity add up to NaN, and so do a weight that is rounded to zero and the pieces of a query.  So a walk whose sums are not
+    // finite is walked again with such keys and values apart throughout: a value counts by who sees it, not by what is left of its weight.
     for (bool again = false;; again = true) {
         begin();
         if (!again && chunk < c1 && 32 * chunk + 31 <= s.pos)

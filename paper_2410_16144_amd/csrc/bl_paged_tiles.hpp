@@ -51,6 +51,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     constexpr bool kBf16 = PIECES == 1;
     constexpr int KW = 4 / RW, DT = (KS + 1) / 2;
     constexpr int NB = 2 / KW;                             // a wave's blocks of 32 keys in a chunk
+    constexpr bool kReload = !kBf16 && KS > 8;             // a second walk loads its rows step by step: they take more registers than there are
     static_assert(RW == 4 || RW == 2, "forms");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int odd_chunk, odd_sums, bad_page, last_one;
@@ -77,16 +78,22 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     const int wave_low = t.s.pos + uniform((t.row0 + rw * 32) / p.group);
     const int wave_high = rw * 32 < t.rows ? t.s.pos + uniform((t.row0 + min(rw * 32 + 31, t.rows - 1)) / p.group) : -1;
     s16x8 q[KS][PIECES];
-    {
+    const auto load_step = [&](int ks) __attribute__((always_inline)) {
+        paged_query<PIECES>(p.q, there ? paged_row_at(p, t, row) : 0, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
+    };
+    const auto load_rows = [&]() __attribute__((always_inline)) {
         const int64_t row_at = there ? paged_row_at(p, t, row) : 0;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) paged_query<PIECES>(p.q, row_at, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
-    }
+        for (int ks = 0; ks < KS; ++ks)
+            if constexpr (kReload) load_step(ks);
+            else paged_query<PIECES>(p.q, row_at, 16 * ks + 8 * g, c.head_dim, there, q[ks]);
+    };
+    load_rows();
 
     // waves 0 and 1 bring a chunk's keys, 2 and 3 its values, 32 positions each
     const bool value = wave >= 2;
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * T::kBytes);
-    PagedRequest<KS, false> req;
+    PagedRequest<KS, false, !kBf16 && KS == 16> req;
     if (value) req.template prepare<true>(lane);
     else req.template prepare<false>(lane);
     const auto first_of = [&](int chunk) { return min(chunk, c1) * kPagedChunk + 32 * (wave & 1); };
@@ -137,9 +144,11 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     };
     f32x16 o[DT];
     float run_m, run_l;                                    // run_l: over this lane half's keys only
-    int v_at[DT];                                          // of the transposing reads
+    // Of the transposing reads: pieces 4 d .. 4 d + 3 trade places among kMoved times 32 elements, what lies beyond is a constant away.
+    constexpr int kMoved = KS % 8 == 0 ? 4 : KS % 4 == 0 ? 2 : KS % 2 == 0 ? 1 : DT;
+    int v_at[kMoved];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
+    for (int d = 0; d < kMoved; ++d) {
         const int key = 4 * g + ((lane & 15) >> 2);
         int piece = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
         if (piece >= 2 * KS) piece = 0;                    // an odd KS: the last 16 elements are never stored
@@ -149,25 +158,32 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
     // Chunks that every row of the tile sees whole, then those that end among the rows' own positions.  (The first kind's code lies side by side: a jump
     // costs as much as two products.)
     // `sure`: chunks whose request, kDepth - 1 chunks on, is there to be made, so that it is known how many requests are behind the chunk's own.
-    // `again`: of the second kind, a walk that was not right the first time (below).
-    const auto walk = [&](int chunk, auto which, auto sure, bool again) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(which)::value, kSure = decltype(sure)::value;
+    // `again`: of the second kind, a walk that was not right the first time (below); code of its own, or the others would be 2 % slower for it.
+    const auto walk = [&](int chunk, auto which, auto sure, auto again) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(which)::value, kSure = decltype(sure)::value, kAgain = decltype(again)::value;
         const int j0 = chunk * kPagedChunk;
         const uint8_t* ring = lds + (chunk & (kDepth - 1)) * (4 * T::kBytes);
         wait_vm<kSure ? (kDepth - 2) * KS : 0>();
         __syncthreads();                                   // the chunk is here, and nobody reads the one before it any more
         if constexpr (kSure) prepare(chunk + kDepth - 1);
         else prepare_if(chunk + kDepth - 1);
-        // Weights of zero may stand before values that a row does not see; infinities and NaN among those are put away and noted.  What lies behind the
-        // sequence's last row is nobody's: zero.
+        // Weights of zero may stand before values that a row does not see.  What lies behind the sequence's last row is nobody's: zero.  Infinities and NaN elsewhere
+        // make sums that are not finite, and the second walk puts them away and notes them.
         bool careful = false;
         if constexpr (kMasked) {
             uint8_t* values = lds + (ring - lds) + 2 * T::kBytes;
-            uint32_t most = 0;
-            const int end = min(kPagedChunk, t.reach - j0) * T::kRow;
+            const int end = min(kPagedChunk, t.reach - j0) * T::kRow;   // (uniform)
+            if (end < 2 * T::kBytes) {
 #pragma unroll 1
-            for (int i = end + tid * 16; i < 2 * T::kBytes; i += 256 * 16) *reinterpret_cast<u32x4*>(values + i) = u32x4{0, 0, 0, 0};
-            for (int i = tid * 16; i < end; i += 256 * 16) {
+                for (int i = end + tid * 16; i < 2 * T::kBytes; i += 256 * 16) *reinterpret_cast<u32x4*>(values + i) = u32x4{0, 0, 0, 0};
+                __syncthreads();
+            }
+        }
+        if constexpr (kAgain) {
+            uint8_t* values = lds + (ring - lds) + 2 * T::kBytes;
+            uint32_t most = 0;
+#pragma unroll 1
+            for (int i = tid * 16; i < 2 * T::kBytes; i += 256 * 16) {
                 const u32x4 x = *reinterpret_cast<const u32x4*>(values + i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = paged_exponents(most, x[j]);
@@ -214,7 +230,19 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
             for (int i = 0; i < kReads; ++i) {
                 const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                x[i % NB] = paged_mfma32<PIECES>(k[i % kAhead], q[i / NB], i < NB ? zero : x[i % NB]);
+                if constexpr (kAgain && !kBf16) {
+                    if (kReload && i % NB == 0) load_step(i / NB);
+                    s16x8 finite, odd;
+                    paged_apart(k[i % kAhead], finite, odd);
+                    x[i % NB] = paged_mfma32<PIECES>(finite, q[i / NB], i < NB ? zero : x[i % NB]);
+                    const u32x4 any = __builtin_bit_cast(u32x4, odd);
+                    if (__any((any[0] | any[1] | any[2] | any[3]) != 0)) {
+                        const s16x8 signs[1] = {paged_signs<PIECES>(q[i / NB])};
+                        x[i % NB] = paged_mfma32<1>(odd, signs, x[i % NB]);
+                    }
+                } else {
+                    x[i % NB] = paged_mfma32<PIECES>(k[i % kAhead], q[i / NB], i < NB ? zero : x[i % NB]);
+                }
                 if (i + kAhead < kReads) k[i % kAhead] = read_k(i + kAhead);
                 send_at(i, sure);
                 __builtin_amdgcn_sched_barrier(0);
@@ -222,7 +250,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             // the first sixteen keys' value operands travel under the softmax
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const auto read_v = [&](int n, int d) __attribute__((always_inline)) {        // 16 keys, 32 elements
-                const uint8_t* at = values + v_at[d] + n * 16 * T::kRow;
+                const uint8_t* at = values + v_at[d % kMoved] + d / kMoved * (64 * kMoved) + n * 16 * T::kRow;
                 const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
                 const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * T::kRow));
                 return s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
@@ -239,7 +267,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                     for (int r = 0; r < 16; ++r)
                         if (32 * n + 8 * (r >> 2) + (r & 3) > seen) x[n][r] = -INFINITY;
             }
-            if (kMasked && careful) {                      // of the keys that the row sees; both, which is NaN, where the score is -infinity and the weight zero
+            if (kAgain && careful) {                       // of the keys that the row sees; both, which is NaN, where the score is -infinity and the weight zero
                 asm volatile("");                          // (a branch: else every chunk pays for it)
                 const int seen = limit - j1 - 4 * g;
 #pragma unroll
@@ -279,9 +307,9 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 run_m = m_new;
             }
             float ref = run_m == -INFINITY ? 0.0f : run_m * p.scale;         // (a row that has seen nothing yet)
-            const float off = kMasked && again && fabsf(ref) > kPagedLargeScore ? run_m : 0.0f;
-            if (kMasked && off != 0.0f) ref = 0.0f;
-            const auto exponent = [&](float score) { return fmaf(kMasked ? score - off : score, p.scale, -ref); };
+            const float off = kAgain && fabsf(ref) > kPagedLargeScore ? run_m : 0.0f;
+            if (kAgain && off != 0.0f) ref = 0.0f;
+            const auto exponent = [&](float score) { return fmaf(kAgain ? score - off : score, p.scale, -ref); };
             const auto weights = [&](int n, s16x8 (&w)[PIECES]) __attribute__((always_inline)) {   // of 16 keys
                 uint32_t words[PIECES][4];
 #pragma unroll
@@ -317,7 +345,7 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
                 if (n + 1 < 2 * NB) weights(n + 1, w[(n + 1) & 1]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (kMasked && careful) {                      // (lane and lane + 32 have the row's keys between them)
+            if (kAgain && careful) {                       // (lane and lane + 32 have the row's keys between them)
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (each has read nothing yet of what the other wrote)
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -336,11 +364,10 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
             req.template send<!kSure>(next, next_at, pieces);
         }
     };
-    // A weight's pieces times an infinity add up to NaN, as a weight of zero does.  So a walk whose sums are not finite is walked again with such values put
-    // away throughout.  So is one with a large maximum, whose product with the scale is rounded by as much as exponents count (from 2^31 on beyond fp32's
+    // A weight's pieces times an infinity add up to NaN, as a weight of zero does, and so do a query's.  So a walk whose sums are not finite is walked again with
+    // such keys and values apart throughout.  So is one with a large maximum, whose product with the scale is rounded by as much as exponents count (from 2^31 on beyond fp32's
     // largest): there, row by row, the difference is formed first.  (In every chunk of the first walk that costs 2 % of a long prompt.)
-    bool again = false;
-    for (int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);; plain = c0, again = true) {
+    const auto attempt = [&](auto again) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < kDepth - 1; ++i) {
             prepare_if(c0 + i);
@@ -353,24 +380,29 @@ __global__ __launch_bounds__(256, KS <= 8 && (PIECES == 1 || KS <= 4) ? 2 : 1) v
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
         int chunk = c0;
-        for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{}, false);
-        for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{}, false);
-        for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{}, again);
-        if (!again) {
-            bool odd = run_m != -INFINITY && fabsf(run_m * p.scale) > kPagedLargeScore;
-            if (plain > c0) {
-                float sums = 0.0f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sums = fmaf(o[d][r], 0.0f, sums);
-                odd = odd || sums != sums;
-            }
-            if (odd) odd_sums = 1;
+        if constexpr (!decltype(again)::value) {
+            const int plain = min(max(uniform((t.low + 1) / kPagedChunk), c0), c1);
+            for (const int sure = min(plain, c1 - (kDepth - 1)); chunk < sure; ++chunk) walk(chunk, std::false_type{}, std::true_type{}, again);
+            for (; chunk < plain; ++chunk) walk(chunk, std::false_type{}, std::false_type{}, again);
         }
-        __syncthreads();
-        if (again || !uniform(odd_sums)) break;
+        for (; chunk < c1; ++chunk) walk(chunk, std::true_type{}, std::false_type{}, again);
+    };
+    attempt(std::false_type{});
+    {
+        f32x4 sums = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sums[r & 3] = fmaf(o[d][r], 0.0f, sums[r & 3]);
+        const float any = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        if (any != any || (run_m != -INFINITY && fabsf(run_m * p.scale) > kPagedLargeScore)) odd_sums = 1;
+    }
+    __syncthreads();
+    if (__builtin_expect(uniform(odd_sums), 0)) {
         look(c0);
+        if constexpr (KS <= 8) load_rows();                // (again: kept across the first walk they would cost its registers)
+        attempt(std::true_type{});
+        __syncthreads();
     }
     run_l = over_blocks<32>(run_l, AddOp());
     if (uniform(bad_page)) run_l = NAN;                             // (rows of a sequence whose table names a page that is not there)

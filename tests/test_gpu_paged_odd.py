@@ -249,3 +249,25 @@ def test_what_nobody_wrote_costs_nothing(dev, dec, heads, new, before, dtype):
     (zeros, a), (nans, b) = time(0.0), time(NAN)
     assert torch.equal(a, b)
     assert nans <= 1.2 * zeros, (nans, zeros)
+
+
+@pytest.mark.parametrize("power", [12, 20, 33])
+@pytest.mark.parametrize("d", [4, 12, 48, 64, 128, 256])
+@pytest.mark.parametrize("before,new,heads", [(0, 14, 32), (3, 60, 8), (40, 1, 8), (40, 1, 36), (700, 9, 4)])
+@pytest.mark.parametrize("dtype", [F, G])
+def test_equal_scores_weigh_the_same(dev, dec, power, d, before, new, heads, dtype):
+    """Every key makes the same score, a small one of large terms that cancel: exact in every order of its sums, if nothing is added to them that is not there.  The outputs are the
+    means of what the rows see, to the roundings of test_scores_of_any_size."""
+    srv, k, v = _sequence(dec, dev, d, before, new, seed=7)
+    k = torch.zeros((before + new, 2, d))
+    for j in range(before + new):
+        for h in range(2):
+            one, two, three = torch.randperm(d, generator=srv.g)[:3].tolist()
+            k[j, h, one] = int(torch.randint(1, 121, (1,), generator=srv.g))
+            k[j, h, two], k[j, h, three] = -k[j, h, one], -1.0
+    q = torch.full((new, heads, d), 2.0 ** power)
+    out, qd, seen = _attend(dec, dev, srv, q, k.to(G), v, before, new, dtype, new == 1, heads // 2)
+    want, plain, S, V = formula(qd, srv.k[0], srv.v[0], heads // 2, seen)
+    got = out.double().cpu().view_as(want)
+    worst = ((got - want).abs().amax(-1) / V).max().item()
+    assert worst <= (2 * H if dtype == G else 0) + 40 * U
